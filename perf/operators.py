@@ -528,7 +528,7 @@ def run(s):
     if c["what"] == "fork":
         brq.kv4_pages_fork(s["pool"], table, lens, refs, s["parents"], s["children"])
         brq.kv4_pages_free(table, lens, refs, s["parents"])
-        brq.kv4_pages_reserve(table, lens, refs, s["children"], s["more"])
+        brq.kv4_pages_reserve(table, refs, s["children"], s["more"])
         return [s["pool"], table, lens, refs]
     brq.kv4_pages_free(table, lens, refs, s["gone"])
     live = brq.kv4_pages_compact(s["pool"], table, refs)
