@@ -24,7 +24,9 @@ LAYOUTS = {"rowmajor": 0, "tiled": 1}
 EXPORTS = ["brq_init", "brq_block_rotate", "brq_operand_bytes", "brq_mxfp4_quantize", "brq_rotate_quantize_fused",
            "brq_swiglu", "brq_swiglu_rotate_quantize_fused", "brq_matrix_rotate",
            "brq_matrix_rotate_quantize_fused", "brq_block_stats", "brq_block_stats_summary", "brq_mxfp4_gemm", "brq_rotate_quantize_gemm_fused", "brq_to_rowmajor", "brq_diag_mfma_ceiling", "brq_diag_mxfp4_gemm_clock", "brq_diag_mxfp4_gemm_no_loads", "brq_diag_mxfp4_gemm_route",
-           "brq_diag_mxfp4_gemm_on", "brq_strerror", "brq_version"]
+           "brq_diag_mxfp4_gemm_on", "brq_qk_norm_rope", "brq_qk_norm_rope_backward", "brq_qk_norm_rope_backward_workspace", "brq_kv4_page_bytes",
+           "brq_kv4_append", "brq_kv4_read", "brq_kv4_attention", "brq_kv4_attention_workspace", "brq_kv4_pages_workspace", "brq_kv4_pages_copy",
+           "brq_kv4_pages_fork", "brq_kv4_pages_free", "brq_kv4_pages_reserve", "brq_kv4_pages_compact", "brq_strerror", "brq_version"]
 
 _lib = None
 _native = None          # the compiled marshalling, its entry points bound to those of _lib; None: not loaded
@@ -81,6 +83,7 @@ def lib():
         L.brq_diag_mxfp4_gemm_on.restype = i32
         L.brq_diag_mfma_ceiling.argtypes = [vp, i64, i64, vp, vp]
         L.brq_diag_mfma_ceiling.restype = i32
+        _attention.declare(L)
         L.brq_init.restype = i32
         L.brq_strerror.argtypes = [i32]
         L.brq_strerror.restype = ctypes.c_char_p
@@ -531,3 +534,9 @@ def diag_mfma_ceiling(operands, iters, workgroups, sink=None, stream=None):
         raise ValueError("sink must be a contiguous float32 GPU tensor of workgroups * 256 elements")
     _check(lib().brq_diag_mfma_ceiling(operands.data_ptr(), iters, workgroups, sink.data_ptr(), _stream(stream)))
     return workgroups * 4 * iters * 16 * 131072
+
+
+from . import attention as _attention          # noqa: E402  (at the end: it uses what is above)
+from .attention import (kv4_append, kv4_attention, kv4_attention_workspace, kv4_page_bytes, kv4_pages_compact, kv4_pages_copy,  # noqa: E402,F401
+                        kv4_pages_fork, kv4_pages_free, kv4_pages_reserve, kv4_pages_workspace, kv4_read, qk_norm_rope,
+                        qk_norm_rope_backward, qk_norm_rope_backward_workspace)

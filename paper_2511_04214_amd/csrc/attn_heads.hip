@@ -1,0 +1,421 @@
+// Passes over query, key and value heads: RMS norm, rotation by position and block rotation in one pass, its backward
+// pass, the same in front of the MXFP4 quantizer that writes the cache, and the cache's values read back.
+//
+// A head of D channels is held by L = D/8 lanes, 8 channels each; a wavefront holds 64/L heads.  The lanes hold the
+// chunks in the order of chunk_of_lane (brq_device.h), in which both the block rotation's wide stages and the
+// partner of a rotation by position over the whole head are DPP reads of the mirror image.
+#include "brq_attn.h"
+#include "brq_device.h"
+#include "brq_launch.h"
+
+namespace brq {
+namespace {
+
+// Lane of a head's lanes that holds chunk c: the inverse of chunk_of_lane.
+__device__ __forceinline__ uint32_t lane_of_chunk(uint32_t c) {
+    const uint32_t b2 = ((c >> 2) ^ (c >> 3)) & 1u;
+    return (c & 24u) | (b2 << 2) | ((c & 3u) ^ (b2 ? 3u : 0u));
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    const int i = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, CTRL, 0xF, 0xF, true));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror16 = 0x140, kMirror8 = 0x141;
+
+// Sum over the L lanes of a head, every lane receiving it.
+template <int L>
+__device__ __forceinline__ float head_sum(float v) {
+    v += dpp<kXor1>(v);
+    v += dpp<kXor2>(v);
+    v += dpp<kMirror8>(v);
+    if constexpr (L >= 16) v += dpp<kMirror16>(v);
+    if constexpr (L >= 32) v += __shfl_xor(v, 16);
+    return v;
+}
+
+// H_B / sqrt(B) on each B channels of the head; 2^l2b <= 8 L.
+template <int L>
+__device__ __forceinline__ void rotate_block(float (&v)[8], int l2b, uint32_t chunk) {
+    float s = 1.0f;
+    switch (l2b) {
+        case 0: return;
+        case 3: wht_inwave<3>(v, chunk); s = wht_sign<3>(chunk) * 0.35355339059327373f; break;
+        case 4: wht_inwave<4>(v, chunk); s = wht_sign<4>(chunk) * 0.25f; break;
+        case 5: wht_inwave<5>(v, chunk); s = wht_sign<5>(chunk) * 0.17677669529663687f; break;
+        case 6: wht_inwave<6>(v, chunk); s = wht_sign<6>(chunk) * 0.125f; break;
+        case 7: if constexpr (L >= 16) { wht_inwave<7>(v, chunk); s = wht_sign<7>(chunk) * 0.08838834764831843f; } break;
+        case 8: if constexpr (L >= 32) { wht_inwave<8>(v, chunk); s = wht_sign<8>(chunk) * 0.0625f; } break;
+        default: break;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= s;
+}
+
+// The rotation of one token as a lane needs it: y = c v + s partner.
+struct Turn {
+    float c[8], s[8];
+    __device__ __forceinline__ void load(const Rope& r, int64_t row, uint32_t chunk, bool back) {
+        const int half = r.rot >> 1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
+        if ((int)chunk * 8 >= r.rot) return;
+        if (r.interleaved) {
+            const v4f cc = *reinterpret_cast<const v4f*>(r.cos + row * half + chunk * 4);
+            const v4f ss = *reinterpret_cast<const v4f*>(r.sin + row * half + chunk * 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                c[i] = cc[i >> 1];
+                s[i] = ((i & 1) != 0) != back ? ss[i >> 1] : -ss[i >> 1];
+            }
+        } else {
+            const bool second = (int)chunk * 8 >= half;
+            const int64_t at = row * half + (second ? (int)chunk * 8 - half : (int)chunk * 8);
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+                const v4f cc = *reinterpret_cast<const v4f*>(r.cos + at + j), ss = *reinterpret_cast<const v4f*>(r.sin + at + j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    c[j + i] = cc[i];
+                    s[j + i] = second != back ? ss[i] : -ss[i];
+                }
+            }
+        }
+    }
+    template <int L>
+    __device__ __forceinline__ void apply(float (&v)[8], const Rope& r, uint32_t lane, uint32_t chunk) const {
+        float p[8];
+        if (r.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = v[i ^ 1];
+        } else if (L <= 16 && r.rot == L * 8) {      // the whole head: the partner is the mirror image
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = L == 16 ? dpp<kMirror16>(v[i]) : dpp<kMirror8>(v[i]);
+        } else {
+            const int n = r.rot >> 4;                // chunks of a half
+            const int other = (int)chunk < n ? (int)chunk + n : (int)chunk < 2 * n ? (int)chunk - n : (int)chunk;
+            const int src = (int)((lane & ~(uint32_t)(L - 1)) | lane_of_chunk((uint32_t)other));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = __shfl(v[i], src);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(p[i], s[i], v[i] * c[i]);
+    }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void store_chunk(uint8_t* p, const float (&v)[8]) {
+    if constexpr (BF16) {
+        *reinterpret_cast<v4i*>(p) = v4i{(int)pack_bf16x2(v[0], v[1]), (int)pack_bf16x2(v[2], v[3]), (int)pack_bf16x2(v[4], v[5]),
+                                        (int)pack_bf16x2(v[6], v[7])};
+    } else {
+        *reinterpret_cast<v4f*>(p) = v4f{v[0], v[1], v[2], v[3]};
+        *(reinterpret_cast<v4f*>(p) + 1) = v4f{v[4], v[5], v[6], v[7]};
+    }
+}
+
+__device__ __forceinline__ void load_weight(const float* w, uint32_t chunk, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 1.0f;
+    if (w) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = w[chunk * 8 + i];
+    }
+}
+
+__device__ __forceinline__ float sum_squares(const float (&v)[8]) {
+    float a = v[0] * v[0], b = v[1] * v[1];
+#pragma unroll
+    for (int i = 2; i < 8; i += 2) {
+        a = __builtin_fmaf(v[i], v[i], a);
+        b = __builtin_fmaf(v[i + 1], v[i + 1], b);
+    }
+    return a + b;
+}
+
+// One wavefront: token t, the groups part, part + splits, ... of 64/L heads; queries first, then keys, then values.
+template <int L, bool IN_BF16, bool OUT_BF16, bool APPEND>
+__global__ __launch_bounds__(256) void k_heads(const HeadsArgs a, int splits) {
+    constexpr int D = L * 8, HPW = 64 / L, ES = IN_BF16 ? 2 : 4, OS = OUT_BF16 ? 2 : 4;
+    const uint32_t lane = threadIdx.x & 63u, l = lane & (L - 1), chunk = chunk_of_lane(l);
+    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t t = wave / splits;
+    const int part = (int)(wave - t * splits);
+    if (t >= a.T) return;
+    const int nq = (a.q.n + HPW - 1) / HPW, nk = (a.k.n + HPW - 1) / HPW, nv = APPEND ? (a.v.n + HPW - 1) / HPW : 0;
+    bool placed = true;
+    Turn turn;
+    if (a.rope.rot) {
+        const int64_t row = a.rope.pos[t];
+        placed = row >= 0 && row < a.rope.rows;
+        turn.load(a.rope, placed ? row : 0, chunk, false);
+    }
+    int64_t slot = -1;
+    if constexpr (APPEND) slot = a.slots[t];
+    const bool write = placed && slot >= 0 && slot < a.num_slots;
+    const int in_page = (int)(slot & (kKv4Page - 1));
+    for (int it = part; it < nq + nk + nv; it += splits) {
+        const bool is_q = it < nq, is_v = it >= nq + nk;
+        const Heads& src = is_q ? a.q : is_v ? a.v : a.k;
+        const int h = (it - (is_q ? 0 : is_v ? nq + nk : nq)) * HPW + (int)(lane / L);
+        const bool there = h < src.n;
+        float v[8];
+        load_chunk<IN_BF16>(src.p + t * src.ts + (there ? h : 0) * src.hs + chunk * 8 * ES, v);
+        if (!is_v) {
+            const float* wp = is_q ? a.wq : a.wk;
+            if (wp) {
+                float w[8];
+                load_weight(wp, chunk, w);
+                const float r = __builtin_amdgcn_rsqf(head_sum<L>(sum_squares(v)) * (1.0f / D) + a.eps);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = v[i] * r * w[i];
+            }
+            if (a.rope.rot) turn.apply<L>(v, a.rope, lane, chunk);
+            rotate_block<L>(v, a.l2b, chunk);
+        } else {
+            rotate_block<L>(v, a.l2bv, chunk);
+        }
+        if (!APPEND || is_q) {
+            const Heads& dst = is_q ? a.qo : a.ko;
+            if (!placed) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = as_f32(0x7fc00000u);
+            }
+            if (there) store_chunk<OUT_BF16>(dst.p + t * dst.ts + h * dst.hs + chunk * 8 * OS, v);
+        }
+        if constexpr (APPEND) {
+            if (!is_q) {
+                const uint32_t sb = e8m0_from_amax(quad_max(absmax8(v)));
+                const uint32_t codes = encode8_e2m1(v, sb);
+                if (write && there) {
+                    uint8_t* head = a.pool + ((slot / kKv4Page) * a.Hk + h) * kv4_head_bytes(D);
+                    if (!is_v) {
+                        *reinterpret_cast<uint32_t*>(head + kv4_key_code(D, in_page) + chunk * 4) = codes;
+                        if ((l & 3u) == 0) head[kv4_key_scale(D, in_page, (int)(chunk >> 2))] = (uint8_t)sb;
+                    } else {
+                        if constexpr (D == 128) {
+                            *reinterpret_cast<uint32_t*>(head + kv4_value_code(D, in_page, (int)chunk)) = codes;
+                        } else {
+                            *reinterpret_cast<uint16_t*>(head + kv4_value_code(D, in_page, (int)chunk * 2)) = (uint16_t)codes;
+                            *reinterpret_cast<uint16_t*>(head + kv4_value_code(D, in_page, (int)chunk * 2 + 1)) = (uint16_t)(codes >> 16);
+                        }
+                        if ((l & 3u) == 0) head[kv4_value_scale(D, in_page, (int)(chunk >> 2))] = (uint8_t)sb;
+                    }
+                }
+            }
+        }
+    }
+}
+
+// Wavefronts of a launch: as many to a token as make about 8 for every SIMD together, at most one for each group of heads.
+int token_splits(int64_t T, int groups) {
+    const int64_t want = (8192 + T - 1) / T;
+    return (int)(want < groups ? want : groups);
+}
+
+}  // namespace
+
+hipError_t launch_heads(int D, bool in_bf16, bool out_bf16, bool append, const HeadsArgs& a, hipStream_t stream) {
+    const int hpw = 512 / D;
+    const int groups = (a.q.n + hpw - 1) / hpw + (a.k.n + hpw - 1) / hpw + (append ? (a.v.n + hpw - 1) / hpw : 0);
+    const int splits = token_splits(a.T, groups);
+    const dim3 grid((uint32_t)((a.T * splits + 3) / 4)), block(256);
+#define BRQ_HEADS(L_, IN, OUT, APP) hipLaunchKernelGGL((k_heads<L_, IN, OUT, APP>), grid, block, 0, stream, a, splits)
+#define BRQ_HEADS_T(L_)                                                        \
+    do {                                                                       \
+        if (in_bf16 && out_bf16) BRQ_HEADS(L_, true, true, false);             \
+        else if (in_bf16) BRQ_HEADS(L_, true, false, false);                   \
+        else if (out_bf16) BRQ_HEADS(L_, false, true, false);                  \
+        else BRQ_HEADS(L_, false, false, false);                               \
+    } while (0)
+    if (append) {
+        if (D == 64) { if (in_bf16) BRQ_HEADS(8, true, true, true); else BRQ_HEADS(8, false, false, true); }
+        else { if (in_bf16) BRQ_HEADS(16, true, true, true); else BRQ_HEADS(16, false, false, true); }
+    } else if (D == 64) BRQ_HEADS_T(8);
+    else if (D == 128) BRQ_HEADS_T(16);
+    else BRQ_HEADS_T(32);
+#undef BRQ_HEADS_T
+#undef BRQ_HEADS
+    return hipGetLastError();
+}
+
+namespace {
+
+// Backward.  A wavefront goes through (token, part) items with a stride and keeps both weights' gradients for its
+// lanes' channels in registers; a workgroup adds its wavefronts' up in LDS and writes one row of partial sums.
+template <int L, bool X_BF16, bool G_BF16>
+__global__ __launch_bounds__(256) void k_heads_backward(const HeadsArgs a, int splits) {
+    constexpr int D = L * 8, HPW = 64 / L, ES = X_BF16 ? 2 : 4, GS = G_BF16 ? 2 : 4;
+    const uint32_t lane = threadIdx.x & 63u, l = lane & (L - 1), chunk = chunk_of_lane(l);
+    const int nq = (a.q.n + HPW - 1) / HPW, nk = (a.k.n + HPW - 1) / HPW;
+    float wq[8], wk[8], dw[2][8] = {};
+    load_weight(a.wq, chunk, wq);
+    load_weight(a.wk, chunk, wk);
+    const int64_t items = a.T * splits;
+    for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
+        const int64_t t = item / splits;
+        const int part = (int)(item - t * splits);
+        Turn turn;
+        bool placed = true;
+        if (a.rope.rot) {
+            const int64_t row = a.rope.pos[t];
+            placed = row >= 0 && row < a.rope.rows;
+            turn.load(a.rope, placed ? row : 0, chunk, true);
+        }
+        for (int it = part; it < nq + nk; it += splits) {
+            const bool is_q = it < nq;
+            const Heads &src = is_q ? a.q : a.k, &gs = is_q ? a.gq : a.gk, &dst = is_q ? a.qo : a.ko;
+            const int h = (is_q ? it : it - nq) * HPW + (int)(lane / L);
+            const bool there = h < src.n;
+            float g[8];
+            load_chunk<G_BF16>(gs.p + t * gs.ts + (there ? h : 0) * gs.hs + chunk * 8 * GS, g);
+            rotate_block<L>(g, a.l2b, chunk);
+            if (a.rope.rot) turn.apply<L>(g, a.rope, lane, chunk);
+            if (!placed) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] = as_f32(0x7fc00000u);
+            }
+            if (is_q ? a.wq != nullptr : a.wk != nullptr) {
+                float x[8], y[8];
+                load_chunk<X_BF16>(src.p + t * src.ts + (there ? h : 0) * src.hs + chunk * 8 * ES, x);
+                const float r = __builtin_amdgcn_rsqf(head_sum<L>(sum_squares(x)) * (1.0f / D) + a.eps);
+                float dot = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] *= r;                                                // u = x / rms
+                    y[i] = g[i] * (is_q ? wq[i] : wk[i]);
+                    dot = __builtin_fmaf(y[i], x[i], dot);
+                    const float gu = there ? g[i] * x[i] : 0.0f;
+                    if (is_q) dw[0][i] += gu; else dw[1][i] += gu;
+                }
+                const float mean = head_sum<L>(dot) * (1.0f / D);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] = r * (y[i] - x[i] * mean);
+            }
+            if (there) store_chunk<X_BF16>(dst.p + t * dst.ts + h * dst.hs + chunk * 8 * ES, g);
+        }
+    }
+    if (!a.partial) return;
+    __shared__ float sum[4][2][D];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float v = dw[n][i];
+#pragma unroll
+            for (int m = L; m < 64; m *= 2) v += __shfl_xor(v, m);
+            if (lane < (uint32_t)L) sum[threadIdx.x >> 6][n][chunk * 8 + i] = v;
+        }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * D; c += 256) {
+        const float* s = &sum[0][0][0] + c;
+        a.partial[(int64_t)blockIdx.x * (2 * D) + c] = (s[0] + s[2 * D]) + (s[4 * D] + s[6 * D]);
+    }
+}
+
+// Sums of the partial sums' columns: 16 columns a workgroup, 16 threads each.
+__global__ __launch_bounds__(256) void k_heads_weight_grads(const float* partial, int rows, int D, float* dwq, float* dwk) {
+    __shared__ float sum[16][17];
+    const int c = (int)blockIdx.x * 16 + (int)(threadIdx.x & 15u), r0 = (int)(threadIdx.x >> 4);
+    float v = 0.0f;
+#pragma unroll 8
+    for (int r = r0; r < rows; r += 16) v += partial[(int64_t)r * (2 * D) + c];
+    sum[r0][threadIdx.x & 15u] = v;
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        float s = 0.0f;
+        for (int i = 0; i < 16; ++i) s += sum[i][threadIdx.x];
+        float* out = c < D ? dwq : dwk;
+        if (out) out[c < D ? c : c - D] = s;
+    }
+}
+
+}  // namespace
+
+int64_t heads_backward_workgroups(int64_t T, int Hq, int Hk, int D) {
+    const int hpw = 512 / D, groups = (Hq + hpw - 1) / hpw + (Hk + hpw - 1) / hpw;
+    const int64_t n = (T * token_splits(T, groups) + 3) / 4;
+    return n < 1024 ? n : 1024;
+}
+
+hipError_t launch_heads_backward(int D, bool x_bf16, bool g_bf16, const HeadsArgs& a, hipStream_t stream) {
+    const int hpw = 512 / D, groups = (a.q.n + hpw - 1) / hpw + (a.k.n + hpw - 1) / hpw;
+    const int splits = token_splits(a.T, groups);
+    const int wgs = (int)heads_backward_workgroups(a.T, a.q.n, a.k.n, D);
+#define BRQ_BACK(L_, X, G) hipLaunchKernelGGL((k_heads_backward<L_, X, G>), dim3(wgs), dim3(256), 0, stream, a, splits)
+#define BRQ_BACK_T(L_)                                          \
+    do {                                                        \
+        if (x_bf16 && g_bf16) BRQ_BACK(L_, true, true);         \
+        else if (x_bf16) BRQ_BACK(L_, true, false);             \
+        else if (g_bf16) BRQ_BACK(L_, false, true);             \
+        else BRQ_BACK(L_, false, false);                        \
+    } while (0)
+    if (D == 64) BRQ_BACK_T(8);
+    else if (D == 128) BRQ_BACK_T(16);
+    else BRQ_BACK_T(32);
+#undef BRQ_BACK_T
+#undef BRQ_BACK
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.partial) return e;
+    return launch_heads_weight_grads(a.partial, wgs, D, a.dwq, a.dwk, stream);
+}
+
+hipError_t launch_heads_weight_grads(const float* partial, int rows, int D, float* dwq, float* dwk, hipStream_t stream) {
+    hipLaunchKernelGGL(k_heads_weight_grads, dim3(2 * D / 16), dim3(256), 0, stream, partial, rows, D, dwq, dwk);
+    return hipGetLastError();
+}
+
+namespace {
+
+// A thread reads back 8 channels of keys and of values of one token and head.
+template <int D, bool OUT_BF16>
+__global__ __launch_bounds__(256) void k_kv4_read(const uint8_t* pool, int64_t num_slots, int Hk, int64_t T, const int64_t* slots, Heads k, Heads v) {
+    constexpr int L = D / 8, OS = OUT_BF16 ? 2 : 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, th = i / L, t = th / Hk;
+    const int chunk = (int)(i % L), h = (int)(th - t * Hk);
+    if (t >= T) return;
+    const int64_t slot = slots[t];
+    float x[2][8];
+    if (slot >= 0 && slot < num_slots) {
+        const int p = (int)(slot & (kKv4Page - 1));
+        const uint8_t* head = pool + ((slot / kKv4Page) * Hk + h) * kv4_head_bytes(D);
+        uint32_t c[2], s[2];
+        c[0] = *reinterpret_cast<const uint32_t*>(head + kv4_key_code(D, p) + chunk * 4);
+        s[0] = head[kv4_key_scale(D, p, chunk >> 2)];
+        if constexpr (D == 128) {
+            c[1] = *reinterpret_cast<const uint32_t*>(head + kv4_value_code(D, p, chunk));
+        } else {
+            c[1] = *reinterpret_cast<const uint16_t*>(head + kv4_value_code(D, p, chunk * 2)) |
+                   (uint32_t)*reinterpret_cast<const uint16_t*>(head + kv4_value_code(D, p, chunk * 2 + 1)) << 16;
+        }
+        s[1] = head[kv4_value_scale(D, p, chunk >> 2)];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const float scale = as_f32(s[n] << 23);
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[n], scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[n], scale, 1);
+            const f2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[n], scale, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[n], scale, 3);
+            x[n][0] = a.x; x[n][1] = a.y; x[n][2] = b.x; x[n][3] = b.y;
+            x[n][4] = d.x; x[n][5] = d.y; x[n][6] = e.x; x[n][7] = e.y;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j >> 3][j & 7] = as_f32(0x7fc00000u);
+    }
+    store_chunk<OUT_BF16>(k.p + t * k.ts + h * k.hs + chunk * 8 * OS, x[0]);
+    store_chunk<OUT_BF16>(v.p + t * v.ts + h * v.hs + chunk * 8 * OS, x[1]);
+}
+
+}  // namespace
+
+hipError_t launch_kv4_read(int D, const uint8_t* pool, int64_t num_slots, int Hk, int64_t T, const int64_t* slots, const Heads& k,
+                           const Heads& v, bool out_bf16, hipStream_t stream) {
+    const dim3 grid((uint32_t)((T * Hk * (D / 8) + 255) / 256)), block(256);
+#define BRQ_READ(D_, OUT) hipLaunchKernelGGL((k_kv4_read<D_, OUT>), grid, block, 0, stream, pool, num_slots, Hk, T, slots, k, v)
+    if (D == 64) { if (out_bf16) BRQ_READ(64, true); else BRQ_READ(64, false); }
+    else { if (out_bf16) BRQ_READ(128, true); else BRQ_READ(128, false); }
+#undef BRQ_READ
+    return hipGetLastError();
+}
+
+}  // namespace brq

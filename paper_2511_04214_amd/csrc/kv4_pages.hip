@@ -1,0 +1,318 @@
+// Pages of the MXFP4 cache: copied, shared, given up, reserved and made dense, on the device (include/brq_attn.h).
+//
+// What moves pages is bound by HBM; what finds them (counts of free and live pages in page order, so that results do not
+// depend on the schedule) is one workgroup that goes through the counts 16 at a time and thread, 16384 a step.
+#include "brq_attn.h"
+#include "brq_device.h"
+#include "brq_launch.h"
+
+namespace brq {
+namespace {
+
+constexpr int kScan = 1024;       // threads of the workgroup that counts
+constexpr int kPer = 16;          // page counts a thread and step
+
+// Sum of v over the workgroup's threads in front of this one; *total: over all.  lds: 17 ints, free on return after the next barrier.
+__device__ __forceinline__ int scan_before(int v, int* lds, int* total) {
+    const int lane = (int)(threadIdx.x & 63u), w = (int)(threadIdx.x >> 6);
+    int x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    if (lane == 63) lds[w] = x;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < kScan / 64; ++i) {
+        const int n = lds[i];
+        before += i < w ? n : 0;
+        all += n;
+    }
+    __syncthreads();
+    *total = all;
+    return before + x - v;
+}
+
+// The counts of 16 pages of a thread: -1 past the end.
+__device__ __forceinline__ void load_refs(const int32_t* refs, int n, int at, int (&r)[kPer]) {
+    if (at + kPer <= n && (reinterpret_cast<uintptr_t>(refs) & 15u) == 0) {
+#pragma unroll
+        for (int i = 0; i < kPer; i += 4) {
+            const v4i v = *reinterpret_cast<const v4i*>(refs + at + i);
+            r[i] = v.x; r[i + 1] = v.y; r[i + 2] = v.z; r[i + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) r[i] = at + i < n ? refs[at + i] : -1;
+    }
+}
+
+__device__ __forceinline__ bool in_range(int x, int n) { return x >= 0 && x < n; }
+
+// Bytes of page `from` to page `to`, by all threads of the workgroups `part` of `parts`.
+__device__ __forceinline__ void move_page(uint8_t* pool, int64_t page_bytes, int from, int to, int part, int parts) {
+    const v4i* s = reinterpret_cast<const v4i*>(pool + (int64_t)from * page_bytes);
+    v4i* d = reinterpret_cast<v4i*>(pool + (int64_t)to * page_bytes);
+    const int n = (int)(page_bytes / 16), step = parts * (int)blockDim.x;
+    int i = part * (int)blockDim.x + (int)threadIdx.x;
+    for (; i + 3 * step < n; i += 4 * step) {
+        const v4i a = s[i], b = s[i + step], c = s[i + 2 * step], e = s[i + 3 * step];
+        d[i] = a; d[i + step] = b; d[i + 2 * step] = c; d[i + 3 * step] = e;
+    }
+    for (; i < n; i += step) d[i] = s[i];
+}
+
+// ---- workspace of fork and reserve: [0] free pages found (no more than wanted), first[n] (a call's pages in front of item i), pages[...]
+struct Found {
+    int32_t *count, *first, *pages;
+    __host__ __device__ Found(int32_t* w, int n) : count(w), first(w + 4), pages(w + 4 + n) {}
+};
+
+// Pages that item i wants: FORK: one where its parent's last page is not full; reserve: its row's columns below the wanted
+// length that have no page, or -1 where the table has too few columns.
+template <bool FORK>
+__device__ __forceinline__ int wanted(const PagesArgs& a, int i) {
+    if constexpr (FORK) {
+        const int p = a.a[i], c = a.b[i];
+        if (!in_range(p, a.S) || !in_range(c, a.S)) return 0;
+        const int len = a.lens[p];
+        if (len <= 0 || len > a.cols * (int64_t)kKv4Page || len % kKv4Page == 0) return 0;
+        return in_range(a.table[(int64_t)p * a.cols + len / kKv4Page], a.num_pages) ? 1 : 0;
+    } else {
+        const int s = a.a[i], tokens = a.b[i];
+        if (!in_range(s, a.S) || tokens <= 0) return 0;
+        const int cols = (tokens - 1) / kKv4Page + 1;
+        if (cols > a.cols) return -1;
+        int n = 0;
+        for (int c = 0; c < cols; ++c) n += a.table[(int64_t)s * a.cols + c] < 0;
+        return n;
+    }
+}
+
+template <bool FORK>
+__global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
+    __shared__ int lds[17];
+    const Found f(a.workspace, a.n);
+    int want = 0, total;
+    for (int i0 = 0; i0 < a.n; i0 += kScan) {
+        const int i = i0 + (int)threadIdx.x, w = i < a.n ? wanted<FORK>(a, i) : 0;
+        const int before = scan_before(w > 0 ? w : 0, lds, &total);
+        if (i < a.n) f.first[i] = min(want + before, a.num_pages);               // (more than there are is as good as any more)
+        want = min(want + total, a.num_pages);
+    }
+    int found = 0;
+    for (int at = 0; at < a.num_pages && found < want; at += kScan * kPer) {
+        int r[kPer], n = 0;
+        const int mine = at + (int)threadIdx.x * kPer;
+        load_refs(a.refs, a.num_pages, mine, r);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) n += r[i] == 0;
+        int rank = found + scan_before(n, lds, &total);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (r[i] == 0) {
+                if (rank < want) f.pages[rank] = mine + i;
+                ++rank;
+            }
+        found += total;
+    }
+    if (threadIdx.x == 0) {
+        f.count[0] = min(found, want);
+        a.result[0] = 0;
+    }
+}
+
+// Pairs (parent, child): `parts` workgroups copy the last page's bytes, the first of them also writes the child's row.
+__global__ __launch_bounds__(256) void k_fork(const PagesArgs a, int parts) {
+    const int i = (int)(blockIdx.x / parts), part = (int)(blockIdx.x % parts);
+    const Found f(a.workspace, a.n);
+    const int p = a.a[i], c = a.b[i];
+    if (!in_range(p, a.S) || !in_range(c, a.S)) return;
+    const int want = wanted<true>(a, i), len = a.lens[p], full = len > 0 ? min(len / kKv4Page, a.cols) : 0;
+    int32_t *from = a.table + (int64_t)p * a.cols, *to = a.table + (int64_t)c * a.cols;
+    const bool failed = want > 0 && f.first[i] >= f.count[0];
+    const int page = want > 0 && !failed ? f.pages[f.first[i]] : -1;
+    if (page >= 0) {
+        const int last = from[full];
+        if (in_range(last, a.num_pages)) move_page(a.pool, a.page_bytes, last, page, part, parts);
+    }
+    if (part != 0) return;
+    for (int k = (int)threadIdx.x; k < a.cols; k += 256) {
+        int32_t e = -1;
+        if (!failed) {
+            if (k < full) {
+                e = from[k];
+                if (in_range(e, a.num_pages)) atomicAdd(a.refs + e, 1);
+                else e = -1;
+            } else if (k == full) {
+                e = page;
+            }
+        }
+        to[k] = e;
+    }
+    if (threadIdx.x == 0) {
+        a.lens[c] = failed ? 0 : len;
+        if (page >= 0) a.refs[page] = 1;
+        if (failed) atomicAdd(a.result, 1);
+    }
+}
+
+// A wavefront fills the empty columns of one row.
+__global__ __launch_bounds__(64) void k_reserve(const PagesArgs a) {
+    const int i = (int)blockIdx.x, lane = (int)threadIdx.x;
+    const Found f(a.workspace, a.n);
+    const int s = a.a[i], tokens = a.b[i];
+    if (!in_range(s, a.S) || tokens <= 0) return;
+    const int cols = (tokens - 1) / kKv4Page + 1;
+    int32_t* row = a.table + (int64_t)s * a.cols;
+    bool failed = cols > a.cols;
+    int need = 0;
+    if (!failed) {
+        for (int c0 = 0; c0 < cols; c0 += 64) need += __popcll(__ballot(c0 + lane < cols && row[c0 + lane] < 0));
+        failed = need > 0 && (int64_t)f.first[i] + need > f.count[0];
+    }
+    if (failed) {
+        if (lane == 0) atomicAdd(a.result, 1);
+        return;
+    }
+    int at = f.first[i];
+    for (int c0 = 0; c0 < cols && need > 0; c0 += 64) {
+        const bool empty = c0 + lane < cols && row[c0 + lane] < 0;
+        const uint64_t m = __ballot(empty);
+        if (empty) {
+            const int page = f.pages[at + __popcll(m & ((1ull << lane) - 1))];
+            row[c0 + lane] = page;
+            a.refs[page] = 1;
+        }
+        at += __popcll(m);
+    }
+}
+
+// The entry is taken out by an exchange: a sequence named twice is given up once.
+__global__ __launch_bounds__(256) void k_free(const PagesArgs a) {
+    const int s = a.a[blockIdx.x];
+    if (!in_range(s, a.S)) return;
+    int32_t* row = a.table + (int64_t)s * a.cols;
+    for (int k = (int)threadIdx.x; k < a.cols; k += 256) {
+        const int e = atomicExch(row + k, -1);
+        if (in_range(e, a.num_pages)) atomicSub(a.refs + e, 1);
+    }
+    if (threadIdx.x == 0) a.lens[s] = 0;
+}
+
+__global__ __launch_bounds__(256) void k_copy(const PagesArgs a, int parts) {
+    const int i = (int)(blockIdx.x / parts), part = (int)(blockIdx.x % parts);
+    const int s = a.a[i], d = a.b[i];
+    if (in_range(s, a.num_pages) && in_range(d, a.num_pages) && s != d) move_page(a.pool, a.page_bytes, s, d, part, parts);
+}
+
+// ---- compaction.  Workspace: [0] moves, pairs from[N/2 + 1], to[N/2 + 1], then map[N].
+struct Moves {
+    int32_t *count, *from, *to, *map;
+    __host__ __device__ Moves(int32_t* w, int n) : count(w), from(w + 4), to(w + 4 + n / 2 + 1), map(w + 4 + 2 * (n / 2 + 1)) {}
+};
+
+__global__ __launch_bounds__(kScan) void k_plan_moves(const PagesArgs a) {
+    __shared__ int lds[17];
+    const Moves v(a.workspace, a.num_pages);
+    int live = 0, total;
+    for (int at = 0; at < a.num_pages; at += kScan * kPer) {
+        int r[kPer], n = 0;
+        load_refs(a.refs, a.num_pages, at + (int)threadIdx.x * kPer, r);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) n += r[i] > 0;
+        scan_before(n, lds, &total);
+        live += total;
+    }
+    // free pages below `live` and live pages at or above it: as many of one as of the other
+    int holes = 0, high = 0;
+    for (int at = 0; at < a.num_pages; at += kScan * kPer) {
+        int r[kPer], nh = 0, ns = 0;
+        const int mine = at + (int)threadIdx.x * kPer;
+        load_refs(a.refs, a.num_pages, mine, r);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            nh += r[i] <= 0 && mine + i < live;
+            ns += r[i] > 0 && mine + i >= live;
+        }
+        int total_high;
+        int hole = holes + scan_before(nh, lds, &total), src = high + scan_before(ns, lds, &total_high);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (r[i] <= 0 && mine + i < live) v.to[hole++] = mine + i;
+            if (r[i] > 0 && mine + i >= live) v.from[src++] = mine + i;
+            if (r[i] <= 0 && mine + i >= live && mine + i < a.num_pages) v.map[mine + i] = -1;       // an entry that names a free page
+        }
+        holes += total;
+        high += total_high;
+    }
+    __syncthreads();
+    for (int k = (int)threadIdx.x; k < high; k += kScan) v.map[v.from[k]] = v.to[k];
+    if (threadIdx.x == 0) {
+        v.count[0] = high;
+        v.count[1] = live;
+        a.result[0] = live;
+    }
+}
+
+__global__ __launch_bounds__(256) void k_move(const PagesArgs a, int parts) {
+    const Moves v(a.workspace, a.num_pages);
+    const int moves = v.count[0], live = v.count[1];
+    for (int64_t k = blockIdx.x; k < (int64_t)moves * parts; k += gridDim.x) {
+        const int i = (int)(k / parts), part = (int)(k % parts), from = v.from[i], to = v.to[i];
+        move_page(a.pool, a.page_bytes, from, to, part, parts);
+        if (part == 0 && threadIdx.x == 0) {
+            a.refs[to] = a.refs[from];
+            a.refs[from] = 0;
+        }
+    }
+    const int64_t entries = (int64_t)a.S * a.cols;
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < entries; k += (int64_t)gridDim.x * 256) {
+        const int e = a.table[k];
+        if (e >= live && e < a.num_pages) a.table[k] = v.map[e];
+    }
+}
+
+// Workgroups to a page: 16 KB each.
+int parts_of(int64_t page_bytes) { return (int)((page_bytes + 16383) / 16384); }
+
+}  // namespace
+
+hipError_t launch_pages_copy(const PagesArgs& a, hipStream_t stream) {
+    const int parts = parts_of(a.page_bytes);
+    hipLaunchKernelGGL(k_copy, dim3((uint32_t)a.n * parts), dim3(256), 0, stream, a, parts);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL(k_find_free<true>, dim3(1), dim3(kScan), 0, stream, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (a.n == 0) return hipSuccess;
+    const int parts = parts_of(a.page_bytes);
+    hipLaunchKernelGGL(k_fork, dim3((uint32_t)a.n * parts), dim3(256), 0, stream, a, parts);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_free(const PagesArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL(k_free, dim3((uint32_t)a.n), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL(k_find_free<false>, dim3(1), dim3(kScan), 0, stream, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (a.n == 0) return hipSuccess;
+    hipLaunchKernelGGL(k_reserve, dim3((uint32_t)a.n), dim3(64), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL(k_plan_moves, dim3(1), dim3(kScan), 0, stream, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_move, dim3(2048), dim3(256), 0, stream, a, parts_of(a.page_bytes));
+    return hipGetLastError();
+}
+
+}  // namespace brq
