@@ -343,15 +343,13 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     }
 }
 
-// Joins the splits of a row: D/4 threads a row and head.
-template <int D>
-__global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int splits, const float* part_o, const float* part_ml) {
-    constexpr int TH = D / 4;
-    const int Hq = a.Hk * a.G, rows = 256 / TH;
-    const int64_t id = (int64_t)blockIdx.x * rows + threadIdx.x / TH;       // (sequence, row, head)
-    const int64_t si = id / Hq;
-    const int h = (int)(id - si * Hq), s = (int)(si / a.max_q), i = (int)(si - (int64_t)s * a.max_q), d = (int)(threadIdx.x % TH) * 4;
-    if (s >= a.S) return;
+// Joins the splits of one row and head: groups of D/4 threads take every so many splits, then their sums are joined.
+template <int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_attention_join(const AttnArgs a, int splits, const float* part_o, const float* part_ml) {
+    constexpr int TH = D / 4, GROUPS = THREADS / TH;
+    const int Hq = a.Hk * a.G, group = (int)threadIdx.x / TH, d = (int)(threadIdx.x % TH) * 4;
+    const int64_t id = blockIdx.x, si = id / Hq;                            // (sequence, row, head)
+    const int h = (int)(id - si * Hq), s = (int)(si / a.max_q), i = (int)(si - (int64_t)s * a.max_q);
     int64_t q0;
     int nq;
     query_rows(a, s, &q0, &nq);
@@ -360,14 +358,34 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
     const float *po = part_o + at * splits * D + d, *pm = part_ml + at * splits * 2;
     float m = -INFINITY, sum = 0.0f;
     v4f y = {0, 0, 0, 0};
-    for (int k = 0; k < splits; ++k) {
+#pragma unroll 4
+    for (int k = group; k < splits; k += GROUPS) {
         const f32x2 ml = *reinterpret_cast<const f32x2*>(pm + k * 2);
         const v4f x = *reinterpret_cast<const v4f*>(po + (int64_t)k * D);
-        if (ml.x == -INFINITY) continue;
-        const float now = fmaxf(m, ml.x), f0 = __builtin_amdgcn_exp2f(m - now), f1 = __builtin_amdgcn_exp2f(ml.x - now);
+        const float now = fmaxf(m, ml.x), r = now == -INFINITY ? 0.0f : now;
+        const float f0 = __builtin_amdgcn_exp2f(m - r), f1 = __builtin_amdgcn_exp2f(ml.x - r);
         y = y * f0 + x * f1;
         sum = sum * f0 + ml.y * f1;
         m = now;
+    }
+    __shared__ float so[GROUPS][D], sm[GROUPS], sl[GROUPS];
+    *reinterpret_cast<v4f*>(&so[group][d]) = y;
+    if (d == 0) {
+        sm[group] = m;
+        sl[group] = sum;
+    }
+    __syncthreads();
+    if (group != 0) return;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, sm[k]);
+    const float r = m == -INFINITY ? 0.0f : m;
+    y = v4f{0, 0, 0, 0};
+    sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) {
+        const float f = __builtin_amdgcn_exp2f(sm[k] - r);
+        y += *reinterpret_cast<const v4f*>(&so[k][d]) * f;
+        sum += sl[k] * f;
     }
     const float k = sum > 0.0f ? 1.0f / sum : 0.0f;
     *reinterpret_cast<v2i*>(a.o.p + t * a.o.ts + h * a.o.hs + d * 2) = v2i{(int)pack_bf16x2(y.x * k, y.y * k), (int)pack_bf16x2(y.z * k, y.w * k)};
@@ -448,10 +466,13 @@ __global__ __launch_bounds__(64) void k_attention_rows(const AttnArgs a) {
 }
 
 // How the pages are split: enough workgroups that each CU has several, none with less than two pages a wavefront.
+#ifndef BRQ_WGS
+#define BRQ_WGS 2
+#endif
 struct Splits { int n, pages; };
 Splits splits_of(int64_t S, int Hk, int64_t max_kv, int cus) {
     const int64_t pages = (max_kv + kKv4Page - 1) / kKv4Page, groups = S * Hk;
-    int64_t n = (cus * 6 + groups - 1) / groups;
+    int64_t n = (cus * BRQ_WGS + groups - 1) / groups;
     n = n < (pages + 7) / 8 ? n : (pages + 7) / 8;
     n = n < 1 ? 1 : n > 256 ? 256 : n;
     const int64_t each = (pages + n - 1) / n;
@@ -476,7 +497,8 @@ static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t strea
         hipLaunchKernelGGL((k_attention_few<D>), dim3((uint32_t)(a.S * a.Hk * sp.n)), dim3(256), 0, stream, a, sp.n, sp.pages, po, pm);
         if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;
         const int64_t rows = (int64_t)a.S * a.max_q * Hq;
-        hipLaunchKernelGGL((k_attention_join<D>), dim3((uint32_t)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, stream, a, sp.n, po, pm);
+        if (sp.n <= 8) hipLaunchKernelGGL((k_attention_join<D, 64>), dim3((uint32_t)rows), dim3(64), 0, stream, a, sp.n, po, pm);
+        else hipLaunchKernelGGL((k_attention_join<D, 256>), dim3((uint32_t)rows), dim3(256), 0, stream, a, sp.n, po, pm);
         return hipGetLastError();
     }
     hipLaunchKernelGGL((k_attention_rows<D>), dim3((uint32_t)((int64_t)a.S * a.max_q * Hq)), dim3(64), 0, stream, a);
