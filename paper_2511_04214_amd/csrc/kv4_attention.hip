@@ -1,10 +1,10 @@
 // Attention over the MXFP4 cache (include/brq_attn.h).
 //
-// Scores on the block-scaled matrix instruction: a key is its 4-bit codes and E8M0 bytes as they stand in the cache, no
-// instruction spent on unpacking; a bf16 query is the sum of two e4m3 terms of 4 significant bits each under one power of
-// two (the second 2^-4 below the first), which costs what one bf16 product would (two 8-bit products at twice the rate)
-// and is exact but for channels 2^-14 below the row's largest.  Values have a scale per token, which
-// is the sum's axis, so they are unpacked to bf16 (exact) and multiplied by the softmax weights rounded to bf16.
+// Keys and values are unpacked to bf16, which holds a 4-bit value under its power of two exactly, by the instruction that
+// converts two codes under a scale, and go to the bf16 matrix instructions.  (The block-scaled instruction would take the keys as they
+// stand, against a query in two e4m3 terms, at the same rate and without the conversions.  But it adds eight products at
+// a time aligned to the largest of them in a window of 14 bits: scores came out 4e-6 of the sum of the products' magnitudes off,
+// 2^-18, and the sums here are to hold 32 bits.)
 // The products are made transposed, S^T = K Q^T and O^T = V^T P^T: a lane then holds one query row's scores for the very
 // tokens that it has to supply to the second product, and one row's output, so that weights go from the first product's
 // accumulators to the second's operand without leaving the lane and a row's rescaling is one factor a lane.
@@ -27,6 +27,27 @@ __device__ __forceinline__ uint32_t two_values(uint32_t w, uint32_t scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, as_f32(scale), B));
 }
 
+// Exponent of byte I of four E8M0 scales, as the conversions take it (bits 30:23; they look at no others).
+template <int I>
+__device__ __forceinline__ uint32_t scale_of(uint32_t b) {
+    return I == 0 ? b << 23 : I == 1 ? b << 15 : I == 2 ? b << 7 : b >> 1;
+}
+__device__ __forceinline__ bf16x8 eight_values(uint32_t w, uint32_t scale) {
+    const v4i x = {(int)two_values<0>(w, scale), (int)two_values<1>(w, scale), (int)two_values<2>(w, scale), (int)two_values<3>(w, scale)};
+    return __builtin_bit_cast(bf16x8, x);
+}
+
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&r)[N], const uint8_t* p) {
+    if constexpr (N == 4) {
+        const v4i x = *reinterpret_cast<const v4i*>(p);
+        r[0] = (uint32_t)x.x; r[1] = (uint32_t)x.y; r[2] = (uint32_t)x.z; r[3] = (uint32_t)x.w;
+    } else {
+        const v2i x = *reinterpret_cast<const v2i*>(p);
+        r[0] = (uint32_t)x.x; r[1] = (uint32_t)x.y;
+    }
+}
+
 // Range of query rows [q0, q1) of a sequence; empty where the offsets are none.
 __device__ __forceinline__ void query_rows(const AttnArgs& a, int s, int64_t* q0, int* n) {
     int64_t b = s, e = (int64_t)s + 1;
@@ -38,39 +59,6 @@ __device__ __forceinline__ void query_rows(const AttnArgs& a, int s, int64_t* q0
     *n = b < 0 || e > a.T || e <= b ? 0 : (int)min(e - b, (int64_t)a.max_q);
 }
 
-// The two e4m3 terms of 16 query channels, and what scales them.  `sign`: 0x8000 to negate.
-struct Terms { v4i hi, lo; };
-__device__ __forceinline__ Terms two_terms(const v4i (&w)[2], uint32_t byte, uint32_t sign) {
-    const float s1 = as_f32(byte << 23), s2 = as_f32((byte - 4u) << 23);
-    Terms t;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        typedef short v2s __attribute__((ext_vector_type(2)));
-        v2s hi = {0, 0}, lo = {0, 0};
-        const uint32_t a = (uint32_t)w[i >> 1][(i & 1) * 2] ^ (sign * 0x10001u), b = (uint32_t)w[i >> 1][(i & 1) * 2 + 1] ^ (sign * 0x10001u);
-        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, bf16_lo(a), bf16_hi(a), s1, false);
-        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, bf16_lo(b), bf16_hi(b), s1, true);
-        const uint32_t h = __builtin_bit_cast(uint32_t, hi);
-        const f32x2 ra = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, s1, false), rb = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, s1, true);
-        lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, bf16_lo(a) - ra.x, bf16_hi(a) - ra.y, s2, false);
-        lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, bf16_lo(b) - rb.x, bf16_hi(b) - rb.y, s2, true);
-        t.hi[i] = (int)h;
-        t.lo[i] = __builtin_bit_cast(int, lo);
-    }
-    return t;
-}
-// E8M0 byte under which a row whose largest channel is `top` lies in [128, 256): at least 4, so that the second term's exists.
-__device__ __forceinline__ uint32_t terms_byte(float top) {
-    const uint32_t e = (as_u32(top) >> 23) & 0xffu;
-    return e < 11u ? 4u : e - 7u;
-}
-__device__ __forceinline__ float absmax_bf16(const v4i& w) {
-    float m = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m = fmaxf(m, fmaxf(fabsf(bf16_lo((uint32_t)w[i])), fabsf(bf16_hi((uint32_t)w[i]))));
-    return m;
-}
-
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // ---- up to 16 query rows (tokens x heads of a group) against a range of pages: decoding
@@ -78,8 +66,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A page of one head as a lane takes it: 4 subtiles of 16 tokens.
 template <int D>
 struct PageRegs {
-    v4i k[4];
-    uint32_t ks;
+    uint32_t k[4][D / 32];       // token 16 u + n, channels D/4 g ...
+    uint32_t ks;                 // byte u: its scale
     uint32_t v[4][D / 32];       // 4 tokens of the lane's column
     v4i vs;                      // byte i of element u: scale of token 16 u + 4 g + i
 };
@@ -116,43 +104,16 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     const int page0 = max(begin_any / kKv4Page, split * pages_a_split);
     const int page1 = min((max(end_any, 0) + kKv4Page - 1) / kKv4Page, (split + 1) * pages_a_split);
 
-    // queries
-    v8i qh, ql;
-    uint32_t qs_hi, qs_lo;
+    // queries: channels D/4 g + 8 j of the lane's row
+    bf16x8 q[D / 32];
     {
         const uint8_t* qp = a.q.p + (q0 + tok) * a.q.ts + head * a.q.hs;
-        const uint32_t sign = a.scale < 0.0f ? 0x8000u : 0u;
+        const int flip = a.scale < 0.0f ? (int)0x80008000u : 0;
         const v4i zero = {0, 0, 0, 0};
-        v4i x[D / 64][2];
-        float top = 0.0f;
 #pragma unroll
-        for (int k = 0; k < D / 64; ++k)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const v4i l = *reinterpret_cast<const v4i*>(qp + (k * 64 + g * 16 + i * 8) * 2);
-                x[k][i] = n < rows ? l : zero;
-                top = fmaxf(top, absmax_bf16(x[k][i]));
-            }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const uint32_t byte = terms_byte(top);
-        const Terms t0 = two_terms(x[0], byte, sign);
-        if constexpr (D == 128) {
-            const Terms t1 = two_terms(x[1], byte, sign);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                qh[i] = t0.hi[i]; qh[i + 4] = t1.hi[i];
-                ql[i] = t0.lo[i]; ql[i + 4] = t1.lo[i];
-            }
-            qs_hi = byte;
-            qs_lo = byte - 4u;
-        } else {                 // both terms are one operand: the second as channels 64 ... 127, against the same keys again
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                qh[i] = t0.hi[i];
-                qh[i + 4] = t0.lo[i];
-            }
-            qs_hi = g < 2 ? byte : byte - 4u;
+        for (int k = 0; k < D / 32; ++k) {
+            const v4i x = *reinterpret_cast<const v4i*>(qp + (g * (D / 4) + k * 8) * 2) ^ flip;
+            q[k] = __builtin_bit_cast(bf16x8, n < rows ? x : zero);
         }
     }
     const float c = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);
@@ -166,22 +127,10 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     auto load = [&](PageRegs<D>& r, int number) {
         const uint8_t* h = uniform_ptr(a.pool + ((int64_t)number * a.Hk + kvh) * HB);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            r.k[u] = *reinterpret_cast<const v4i*>(h + u * 8 * D + n * (D / 2) + (D == 128 ? g : g & 1) * 16);
-        r.ks = *reinterpret_cast<const uint32_t*>(h + 32 * D + ((D == 128 ? g : g & 1) * 16 + n) * 4);
+        for (int u = 0; u < 4; ++u) load_words<D / 32>(r.k[u], h + (u * 64 + n * 4 + g) * (D / 8));
+        r.ks = *reinterpret_cast<const uint32_t*>(h + 32 * D + (g * D / 128 * 16 + n) * 4);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const uint8_t* vp = h + 34 * D + (u * 64 + lane) * (D / 8);
-            if constexpr (D == 128) {
-                const v4i x = *reinterpret_cast<const v4i*>(vp);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) r.v[u][i] = (uint32_t)x[i];
-            } else {
-                const v2i x = *reinterpret_cast<const v2i*>(vp);
-                r.v[u][0] = (uint32_t)x[0];
-                r.v[u][1] = (uint32_t)x[1];
-            }
-        }
+        for (int u = 0; u < 4; ++u) load_words<D / 32>(r.v[u], h + 34 * D + (u * 64 + lane) * (D / 8));
         r.vs = *reinterpret_cast<const v4i*>(h + 66 * D + (g * (D / 32) + n * D / 512) * 16);
     };
     auto use = [&](PageRegs<D>& r, int page) {
@@ -189,9 +138,10 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
         v4f x[4];
         static_for([&](auto iu) {
             constexpr int u = decltype(iu)::value;
-            v8i kk = {r.k[u].x, r.k[u].y, r.k[u].z, r.k[u].w, 0, 0, 0, 0};
-            x[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kk, qh, v4f{0, 0, 0, 0}, 4, 0, u, (int)r.ks, 0, (int)qs_hi);
-            if constexpr (D == 128) x[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kk, ql, x[u], 4, 0, u, (int)r.ks, 0, (int)qs_lo);
+            x[u] = v4f{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k)
+                x[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_values(r.k[u][k], scale_of<u>(r.ks)), q[k], x[u], 0, 0, 0);
         }, IC<4>{});
         if (t0 < begin_all || t0 + kKv4Page > end_all) {               // some row does not see some token
 #pragma unroll
@@ -241,10 +191,10 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const uint32_t b = (uint32_t)r.vs[2 * h + u];
-                sc[u][0] = b << 23;
-                sc[u][1] = b << 15;
-                sc[u][2] = b << 7;
-                sc[u][3] = b >> 1;
+                sc[u][0] = scale_of<0>(b);
+                sc[u][1] = scale_of<1>(b);
+                sc[u][2] = scale_of<2>(b);
+                sc[u][3] = scale_of<3>(b);
             }
             static_for([&](auto ib) {            // channels 2 b and 2 b + 1 of the lane's column
                 constexpr int b = decltype(ib)::value;
@@ -253,12 +203,12 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
                 for (int u = 0; u < 2; ++u) {
                     if constexpr (D == 128) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) y[u][i] = two_values<b>(r.v[2 * h + u][i], sc[u][i] & 0x7fffffffu);
+                        for (int i = 0; i < 4; ++i) y[u][i] = two_values<b>(r.v[2 * h + u][i], sc[u][i]);
                     } else {
-                        y[u][0] = two_values<b>(r.v[2 * h + u][0], sc[u][0] & 0x7fffffffu);
-                        y[u][1] = two_values<b + 2>(r.v[2 * h + u][0], sc[u][1] & 0x7fffffffu);
-                        y[u][2] = two_values<b>(r.v[2 * h + u][1], sc[u][2] & 0x7fffffffu);
-                        y[u][3] = two_values<b + 2>(r.v[2 * h + u][1], sc[u][3] & 0x7fffffffu);
+                        y[u][0] = two_values<b>(r.v[2 * h + u][0], sc[u][0]);
+                        y[u][1] = two_values<b + 2>(r.v[2 * h + u][0], sc[u][1]);
+                        y[u][2] = two_values<b>(r.v[2 * h + u][1], sc[u][2]);
+                        y[u][3] = two_values<b + 2>(r.v[2 * h + u][1], sc[u][3]);
                     }
                 }
                 v4i even, odd;
@@ -343,6 +293,243 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     }
 }
 
+// ---- many query rows: prompts and chunks
+
+// A page of one head as a wavefront takes its keys (all 64 tokens, 32 x 32 x 64 products) and a thread its share of the values.
+template <int D>
+struct ManyRegs {
+    uint32_t k[2][D / 64][4];    // tokens 32 i + lane % 32, channels 64 s + 32 (lane / 32) ...
+    uint32_t ks[D / 64];
+    uint32_t v[D / 32];          // 4 tokens of a column
+    uint32_t vs;
+};
+
+// Workgroup: 128 rows (query tokens x heads of a group) of a sequence and cache head, 32 to a wavefront, against the pages of a
+// split.  The keys go from memory to the wavefronts' registers as operands; the values are unpacked by the four wavefronts
+// together, a quarter each, into LDS: [channel][64 tokens] bf16, in the order in which a lane of the second product takes them:
+// quads of tokens 4 s + h and 4 s + 2 + h of its half h side by side.  Channel D/16 c + j is row 16 j + c, so that 16 columns'
+// writes fall on neighbouring rows, and a lane ends up with whole columns of the output.  Two buffers, one barrier a page.
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int tiles, int splits, int pages_a_split, float* part_o, float* part_ml) {
+    constexpr int MT = D / 32, KS = D / 64, HB = kv4_head_bytes(D), ROW = 64 * 2 + 16;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2][D * ROW];
+    const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+    // neighbouring workgroups take different heads (each XCD its own), the longest rows of a causal prompt first
+    int id = (int)blockIdx.x;
+    const int kvh = id % a.Hk;
+    id /= a.Hk;
+    const int split = id % splits;
+    id /= splits;
+    const int s = id % a.S, tile = tiles - 1 - id / a.S;
+    int64_t q0;
+    int nq;
+    query_rows(a, s, &q0, &nq);
+    const int rows = nq * a.G, r0 = tile * 128;
+    if (r0 >= rows) return;
+    const int len = a.kv_lens[s], all = min(len, min(a.max_kv, a.table_cols * kKv4Page));
+    const int first = len - (a.cu_q ? (int)(a.cu_q[s + 1] - a.cu_q[s]) : 1);          // position of the sequence's first row
+    const int r = r0 + w * 32 + n, rc = min(r, rows - 1), tok = rc / a.G, head = kvh * a.G + (rc - tok * a.G);
+    // tokens that a row of the workgroup sees; that every row of the wavefront sees, and any; that this lane's row sees
+    int begin = 0, end = all, begin_wg = 0, end_wg = all, begin_all = 0, end_all = all, begin_any = 0, end_any = all;
+    if (a.causal) {
+        const int wa = min(r0 + w * 32, rows - 1) / a.G, wb = min(r0 + w * 32 + 31, rows - 1) / a.G, ga = r0 / a.G, gb = min(r0 + 127, rows - 1) / a.G;
+        end = min(all, first + tok + 1);
+        end_all = min(all, first + wa + 1);
+        end_any = min(all, first + wb + 1);
+        end_wg = min(all, first + gb + 1);
+        if (a.window) {
+            begin = max(0, first + tok - a.window + 1);
+            begin_all = max(0, first + wb - a.window + 1);
+            begin_any = max(0, first + wa - a.window + 1);
+            begin_wg = max(0, first + ga - a.window + 1);
+        }
+    }
+    if (r0 + w * 32 >= rows) end_any = 0;                // a wavefront without rows only unpacks
+    const int page0 = max(begin_wg / kKv4Page, split * pages_a_split);
+    const int page1 = min((max(end_wg, 0) + kKv4Page - 1) / kKv4Page, (split + 1) * pages_a_split);
+
+    bf16x8 q[KS][4];                                      // channels 64 k + 32 h + 8 j
+    {
+        const uint8_t* qp = a.q.p + (q0 + tok) * a.q.ts + head * a.q.hs;
+        const int flip = a.scale < 0.0f ? (int)0x80008000u : 0;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const v4i x = *reinterpret_cast<const v4i*>(qp + (k * 64 + h * 32 + j * 8) * 2) ^ flip;
+                q[k][j] = __builtin_bit_cast(bf16x8, x);
+            }
+    }
+    const float c = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);
+
+    v16f o[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[j][i] = 0.0f;
+    float l = 0.0f, ref = 0.0f, top_ref = -INFINITY;
+
+    const int vq = (int)threadIdx.x >> 4, vc = (int)threadIdx.x & 15;                 // this thread's quad of tokens and column of the values
+    const int vpos = ((vq & ~3) | ((vq & 1) << 1) | ((vq >> 1) & 1)) * 8;             // where the quad lies in a row of LDS
+    ManyRegs<D> g;
+    auto page_at = [&](int number) { return uniform_ptr(a.pool + ((int64_t)number * a.Hk + kvh) * HB); };
+    auto load_keys = [&](const uint8_t* p) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < KS; ++k) load_words<4>(g.k[i][k], p + (i * 32 + n) * (D / 2) + k * 32 + h * 16);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) g.ks[k] = *reinterpret_cast<const uint32_t*>(p + 32 * D + ((k * 2 + h) * 16 + (n & 15)) * 4);
+    };
+    auto load_values = [&](const uint8_t* p) {
+        load_words<D / 32>(g.v, p + 34 * D + (int)threadIdx.x * (D / 8));
+        g.vs = *reinterpret_cast<const uint32_t*>(p + 66 * D + ((vq & 3) * (D / 32) + vc * D / 512) * 16 + (vq >> 2) * 4);
+    };
+    auto unpack = [&](int page, uint8_t* buf) {
+        const int left = all - (page * kKv4Page + vq * 4);                            // tokens that are none: 0 times whatever they hold is to be 0
+        const uint32_t sb = left >= 4 ? g.vs : left <= 0 ? 0u : g.vs & ((1u << (8 * left)) - 1u);
+        const uint32_t sc[4] = {scale_of<0>(sb), scale_of<1>(sb), scale_of<2>(sb), scale_of<3>(sb)};
+        static_for([&](auto ib) {
+            constexpr int b = decltype(ib)::value;
+            uint32_t y[4];
+            if constexpr (D == 128) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = two_values<b>(g.v[i], sc[i]);
+            } else {
+                y[0] = two_values<b>(g.v[0], sc[0]);
+                y[1] = two_values<b + 2>(g.v[0], sc[1]);
+                y[2] = two_values<b>(g.v[1], sc[2]);
+                y[3] = two_values<b + 2>(g.v[1], sc[3]);
+            }
+            const v2i even = {(int)__builtin_amdgcn_perm(y[1], y[0], 0x05040100u), (int)__builtin_amdgcn_perm(y[3], y[2], 0x05040100u)};
+            const v2i odd = {(int)__builtin_amdgcn_perm(y[1], y[0], 0x07060302u), (int)__builtin_amdgcn_perm(y[3], y[2], 0x07060302u)};
+            *reinterpret_cast<v2i*>(buf + ((2 * b) * 16 + vc) * ROW + vpos) = even;
+            *reinterpret_cast<v2i*>(buf + ((2 * b + 1) * 16 + vc) * ROW + vpos) = odd;
+        }, IC<D / 32>{});
+    };
+    auto use = [&](int page, const uint8_t* buf, const uint8_t* following) {          // following: the next page, null: none
+        const int t0 = page * kKv4Page;
+        const bool mine = t0 < end_any && t0 + kKv4Page > begin_any;                  // some row of the wavefront sees some of it
+        v4i pw[4];
+        if (mine) {
+            v16f x[2];
+            static_for([&](auto ii) {
+                constexpr int i = decltype(ii)::value;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[i][e] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    const uint32_t sc = scale_of<2 * i>(g.ks[k] >> (n & 16 ? 8 : 0));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_values(g.k[i][k][j], sc), q[k][j], x[i], 0, 0, 0);
+                }
+            }, IC<2>{});
+            if (following) load_keys(following);
+            if (t0 < begin_all || t0 + kKv4Page > end_all) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int t = t0 + i * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
+                        x[i][e] = t >= begin && t < end ? x[i][e] : -INFINITY;
+                    }
+            }
+            float top = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+            for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(top, x[0][e]), x[1][e]);
+            top *= c;
+            if (__any(top > top_ref + 8.0f)) {
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float now = fmaxf(top, top_ref), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top_ref - now);
+                top_ref = now;
+                ref = now == -INFINITY ? 0.0f : now;
+                l *= f;
+#pragma unroll
+                for (int j = 0; j < MT; ++j) o[j] *= f;
+            }
+#pragma unroll
+            for (int st = 0; st < 4; ++st)
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st >> 1][(st & 1) * 8 + e], c, -ref));
+                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st >> 1][(st & 1) * 8 + e + 1], c, -ref));
+                    l += e0 + e1;
+                    pw[st][e >> 1] = (int)pack_bf16x2(e0, e1);
+                }
+        } else if (following) {
+            load_keys(following);
+        }
+        lds_wait_and_barrier();
+        if (mine) {
+#pragma unroll
+            for (int st = 0; st < 4; ++st)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    const v4i vv = *reinterpret_cast<const v4i*>(buf + (j * 32 + n) * ROW + st * 32 + h * 16);
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vv), __builtin_bit_cast(bf16x8, pw[st]), o[j], 0, 0, 0);
+                }
+        }
+    };
+
+    const int32_t* row = a.table + (int64_t)s * a.table_cols;
+    for (int chunk = page0; chunk < page1; chunk += 64) {
+        const int entry = chunk + lane < page1 ? row[chunk + lane] : -1;
+        uint64_t left = __ballot(entry >= 0 && entry < a.num_pages);
+        auto next = [&](int* page) {
+            if (left == 0) return -1;
+            const int i = __builtin_ctzll(left);
+            left &= left - 1;
+            *page = chunk + i;
+            return __builtin_amdgcn_readlane(entry, i);
+        };
+        int page = 0, after = 0, number = next(&page);
+        if (number >= 0) {
+            load_keys(page_at(number));
+            load_values(page_at(number));
+        }
+        for (int b = 0; number >= 0; b ^= 1) {
+            unpack(page, lds[b]);
+            const int following = next(&after);
+            const uint8_t* p = following >= 0 ? page_at(following) : nullptr;
+            if (p) load_values(p);
+            use(page, lds[b], p);
+            page = after;
+            number = following;
+        }
+        lds_wait_and_barrier();                      // the next 64 begin with the first buffer
+    }
+
+    l += __shfl_xor(l, 32);
+    if (r >= rows) return;
+    const int64_t t = q0 + tok, at = t * (a.Hk * a.G) + head;
+    if (part_o) {
+        float* po = part_o + (at * splits + split) * D;
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+#pragma unroll
+            for (int j = 0; j < D / 16; j += 4) {
+                v4f y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = o[(j + e) >> 1][((j + e) & 1) * 8 + q];
+                *reinterpret_cast<v4f*>(po + ((q >> 2) * 8 + h * 4 + (q & 3)) * (D / 16) + j) = y;
+            }
+        if (h == 0) *reinterpret_cast<f32x2*>(part_ml + (at * splits + split) * 2) = f32x2{top_ref, l};
+        return;
+    }
+    const float k = l > 0.0f ? 1.0f / l : 0.0f;
+    uint8_t* op = a.o.p + t * a.o.ts + head * a.o.hs;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        uint32_t y[D / 32];
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) y[j] = pack_bf16x2(o[j][q] * k, o[j][8 + q] * k);
+        uint8_t* d = op + ((q >> 2) * 8 + h * 4 + (q & 3)) * (D / 8);
+        if constexpr (D == 128) *reinterpret_cast<v4i*>(d) = v4i{(int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+        else *reinterpret_cast<v2i*>(d) = v2i{(int)y[0], (int)y[1]};
+    }
+    if (a.lse && h == 0) a.lse[at] = l > 0.0f ? (top_ref + __log2f(l)) * kLn2 : -INFINITY;
+}
+
 // Joins the splits of one row and head: groups of D/4 threads take every so many splits, then their sums are joined.
 template <int D, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_attention_join(const AttnArgs a, int splits, const float* part_o, const float* part_ml) {
@@ -392,116 +579,43 @@ __global__ __launch_bounds__(THREADS) void k_attention_join(const AttnArgs a, in
     if (a.lse && d == 0) a.lse[at] = sum > 0.0f ? (m + __log2f(sum)) * kLn2 : -INFINITY;
 }
 
-// One wavefront: one query row and head.  A lane owns a token of the page for the scores, D/64 channels for the sum.
-template <int D>
-__global__ __launch_bounds__(64) void k_attention_rows(const AttnArgs a) {
-    const int lane = (int)threadIdx.x, Hq = a.Hk * a.G;
-    const int64_t id = blockIdx.x, si = id / Hq;
-    const int h = (int)(id - si * Hq), s = (int)(si / a.max_q), i = (int)(si - (int64_t)s * a.max_q);
-    int64_t q0 = s, q1 = s + 1;
-    if (a.cu_q) {
-        q0 = a.cu_q[s];
-        q1 = a.cu_q[s + 1];
+// How a call is cut up.  Up to 16 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
+// pages; more: tiles of 128 rows.  The pages are split where that alone leaves CUs idle: two workgroups a CU, none with less than
+// two pages a wavefront.
+struct Plan {
+    bool few;
+    int64_t tiles;
+    int splits, pages;
+    static Plan of(int64_t S, int Hk, int G, int64_t max_q, int64_t max_kv, int cus) {
+        const bool few = max_q * G <= 16;
+        const int64_t tiles = few ? 1 : (max_q * G + 127) / 128, pages = (max_kv + kKv4Page - 1) / kKv4Page, groups = S * Hk * tiles;
+        int64_t n = (2 * cus + groups - 1) / groups;
+        n = n < (pages + 7) / 8 ? n : (pages + 7) / 8;
+        n = n < 1 ? 1 : n > 256 ? 256 : n;
+        const int64_t each = (pages + n - 1) / n;
+        return {few, tiles, (int)(each ? (pages + each - 1) / each : 1), (int)(each ? each : 1)};
     }
-    if (q0 < 0 || q1 > a.T || i >= q1 - q0) return;
-    const int64_t t = q0 + i;
-    const int len = a.kv_lens[s], p = len - (int)(q1 - q0) + i;
-    int end = min(len, min(a.max_kv, a.table_cols * kKv4Page)), begin = 0;
-    if (a.causal) {
-        end = min(end, p + 1);
-        if (a.window) begin = max(0, p - a.window + 1);
-    }
-    __shared__ float qs[D], ps[64];
-    for (int d = lane; d < D; d += 64)
-        qs[d] = bf16_lo(*reinterpret_cast<const uint16_t*>(a.q.p + t * a.q.ts + h * a.q.hs + d * 2));
-    __syncthreads();
-    constexpr int N = D / 64;
-    float m = -INFINITY, l = 0.0f, o[N] = {};
-    for (int page = begin / kKv4Page; page * kKv4Page < end; ++page) {
-        const int number = a.table[(int64_t)s * a.table_cols + page];
-        if (number < 0 || number >= a.num_pages) continue;
-        const uint8_t* head = a.pool + ((int64_t)number * a.Hk + h / a.G) * kv4_head_bytes(D);
-        const int j = page * kKv4Page + lane;
-        float x = 0.0f;
-        for (int c = 0; c < D / 8; ++c) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(head + kv4_key_code(D, lane) + c * 4);
-            const float scale = as_f32((uint32_t)head[kv4_key_scale(D, lane, c >> 2)] << 23);
-            const f32x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
-            const f32x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-            const float* q = qs + c * 8;
-            x += q[0] * v0.x + q[1] * v0.y + q[2] * v1.x + q[3] * v1.y + q[4] * v2.x + q[5] * v2.y + q[6] * v3.x + q[7] * v3.y;
-        }
-        x = j >= begin && j < end ? x * a.scale : -INFINITY;
-        float mx = x;
-        for (int k = 1; k < 64; k *= 2) mx = fmaxf(mx, __shfl_xor(mx, k));
-        const float m2 = fmaxf(m, mx), f = expf(m - m2), e = expf(x - m2);       // (a page that is gone through has a token that is seen)
-        float sum = e;
-        for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
-        l = l * f + sum;
-        m = m2;
-        ps[lane] = e;
-        __syncthreads();
-        for (int n = 0; n < N; ++n) o[n] *= f;
-        const int channel = lane * N;                                           // N = 1: half of a byte
-        for (int tok = 0; tok < kKv4Page; ++tok) {
-            const int at = page * kKv4Page + tok;
-            if (at < begin || at >= end) continue;
-            const int byte = channel / 2;
-            const uint32_t w = head[kv4_value_code(D, tok, byte / (D / 32)) + byte % (D / 32)];
-            const float scale = as_f32((uint32_t)head[kv4_value_scale(D, tok, channel / 32)] << 23);
-            const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0);
-            if constexpr (N == 1) {
-                o[0] += ps[tok] * ((channel & 1) ? v.y : v.x);
-            } else {
-                o[0] += ps[tok] * v.x;
-                o[1] += ps[tok] * v.y;
-            }
-        }
-        __syncthreads();
-    }
-    const float r = l > 0.0f ? 1.0f / l : 0.0f;
-    for (int n = 0; n < N; ++n)
-        *reinterpret_cast<uint16_t*>(a.o.p + t * a.o.ts + h * a.o.hs + (lane * N + n) * 2) = (uint16_t)f32_to_bf16_bits(o[n] * r);
-    if (a.lse && lane == 0) a.lse[t * Hq + h] = l > 0.0f ? m + logf(l) : -INFINITY;
-}
-
-// How the pages are split: enough workgroups that each CU has several, none with less than two pages a wavefront.
-#ifndef BRQ_WGS
-#define BRQ_WGS 2
-#endif
-struct Splits { int n, pages; };
-Splits splits_of(int64_t S, int Hk, int64_t max_kv, int cus) {
-    const int64_t pages = (max_kv + kKv4Page - 1) / kKv4Page, groups = S * Hk;
-    int64_t n = (cus * BRQ_WGS + groups - 1) / groups;
-    n = n < (pages + 7) / 8 ? n : (pages + 7) / 8;
-    n = n < 1 ? 1 : n > 256 ? 256 : n;
-    const int64_t each = (pages + n - 1) / n;
-    return {(int)(each ? (pages + each - 1) / each : 1), (int)(each ? each : 1)};
-}
-bool few_rows(int64_t max_q, int G) { return max_q * G <= 16; }
+};
 
 }  // namespace
 
 int64_t kv4_attention_workspace(int64_t T, int64_t S, int Hq, int Hk, int D, int64_t max_q, int64_t max_kv, int cus) {
-    if (!few_rows(max_q, Hq / Hk)) return 0;
-    const Splits sp = splits_of(S, Hk, max_kv, cus);
-    return sp.n == 1 ? 0 : T * Hq * sp.n * (D + 2) * 4;
+    const Plan p = Plan::of(S, Hk, Hq / Hk, max_q, max_kv, cus);
+    return p.splits == 1 ? 0 : T * Hq * p.splits * (D + 2) * 4;
 }
 
 template <int D>
 static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t stream) {
     const int Hq = a.Hk * a.G;
-    if (few_rows(a.max_q, a.G)) {
-        const Splits sp = splits_of(a.S, a.Hk, a.max_kv, cus);
-        float *po = sp.n == 1 ? nullptr : static_cast<float*>(a.workspace), *pm = po ? po + a.T * Hq * sp.n * D : nullptr;
-        hipLaunchKernelGGL((k_attention_few<D>), dim3((uint32_t)(a.S * a.Hk * sp.n)), dim3(256), 0, stream, a, sp.n, sp.pages, po, pm);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;
-        const int64_t rows = (int64_t)a.S * a.max_q * Hq;
-        if (sp.n <= 8) hipLaunchKernelGGL((k_attention_join<D, 64>), dim3((uint32_t)rows), dim3(64), 0, stream, a, sp.n, po, pm);
-        else hipLaunchKernelGGL((k_attention_join<D, 256>), dim3((uint32_t)rows), dim3(256), 0, stream, a, sp.n, po, pm);
-        return hipGetLastError();
-    }
-    hipLaunchKernelGGL((k_attention_rows<D>), dim3((uint32_t)((int64_t)a.S * a.max_q * Hq)), dim3(64), 0, stream, a);
+    const Plan p = Plan::of(a.S, a.Hk, a.G, a.max_q, a.max_kv, cus);
+    float *po = p.splits == 1 ? nullptr : static_cast<float*>(a.workspace), *pm = po ? po + a.T * Hq * p.splits * D : nullptr;
+    const dim3 grid((uint32_t)(a.S * a.Hk * p.tiles * p.splits));
+    if (p.few) hipLaunchKernelGGL((k_attention_few<D>), grid, dim3(256), 0, stream, a, p.splits, p.pages, po, pm);
+    else hipLaunchKernelGGL((k_attention_many<D>), grid, dim3(256), 0, stream, a, (int)p.tiles, p.splits, p.pages, po, pm);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;
+    const dim3 rows((uint32_t)((int64_t)a.S * a.max_q * Hq));
+    if (p.splits <= 8) hipLaunchKernelGGL((k_attention_join<D, 64>), rows, dim3(64), 0, stream, a, p.splits, po, pm);
+    else hipLaunchKernelGGL((k_attention_join<D, 256>), rows, dim3(256), 0, stream, a, p.splits, po, pm);
     return hipGetLastError();
 }
 
