@@ -6,7 +6,7 @@ include/brq.h, and returns the output tensors.  No arithmetic of the method happ
 here.  There is no CPU fallback: without the built library, or without a GPU tensor, the
 calls raise.
 
-The five calls that layers are made of, and the two of the analysis, are marshalled in csrc/binding.cpp where their arguments are plain; what it leaves
+The five calls that layers are made of, the two of the analysis, and those of the attention side (attention.py) are marshalled in csrc/binding.cpp where their arguments are plain; what it leaves
 (it returns None) goes the way written here, which takes and refuses everything.  So do all calls where that part cannot be
 loaded: it is linked to one torch's C++ interface, libbrq.so to none.
 """
@@ -99,14 +99,15 @@ def _load_native(L):
         from . import _binding
         if getattr(_binding, "TORCH", None) != str(torch.__version__):
             raise ImportError("built against another torch than %s" % torch.__version__)
-        bind, bind_stats = _binding.bind, _binding.bind_stats
-    except (ImportError, AttributeError) as e:              # (AttributeError: built before the call came)
+        bind, bind_stats, bind_attention = _binding.bind, _binding.bind_stats, _binding.bind_attention
+    except (ImportError, AttributeError) as e:              # (AttributeError: built before these calls came)
         warnings.warn("the compiled part of the binding is not used, calls take some us longer: %s" % e, RuntimeWarning, stacklevel=3)
         return None
     bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.brq_rotate_quantize_fused, L.brq_swiglu_rotate_quantize_fused, L.brq_matrix_rotate_quantize_fused, L.brq_mxfp4_gemm,
         L.brq_rotate_quantize_gemm_fused)))
     bind_stats(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.brq_block_stats, L.brq_block_stats_summary)))
+    bind_attention(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in _attention.NATIVE))
     return _binding
 
 

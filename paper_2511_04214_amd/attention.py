@@ -13,6 +13,10 @@ import torch
 import paper_2511_04214_amd as _brq
 
 KV4_PAGE = 64
+# the entry points that the compiled marshalling calls, in its order
+NATIVE = ("brq_qk_norm_rope", "brq_qk_norm_rope_backward", "brq_qk_norm_rope_backward_workspace", "brq_kv4_append", "brq_kv4_read", "brq_kv4_attention",
+          "brq_kv4_attention_workspace", "brq_kv4_pages_workspace", "brq_kv4_pages_copy", "brq_kv4_pages_fork", "brq_kv4_pages_free", "brq_kv4_pages_reserve",
+          "brq_kv4_pages_compact")
 
 
 class _Heads(ctypes.Structure):
@@ -61,6 +65,8 @@ def _heads(t, name, shape=None):
 
 
 def _same_device(like, *tensors):
+    if like.is_cuda and like.device.index != torch.cuda.current_device():
+        raise ValueError("tensors on %s, which is not the current device" % like.device)
     for t in tensors:
         if t is not None and t.device != like.device:
             raise ValueError("tensors on several devices: %s and %s" % (like.device, t.device))
@@ -94,6 +100,16 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _native(name, stream, *args):
+    """What the compiled marshalling answers: None where it leaves the call to Python."""
+    if stream is not None or _brq._native is None:
+        return None
+    r = getattr(_brq._native, name)(*args)
+    if type(r) is int:
+        _brq._check(r)
+    return r
+
+
 def _ref(x):
     return None if x is None else ctypes.byref(x)
 
@@ -109,6 +125,9 @@ def qk_norm_rope(q, k=None, wq=None, wk=None, eps=1e-6, cos=None, sin=None, posi
     """(q', k') of queries [T, Hq, D] and keys [T, Hk, D]: RMS norm of every head with weights wq, wk (fp32 [D]; None: no norm),
     rotation by position (cos, sin fp32 [rows, rot / 2], positions int64 [T]; None: none), block rotation (B = 1: none)
     (brq_qk_norm_rope).  Without `k` the second result is None."""
+    r = _native("qk_norm_rope", stream, q, k, wq, wk, eps, cos, sin, positions, interleaved, B, out_dtype, q_out, k_out)
+    if r is not None:
+        return r
     hq, hk = _heads(q, "q"), _heads(k, "k", None if k is None else (q.shape[0], None, q.shape[2]))
     T, _, D = q.shape
     if k is not None and k.dtype != q.dtype:
@@ -140,6 +159,9 @@ def qk_norm_rope_backward(q, k, gq, gk, wq=None, wk=None, eps=1e-6, cos=None, si
                           dk=None, workspace=None, stream=None):
     """(dq, dk, dwq, dwk) from the inputs of qk_norm_rope and the gradients gq, gk of its results (brq_qk_norm_rope_backward).
     dwq, dwk are fp32 [D], None where the weight is."""
+    r = _native("qk_norm_rope_backward", stream, q, k, gq, gk, wq, wk, eps, cos, sin, positions, interleaved, B, dq, dk, workspace)
+    if r is not None:
+        return r
     T, Hq, D = q.shape if q.dim() == 3 else (0, 0, 0)
     hq, hk = _heads(q, "q"), _heads(k, "k", None if k is None else (T, None, D))
     if (k is None) != (gk is None):
@@ -190,6 +212,9 @@ def kv4_append(pool, slots, k, v, q=None, wq=None, wk=None, eps=1e-6, cos=None, 
                q_out=None, stream=None):
     """Writes keys and values [T, Hk, D] to slots (int64 [T], page * KV4_PAGE + place) of the cache: keys as qk_norm_rope makes
     them, values rotated by Bv, both as MXFP4 (brq_kv4_append).  With q the queries come along: returns q', else None."""
+    r = _native("kv4_append", stream, pool, slots, k, v, q, wq, wk, eps, cos, sin, positions, interleaved, B, Bv, q_out)
+    if r is not None:
+        return None if r is True else r
     hk = _heads(k, "k")
     T, Hk, D = k.shape
     hv, hq = _heads(v, "v", k.shape), _heads(q, "q", (T, None, D))
@@ -213,6 +238,9 @@ def kv4_append(pool, slots, k, v, q=None, wq=None, wk=None, eps=1e-6, cos=None, 
 
 def kv4_read(pool, slots, D, out_dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
     """(k, v), each [T, Hk, D]: the values that stand at slots (int64 [T]) of the cache (brq_kv4_read)."""
+    r = _native("kv4_read", stream, pool, slots, D, out_dtype, k_out, v_out)
+    if r is not None:
+        return r
     p, pages, Hk = _pool(pool, None, D)
     sl = _array(slots, "slots", torch.int64, (None,))
     shape = (slots.shape[0], Hk, D)
@@ -239,6 +267,13 @@ def kv4_attention(q, pool, table, kv_lens, scale=None, causal=True, window=0, cu
     table int32 [S, columns], kv_lens int32 [S]; cu_q int32 [S + 1] says which rows are whose (None: one row a sequence,
     T = S).  max_q: the longest sequence's rows (None: 1 without cu_q, else T); max_kv: the longest context (None: what the
     table has room for).  scale: None for D ** -0.5.  Returns out, or (out, lse) where lse is given or wanted."""
+    if q.dim() == 3 and table.dim() == 2:
+        max_q = (1 if cu_q is None else max(1, q.shape[0])) if max_q is None else max_q
+        max_kv = table.shape[1] * KV4_PAGE if max_kv is None else max_kv
+        scale = q.shape[2] ** -0.5 if scale is None and q.shape[2] else scale
+    r = _native("kv4_attention", stream, q, pool, table, kv_lens, scale, causal, window, cu_q, max_q, max_kv, out, lse, want_lse, workspace)
+    if r is not None:
+        return r
     hq = _heads(q, "q")
     T, Hq, D = q.shape
     if q.dtype != torch.bfloat16 or (out is not None and out.dtype != torch.bfloat16):
@@ -250,8 +285,6 @@ def kv4_attention(q, pool, table, kv_lens, scale=None, causal=True, window=0, cu
     pl, pc = _array(kv_lens, "kv_lens", torch.int32, (S,)), _array(cu_q, "cu_q", torch.int32, (S + 1,), True)
     if cu_q is None and T != S:
         raise ValueError("cu_q must be given where the number of rows is not that of the sequences")
-    max_q = (1 if cu_q is None else max(1, T)) if max_q is None else max_q
-    max_kv = cols * KV4_PAGE if max_kv is None else max_kv
     need = kv4_attention_workspace(T, S, Hq, Hk, D, max_q, max_kv)
     with _on(stream):
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
@@ -261,7 +294,7 @@ def kv4_attention(q, pool, table, kv_lens, scale=None, causal=True, window=0, cu
             workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
     ho = _heads(out, "out", q.shape)
     _brq._check(_brq.lib().brq_kv4_attention(
-        _ref(hq), T, D, p, pages, Hk, pt, cols, pl, pc, S, D ** -0.5 if scale is None else scale, int(bool(causal)), window, max_q, max_kv,
+        _ref(hq), T, D, p, pages, Hk, pt, cols, pl, pc, S, scale, int(bool(causal)), window, max_q, max_kv,
         _ref(ho), _array(lse, "lse", torch.float32, (T, Hq), True), _array(workspace, "workspace", torch.uint8, (None,), True),
         0 if workspace is None else workspace.numel(), _brq._stream(stream)))
     return out if lse is None else (out, lse)
@@ -297,6 +330,8 @@ def _space(n, num_pages, workspace, like, stream):
 
 def kv4_pages_copy(pool, src, dst, stream=None):
     """Page dst[i] = page src[i] of the cache; src, dst int32 (brq_kv4_pages_copy)."""
+    if _native("kv4_pages_copy", stream, pool, src, dst) is not None:
+        return
     p, pages, _ = _pool(pool)
     ps, pd, n = _lists(src, dst, ("src", "dst"))
     _same_device(pool, src, dst)
@@ -306,6 +341,9 @@ def kv4_pages_copy(pool, src, dst, stream=None):
 def kv4_pages_fork(pool, table, lens, refs, parents, children, workspace=None, stream=None):
     """Sequences children[i] become copies of parents[i] (int32 lists): full pages shared, a last one that is not full copied
     (brq_kv4_pages_fork).  Returns failed, int32 [1]: pairs for which no free page was left."""
+    r = _native("kv4_pages_fork", stream, pool, table, lens, refs, parents, children, workspace)
+    if r is not None:
+        return r
     p, pages, _ = _pool(pool)
     pt, S, cols, pl, pr = _state(table, lens, refs, pages)
     pp, pc, n = _lists(parents, children, ("parents", "children"))
@@ -317,6 +355,8 @@ def kv4_pages_fork(pool, table, lens, refs, parents, children, workspace=None, s
 
 def kv4_pages_free(table, lens, refs, seqs, stream=None):
     """The pages of sequences seqs (int32) are given up (brq_kv4_pages_free)."""
+    if _native("kv4_pages_free", stream, table, lens, refs, seqs) is not None:
+        return
     pt, S, cols, pl, pr = _state(table, lens, refs, None)
     ps, _, n = _lists(seqs, None, ("seqs",))
     _same_device(table, lens, refs, seqs)
@@ -326,6 +366,9 @@ def kv4_pages_free(table, lens, refs, seqs, stream=None):
 def kv4_pages_reserve(table, refs, seqs, tokens, workspace=None, stream=None):
     """Sequences seqs[i] get pages for tokens[i] tokens (int32 lists) (brq_kv4_pages_reserve).  Returns failed, int32 [1]:
     sequences that got none for want of pages or columns."""
+    r = _native("kv4_pages_reserve", stream, table, refs, seqs, tokens, workspace)
+    if r is not None:
+        return r
     pt, S, cols, _, pr = _state(table, None, refs, None)
     ps, pk, n = _lists(seqs, tokens, ("seqs", "tokens"))
     _same_device(table, refs, seqs, tokens, workspace)
@@ -336,6 +379,9 @@ def kv4_pages_reserve(table, refs, seqs, tokens, workspace=None, stream=None):
 
 def kv4_pages_compact(pool, table, refs, workspace=None, stream=None):
     """The live pages move to the lowest numbers, table and refs follow (brq_kv4_pages_compact).  Returns live, int32 [1]."""
+    r = _native("kv4_pages_compact", stream, pool, table, refs, workspace)
+    if r is not None:
+        return r
     p, pages, _ = _pool(pool)
     pt, S, cols, _, pr = _state(table, None, refs, pages)
     _same_device(pool, table, refs, workspace)

@@ -19,6 +19,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/brq.h"
+#include "../../include/brq_attn.h"
 
 namespace {
 
@@ -443,9 +444,378 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// ---- the attention side: through Python and ctypes a call took 9 to 20 us of the host (a decoding step's two 41), the GPU 5 to 8.
+// `o`: None where that is allowed, else a tensor that fits, or the call is left to Python.
+
+decltype(&brq_qk_norm_rope) f_norm;
+decltype(&brq_qk_norm_rope_backward) f_norm_back;
+decltype(&brq_qk_norm_rope_backward_workspace) f_norm_back_space;
+decltype(&brq_kv4_append) f_append;
+decltype(&brq_kv4_read) f_read;
+decltype(&brq_kv4_attention) f_attention;
+decltype(&brq_kv4_attention_workspace) f_attention_space;
+decltype(&brq_kv4_pages_workspace) f_pages_space;
+decltype(&brq_kv4_pages_copy) f_copy;
+decltype(&brq_kv4_pages_fork) f_fork;
+decltype(&brq_kv4_pages_free) f_free;
+decltype(&brq_kv4_pages_reserve) f_reserve;
+decltype(&brq_kv4_pages_compact) f_compact;
+bool g_attention;                    // bind_attention() was called
+
+// The tensors of a call: on one device, the current one.
+struct Call {
+    c10::DeviceIndex device = -1;
+    const at::Tensor* take(PyObject* o) {
+        const at::Tensor* t = plain(o);
+        if (!t) return nullptr;
+        if (device < 0) {
+            if (t->device().index() != c10::hip::current_device()) return nullptr;
+            device = t->device().index();
+        }
+        return t->device().index() == device ? t : nullptr;
+    }
+    at::TensorOptions options(at::ScalarType s) const { return at::TensorOptions().dtype(s).device(c10::DeviceType::CUDA, device); }
+};
+
+struct HeadSet {
+    at::Tensor t;                    // undefined: None
+    brq_heads h{};
+    int64_t T = 0, D = 0;
+    brq_dtype dt = BRQ_F32;
+    const brq_heads* get() const { return t.defined() ? &h : nullptr; }
+    void fill() { h = brq_heads{t.data_ptr(), t.size(1), t.stride(0), t.stride(1)}; }
+};
+bool head_set(Call& c, PyObject* o, HeadSet* x, bool optional = false) {
+    if (optional && o == Py_None) return true;
+    const at::Tensor* t = c.take(o);
+    if (!t || t->dim() != 3 || (t->size(2) > 1 && t->stride(2) != 1) || !dtype_of(t->scalar_type(), &x->dt)) return false;
+    x->t = *t;
+    x->T = t->size(0);
+    x->D = t->size(2);
+    x->fill();
+    return true;
+}
+bool same_tokens(const HeadSet& a, const HeadSet& b) { return !b.t.defined() || (a.T == b.T && a.D == b.D && a.dt == b.dt); }
+// An output: given, of `like`'s sizes and type `s`, or to be made.
+bool head_out(Call& c, PyObject* o, const HeadSet& like, at::ScalarType s, HeadSet* x) {
+    if (!like.t.defined()) return o == Py_None;
+    if (o == Py_None) return true;
+    return head_set(c, o, x) && x->t.sizes() == like.t.sizes() && x->t.scalar_type() == s;
+}
+bool make(const Call& c, at::IntArrayRef sizes, at::ScalarType s, at::Tensor* t) {
+    if (!t->defined()) {
+        const Unlocked u;
+        *t = at::empty(sizes, c.options(s));
+    }
+    return on_gpu(*t);
+}
+bool make_heads(const Call& c, const HeadSet& like, at::ScalarType s, HeadSet* x) {
+    if (!like.t.defined()) return true;
+    if (!make(c, like.t.sizes(), s, &x->t)) return false;
+    x->fill();
+    return true;
+}
+at::ScalarType scalar_of(brq_dtype d) { return d == BRQ_BF16 ? at::kBFloat16 : at::kFloat; }
+
+// A contiguous array of one type; sizes of -1 are any.
+bool array_of(Call& c, PyObject* o, at::ScalarType s, std::initializer_list<int64_t> sizes, at::Tensor* t, bool optional = false) {
+    if (optional && o == Py_None) return true;
+    const at::Tensor* p = c.take(o);
+    if (!p || p->scalar_type() != s || !p->is_contiguous() || p->dim() != (int64_t)sizes.size()) return false;
+    int i = 0;
+    for (int64_t n : sizes)
+        if (const int64_t m = p->size(i++); n >= 0 && n != m) return false;
+    *t = *p;
+    return true;
+}
+
+// wq, wk, eps, cos, sin, positions, interleaved, B: the arguments a[0] ... a[7] of the passes over heads
+struct NormArgs {
+    at::Tensor wq, wk, cos, sin, pos;
+    double eps;
+    int64_t B;
+    brq_rope r{};
+    const brq_rope* rope() const { return cos.defined() ? &r : nullptr; }
+};
+bool norm_args(Call& c, PyObject* const* a, int64_t T, int64_t D, NormArgs* n) {
+    if (!array_of(c, a[0], at::kFloat, {D}, &n->wq, true) || !array_of(c, a[1], at::kFloat, {D}, &n->wk, true) || !number(a[2], &n->eps) ||
+        !PyBool_Check(a[6]) || !integer(a[7], &n->B)) return false;
+    if (a[3] == Py_None) return a[4] == Py_None && a[5] == Py_None;
+    if (!array_of(c, a[3], at::kFloat, {-1, -1}, &n->cos) || !array_of(c, a[4], at::kFloat, {n->cos.size(0), n->cos.size(1)}, &n->sin) ||
+        !array_of(c, a[5], at::kLong, {T}, &n->pos)) return false;
+    n->r = brq_rope{address<float>(n->cos), address<float>(n->sin), address<int64_t>(n->pos), n->cos.size(0), n->cos.size(1) * 2, a[6] == Py_True};
+    return true;
+}
+
+PyObject* wrapped(PyObject* given, at::Tensor& t) {
+    if (!t.defined()) Py_RETURN_NONE;
+    return handed(given, t);
+}
+template <int N>
+PyObject* tuple_of(PyObject* (&items)[N]) {
+    bool fine = true;
+    for (PyObject* o : items) fine = fine && o;
+    PyObject* r = fine ? PyTuple_New(N) : nullptr;
+    for (int i = 0; i < N; ++i) {
+        if (r) PyTuple_SET_ITEM(r, i, items[i]);
+        else Py_XDECREF(items[i]);
+    }
+    return r;
+}
+
+// qk_norm_rope(q, k, wq, wk, eps, cos, sin, positions, interleaved, B, out_dtype, q_out, k_out)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    HeadSet q, k, qo, ko;
+    NormArgs m;
+    at::ScalarType s;
+    brq_dtype dt;
+    if (n != 13 || !g_attention || !quiet() || !head_set(c, a[0], &q) || !head_set(c, a[1], &k, true) || !same_tokens(q, k) || !norm_args(c, a + 2, q.T, q.D, &m)) Py_RETURN_NONE;
+    if (a[11] != Py_None) {
+        if (!head_set(c, a[11], &qo)) Py_RETURN_NONE;
+        s = qo.t.scalar_type();
+    } else if (a[10] == Py_None) {
+        s = q.t.scalar_type();
+    } else if (!dtype_arg(a[10], &s, &dt)) {
+        Py_RETURN_NONE;
+    }
+    if (!head_out(c, a[11], q, s, &qo) || !head_out(c, a[12], k, s, &ko) || !make_heads(c, q, s, &qo) || !make_heads(c, k, s, &ko) || !dtype_of(s, &dt)) Py_RETURN_NONE;
+    void* st = current_stream();
+    const brq_status r = released([&] {
+        return f_norm(q.get(), k.get(), q.dt, q.T, q.D, address<float>(m.wq), address<float>(m.wk), (float)m.eps, m.rope(), m.B, qo.get(), ko.get(), dt, st);
+    });
+    if (r != BRQ_OK) return status(r);
+    PyObject* items[2] = {wrapped(a[11], qo.t), wrapped(a[12], ko.t)};
+    return tuple_of(items);
+    END_HANDLE_TH_ERRORS
+}
+
+// qk_norm_rope_backward(q, k, gq, gk, wq, wk, eps, cos, sin, positions, interleaved, B, dq, dk, workspace)
+PyObject* qk_norm_rope_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    HeadSet q, k, gq, gk, dq, dk;
+    NormArgs m;
+    at::Tensor dwq, dwk, space;
+    if (n != 15 || !g_attention || !quiet() || !head_set(c, a[0], &q) || !head_set(c, a[1], &k, true) || !same_tokens(q, k) || !head_set(c, a[2], &gq) || !head_set(c, a[3], &gk, true) ||
+        gq.t.sizes() != q.t.sizes() || k.t.defined() != gk.t.defined() || (k.t.defined() && (gk.t.sizes() != k.t.sizes() || gk.dt != gq.dt)) ||
+        !norm_args(c, a + 4, q.T, q.D, &m) || !array_of(c, a[14], at::kByte, {-1}, &space, true)) Py_RETURN_NONE;
+    const at::ScalarType s = q.t.scalar_type();
+    if (!head_out(c, a[12], q, s, &dq) || !head_out(c, a[13], k, s, &dk) || !make_heads(c, q, s, &dq) || !make_heads(c, k, s, &dk)) Py_RETURN_NONE;
+    int64_t need = 0;
+    if (m.wq.defined() || (m.wk.defined() && k.t.defined())) {
+        if (const brq_status r = f_norm_back_space(q.T, q.h.heads, k.t.defined() ? k.h.heads : 0, q.D, &need); r != BRQ_OK) return status(r);
+        if (need && !make(c, {need}, at::kByte, &space)) Py_RETURN_NONE;
+    }
+    if ((m.wq.defined() && !make(c, {q.D}, at::kFloat, &dwq)) || (m.wk.defined() && k.t.defined() && !make(c, {q.D}, at::kFloat, &dwk))) Py_RETURN_NONE;
+    void* st = current_stream();
+    const brq_status r = released([&] {
+        return f_norm_back(q.get(), k.get(), q.dt, q.T, q.D, address<float>(m.wq), address<float>(m.wk), (float)m.eps, m.rope(), m.B, gq.get(), gk.get(), gq.dt, dq.get(),
+                           dk.get(), address<float>(dwq), address<float>(dwk), address<void>(space), space.defined() ? space.numel() : 0, st);
+    });
+    if (r != BRQ_OK) return status(r);
+    PyObject* items[4] = {wrapped(a[12], dq.t), wrapped(a[13], dk.t), wrapped(Py_None, dwq), wrapped(Py_None, dwk)};
+    return tuple_of(items);
+    END_HANDLE_TH_ERRORS
+}
+
+// A cache of heads of D channels; *Hk: its heads, to be found where negative.
+bool cache(Call& c, PyObject* o, int64_t D, int64_t* Hk, at::Tensor* t) {
+    if (!array_of(c, o, at::kByte, {-1, -1}, t) || D <= 0 || t->size(1) % (68 * D) != 0 || t->size(1) < 68 * D) return false;
+    if (*Hk < 0) *Hk = t->size(1) / (68 * D);
+    return *Hk * 68 * D == t->size(1);
+}
+
+// kv4_append(pool, slots, k, v, q, wq, wk, eps, cos, sin, positions, interleaved, B, Bv, q_out); True: there is no q
+PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    HeadSet q, k, v, qo;
+    NormArgs m;
+    at::Tensor pool, slots;
+    int64_t Bv;
+    if (n != 15 || !g_attention || !quiet() || !head_set(c, a[2], &k) || !head_set(c, a[3], &v) || v.t.sizes() != k.t.sizes() || v.dt != k.dt || !head_set(c, a[4], &q, true) ||
+        !same_tokens(k, q) || !norm_args(c, a + 5, k.T, k.D, &m) || !integer(a[13], &Bv) || !array_of(c, a[1], at::kLong, {k.T}, &slots)) Py_RETURN_NONE;
+    int64_t Hk = k.h.heads;
+    if (!cache(c, a[0], k.D, &Hk, &pool) || !head_out(c, a[14], q, scalar_of(k.dt), &qo) || !make_heads(c, q, scalar_of(k.dt), &qo)) Py_RETURN_NONE;
+    void* st = current_stream();
+    const brq_status r = released([&] {
+        return f_append(q.get(), k.get(), v.get(), k.dt, k.T, k.D, address<float>(m.wq), address<float>(m.wk), (float)m.eps, m.rope(), m.B, Bv, address<int64_t>(slots),
+                        address<uint8_t>(pool), pool.size(0), qo.get(), st);
+    });
+    if (r != BRQ_OK) return status(r);
+    if (!q.t.defined()) Py_RETURN_TRUE;
+    return wrapped(a[14], qo.t);
+    END_HANDLE_TH_ERRORS
+}
+
+// kv4_read(pool, slots, D, out_dtype, k_out, v_out)
+PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    HeadSet k, v;
+    at::Tensor pool, slots;
+    int64_t D, Hk = -1;
+    at::ScalarType s;
+    brq_dtype dt;
+    if (n != 6 || !g_attention || !quiet() || !integer(a[2], &D) || !cache(c, a[0], D, &Hk, &pool) || !array_of(c, a[1], at::kLong, {-1}, &slots) || !dtype_arg(a[3], &s, &dt)) Py_RETURN_NONE;
+    const int64_t shape[3] = {slots.size(0), Hk, D};
+    const at::IntArrayRef sizes(shape);
+    if (!head_set(c, a[4], &k, true) || (k.t.defined() && k.t.sizes() != sizes)) Py_RETURN_NONE;
+    if (k.t.defined()) s = k.t.scalar_type();
+    if (!head_set(c, a[5], &v, true) || (v.t.defined() && (v.t.sizes() != sizes || v.t.scalar_type() != s)) || !make(c, sizes, s, &k.t) || !make(c, sizes, s, &v.t)) Py_RETURN_NONE;
+    k.fill();
+    v.fill();
+    dtype_of(s, &dt);
+    void* st = current_stream();
+    const brq_status r = released([&] { return f_read(address<uint8_t>(pool), pool.size(0), sizes[0], D, address<int64_t>(slots), k.get(), v.get(), dt, st); });
+    if (r != BRQ_OK) return status(r);
+    PyObject* items[2] = {wrapped(a[4], k.t), wrapped(a[5], v.t)};
+    return tuple_of(items);
+    END_HANDLE_TH_ERRORS
+}
+
+// kv4_attention(q, pool, table, kv_lens, scale, causal, window, cu_q, max_q, max_kv, out, lse, want_lse, workspace)
+PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    HeadSet q, out;
+    at::Tensor pool, table, lens, cu, lse, space;
+    double scale = 0.0;
+    int64_t Hk = -1, window, max_q, max_kv, need = 0;
+    if (n != 14 || !g_attention || !quiet() || !head_set(c, a[0], &q) || q.dt != BRQ_BF16 || !cache(c, a[1], q.D, &Hk, &pool) || !array_of(c, a[2], at::kInt, {-1, -1}, &table) ||
+        !array_of(c, a[3], at::kInt, {table.size(0)}, &lens) || !array_of(c, a[7], at::kInt, {table.size(0) + 1}, &cu, true) || (!cu.defined() && q.T != table.size(0)) ||
+        !number(a[4], &scale) || !PyBool_Check(a[5]) || !integer(a[6], &window) || !integer(a[8], &max_q) || !integer(a[9], &max_kv) ||
+        !head_out(c, a[10], q, at::kBFloat16, &out) || !array_of(c, a[11], at::kFloat, {q.T, q.h.heads}, &lse, true) || !PyBool_Check(a[12]) ||
+        !array_of(c, a[13], at::kByte, {-1}, &space, true)) Py_RETURN_NONE;
+    const int64_t S = table.size(0);
+    if (const brq_status r = f_attention_space(q.T, S, q.h.heads, Hk, q.D, max_q, max_kv, &need); r != BRQ_OK) return status(r);
+    if (!make_heads(c, q, at::kBFloat16, &out) || (a[12] == Py_True && !make(c, {q.T, q.h.heads}, at::kFloat, &lse)) || (need && !make(c, {need}, at::kByte, &space))) Py_RETURN_NONE;
+    void* st = current_stream();
+    const brq_status r = released([&] {
+        return f_attention(q.get(), q.T, q.D, address<uint8_t>(pool), pool.size(0), Hk, address<int32_t>(table), table.size(1), address<int32_t>(lens), address<int32_t>(cu), S,
+                           (float)scale, a[5] == Py_True, window, max_q, max_kv, out.get(), address<float>(lse), address<void>(space), space.defined() ? space.numel() : 0, st);
+    });
+    if (r != BRQ_OK) return status(r);
+    if (!lse.defined()) return wrapped(a[10], out.t);
+    PyObject* items[2] = {wrapped(a[10], out.t), wrapped(a[11], lse)};
+    return tuple_of(items);
+    END_HANDLE_TH_ERRORS
+}
+
+// A scheduler's state and two lists of one length
+struct PageState {
+    at::Tensor table, lens, refs, x, y, space, result;
+    bool state(Call& c, PyObject* t, PyObject* l, PyObject* r, int64_t pages) {
+        return array_of(c, t, at::kInt, {-1, -1}, &table) && (!l || array_of(c, l, at::kInt, {table.size(0)}, &lens)) && array_of(c, r, at::kInt, {pages}, &refs);
+    }
+    bool lists(Call& c, PyObject* a, PyObject* b) { return array_of(c, a, at::kInt, {-1}, &x) && (!b || array_of(c, b, at::kInt, {x.size(0)}, &y)); }
+    bool room(Call& c, PyObject* o, int64_t n) {
+        int64_t need = 0;
+        return array_of(c, o, at::kByte, {-1}, &space, true) && f_pages_space(n, refs.size(0), &need) == BRQ_OK && make(c, {need}, at::kByte, &space) &&
+               space.numel() >= need && make(c, {1}, at::kInt, &result);
+    }
+    PyObject* answer(brq_status r) { return r != BRQ_OK ? status(r) : THPVariable_Wrap(std::move(result)); }
+};
+
+// kv4_pages_copy(pool, src, dst) -> status
+PyObject* kv4_pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    PageState p;
+    at::Tensor pool;
+    if (n != 3 || !g_attention || !quiet() || !array_of(c, a[0], at::kByte, {-1, -1}, &pool) || !p.lists(c, a[1], a[2])) Py_RETURN_NONE;
+    void* st = current_stream();
+    return status(released([&] { return f_copy(address<uint8_t>(pool), pool.size(1), pool.size(0), address<int32_t>(p.x), address<int32_t>(p.y), p.x.size(0), st); }));
+    END_HANDLE_TH_ERRORS
+}
+
+// kv4_pages_fork(pool, table, lens, refs, parents, children, workspace) -> failed
+PyObject* kv4_pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    PageState p;
+    at::Tensor pool;
+    if (n != 7 || !g_attention || !quiet() || !array_of(c, a[0], at::kByte, {-1, -1}, &pool) || !p.state(c, a[1], a[2], a[3], pool.size(0)) || !p.lists(c, a[4], a[5]) ||
+        !p.room(c, a[6], p.x.size(0))) Py_RETURN_NONE;
+    void* st = current_stream();
+    return p.answer(released([&] {
+        return f_fork(address<uint8_t>(pool), pool.size(1), pool.size(0), address<int32_t>(p.table), p.table.size(0), p.table.size(1), address<int32_t>(p.lens), address<int32_t>(p.refs),
+                      address<int32_t>(p.x), address<int32_t>(p.y), p.x.size(0), address<int32_t>(p.result), address<void>(p.space), st);
+    }));
+    END_HANDLE_TH_ERRORS
+}
+
+// kv4_pages_free(table, lens, refs, seqs) -> status
+PyObject* kv4_pages_free(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    PageState p;
+    if (n != 4 || !g_attention || !quiet() || !p.state(c, a[0], a[1], a[2], -1) || !p.lists(c, a[3], nullptr)) Py_RETURN_NONE;
+    void* st = current_stream();
+    return status(released([&] {
+        return f_free(address<int32_t>(p.table), p.table.size(0), p.table.size(1), address<int32_t>(p.lens), address<int32_t>(p.refs), p.refs.size(0), address<int32_t>(p.x), p.x.size(0), st);
+    }));
+    END_HANDLE_TH_ERRORS
+}
+
+// kv4_pages_reserve(table, refs, seqs, tokens, workspace) -> failed
+PyObject* kv4_pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    PageState p;
+    if (n != 5 || !g_attention || !quiet() || !p.state(c, a[0], nullptr, a[1], -1) || !p.lists(c, a[2], a[3]) || !p.room(c, a[4], p.x.size(0))) Py_RETURN_NONE;
+    void* st = current_stream();
+    return p.answer(released([&] {
+        return f_reserve(address<int32_t>(p.table), p.table.size(0), p.table.size(1), address<int32_t>(p.refs), p.refs.size(0), address<int32_t>(p.x), address<int32_t>(p.y), p.x.size(0),
+                         address<int32_t>(p.result), address<void>(p.space), st);
+    }));
+    END_HANDLE_TH_ERRORS
+}
+
+// kv4_pages_compact(pool, table, refs, workspace) -> live
+PyObject* kv4_pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    PageState p;
+    at::Tensor pool;
+    if (n != 4 || !g_attention || !quiet() || !array_of(c, a[0], at::kByte, {-1, -1}, &pool) || !p.state(c, a[1], nullptr, a[2], pool.size(0)) || !p.room(c, a[3], 0)) Py_RETURN_NONE;
+    void* st = current_stream();
+    return p.answer(released([&] {
+        return f_compact(address<uint8_t>(pool), pool.size(1), pool.size(0), address<int32_t>(p.table), p.table.size(0), p.table.size(1), address<int32_t>(p.refs),
+                         address<int32_t>(p.result), address<void>(p.space), st);
+    }));
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_attention(addresses of the entry points of the attention side, in the order of their declaration above)
+PyObject* bind_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void* p[13];
+    if (n != 13) {
+        PyErr_SetString(PyExc_TypeError, "bind_attention takes the addresses of thirteen entry points");
+        return nullptr;
+    }
+    for (int i = 0; i < 13; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (!p[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an entry point's address is NULL");
+            return nullptr;
+        }
+    }
+    int i = 0;
+    auto set = [&](auto& f) { f = reinterpret_cast<std::decay_t<decltype(f)>>(p[i++]); };
+    set(f_norm), set(f_norm_back), set(f_norm_back_space), set(f_append), set(f_read), set(f_attention), set(f_attention_space), set(f_pages_space), set(f_copy), set(f_fork),
+        set(f_free), set(f_reserve), set(f_compact);
+    g_attention = true;
+    Py_RETURN_NONE;
+}
+
 #define BRQ_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {BRQ_METHOD(bind), BRQ_METHOD(rotate_quantize), BRQ_METHOD(swiglu_rotate_quantize), BRQ_METHOD(matrix_rotate_quantize),
-                         BRQ_METHOD(gemm), BRQ_METHOD(rotate_quantize_gemm), BRQ_METHOD(bind_stats), BRQ_METHOD(block_stats), BRQ_METHOD(block_stats_summary), {nullptr, nullptr, 0, nullptr}};
+                         BRQ_METHOD(gemm), BRQ_METHOD(rotate_quantize_gemm), BRQ_METHOD(bind_stats), BRQ_METHOD(block_stats), BRQ_METHOD(block_stats_summary),
+                         BRQ_METHOD(bind_attention), BRQ_METHOD(qk_norm_rope), BRQ_METHOD(qk_norm_rope_backward), BRQ_METHOD(kv4_append), BRQ_METHOD(kv4_read), BRQ_METHOD(kv4_attention),
+                         BRQ_METHOD(kv4_pages_copy), BRQ_METHOD(kv4_pages_fork), BRQ_METHOD(kv4_pages_free), BRQ_METHOD(kv4_pages_reserve), BRQ_METHOD(kv4_pages_compact), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
