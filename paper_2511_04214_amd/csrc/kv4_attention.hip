@@ -48,6 +48,13 @@ __device__ __forceinline__ void load_words(uint32_t (&r)[N], const uint8_t* p) {
     }
 }
 
+// Pages [*first, *end) of a split: the pages that rows see, [b, e), in even parts of at least `least`.
+__device__ __forceinline__ void split_pages(int b, int e, int split, int splits, int least, int* first, int* end) {
+    const int n = max(e - b, 0), each = max((n + splits - 1) / splits, least);
+    *first = b + min(split * each, n);
+    *end = b + min((split + 1) * each, n);
+}
+
 // Range of query rows [q0, q1) of a sequence; empty where the offsets are none.
 __device__ __forceinline__ void query_rows(const AttnArgs& a, int s, int64_t* q0, int* n) {
     int64_t b = s, e = (int64_t)s + 1;
@@ -74,7 +81,7 @@ struct PageRegs {
 
 // Workgroup: sequence, cache head, split.  Wavefront w goes through pages first + w, first + w + 4, ...
 template <int D>
-__global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int splits, int pages_a_split, float* part_o, float* part_ml) {
+__global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int splits, float* part_o, float* part_ml) {
     constexpr int MT = D / 16, HB = kv4_head_bytes(D);
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int split = (int)blockIdx.x % splits, sh = (int)blockIdx.x / splits, s = sh / a.Hk, kvh = sh - s * a.Hk;
@@ -101,8 +108,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     begin_any = __builtin_amdgcn_readfirstlane(begin_any);
     end_all = __builtin_amdgcn_readfirstlane(end_all);
     begin_all = __builtin_amdgcn_readfirstlane(begin_all);
-    const int page0 = max(begin_any / kKv4Page, split * pages_a_split);
-    const int page1 = min((max(end_any, 0) + kKv4Page - 1) / kKv4Page, (split + 1) * pages_a_split);
+    int page0, page1;
+    split_pages(begin_any / kKv4Page, (max(end_any, 0) + kKv4Page - 1) / kKv4Page, split, splits, 4, &page0, &page1);
 
     // queries: channels D/4 g + 8 j of the lane's row
     bf16x8 q[D / 32];
@@ -310,7 +317,7 @@ struct ManyRegs {
 // quads of tokens 4 s + h and 4 s + 2 + h of its half h side by side.  Channel D/16 c + j is row 16 j + c, so that 16 columns'
 // writes fall on neighbouring rows, and a lane ends up with whole columns of the output.  Two buffers, one barrier a page.
 template <int D>
-__global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int tiles, int splits, int pages_a_split, float* part_o, float* part_ml) {
+__global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int tiles, int splits, float* part_o, float* part_ml) {
     constexpr int MT = D / 32, KS = D / 64, HB = kv4_head_bytes(D), ROW = 64 * 2 + 16;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][D * ROW];
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
@@ -345,8 +352,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
         }
     }
     if (r0 + w * 32 >= rows) end_any = 0;                // a wavefront without rows only unpacks
-    const int page0 = max(begin_wg / kKv4Page, split * pages_a_split);
-    const int page1 = min((max(end_wg, 0) + kKv4Page - 1) / kKv4Page, (split + 1) * pages_a_split);
+    int page0, page1;
+    split_pages(begin_wg / kKv4Page, (max(end_wg, 0) + kKv4Page - 1) / kKv4Page, split, splits, 1, &page0, &page1);
 
     bf16x8 q[KS][4];                                      // channels 64 k + 32 h + 8 j
     {
@@ -371,9 +378,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
 
     const int vq = (int)threadIdx.x >> 4, vc = (int)threadIdx.x & 15;                 // this thread's quad of tokens and column of the values
     const int vpos = ((vq & ~3) | ((vq & 1) << 1) | ((vq >> 1) & 1)) * 8;             // where the quad lies in a row of LDS
-    ManyRegs<D> g;
     auto page_at = [&](int number) { return uniform_ptr(a.pool + ((int64_t)number * a.Hk + kvh) * HB); };
-    auto load_keys = [&](const uint8_t* p) {
+    auto load_keys = [&](ManyRegs<D>& g, const uint8_t* p) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -381,11 +387,11 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
 #pragma unroll
         for (int k = 0; k < KS; ++k) g.ks[k] = *reinterpret_cast<const uint32_t*>(p + 32 * D + ((k * 2 + h) * 16 + (n & 15)) * 4);
     };
-    auto load_values = [&](const uint8_t* p) {
+    auto load_values = [&](ManyRegs<D>& g, const uint8_t* p) {
         load_words<D / 32>(g.v, p + 34 * D + (int)threadIdx.x * (D / 8));
         g.vs = *reinterpret_cast<const uint32_t*>(p + 66 * D + ((vq & 3) * (D / 32) + vc * D / 512) * 16 + (vq >> 2) * 4);
     };
-    auto unpack = [&](int page, uint8_t* buf) {
+    auto unpack = [&](const ManyRegs<D>& g, int page, uint8_t* buf) {
         const int left = all - (page * kKv4Page + vq * 4);                            // tokens that are none: 0 times whatever they hold is to be 0
         const uint32_t sb = left >= 4 ? g.vs : left <= 0 ? 0u : g.vs & ((1u << (8 * left)) - 1u);
         const uint32_t sc[4] = {scale_of<0>(sb), scale_of<1>(sb), scale_of<2>(sb), scale_of<3>(sb)};
@@ -407,7 +413,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
             *reinterpret_cast<v2i*>(buf + ((2 * b + 1) * 16 + vc) * ROW + vpos) = odd;
         }, IC<D / 32>{});
     };
-    auto use = [&](int page, const uint8_t* buf, const uint8_t* following) {          // following: the next page, null: none
+    auto use = [&](ManyRegs<D>& g, int page, const uint8_t* buf, const uint8_t* following) {      // following: whose keys come next into g, null: none
         const int t0 = page * kKv4Page;
         const bool mine = t0 < end_any && t0 + kKv4Page > begin_any;                  // some row of the wavefront sees some of it
         v4i pw[4];
@@ -424,7 +430,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
                     for (int j = 0; j < 4; ++j) x[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_values(g.k[i][k][j], sc), q[k][j], x[i], 0, 0, 0);
                 }
             }, IC<2>{});
-            if (following) load_keys(following);
+            if (following) load_keys(g, following);
             if (t0 < begin_all || t0 + kKv4Page > end_all) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -457,7 +463,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
                     pw[st][e >> 1] = (int)pack_bf16x2(e0, e1);
                 }
         } else if (following) {
-            load_keys(following);
+            load_keys(g, following);
         }
         lds_wait_and_barrier();
         if (mine) {
@@ -482,19 +488,29 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
             *page = chunk + i;
             return __builtin_amdgcn_readlane(entry, i);
         };
-        int page = 0, after = 0, number = next(&page);
-        if (number >= 0) {
-            load_keys(page_at(number));
-            load_values(page_at(number));
+        ManyRegs<D> ga, gb;
+        int pa = 0, pb = 0, na = next(&pa), nb = next(&pb);
+        if (na >= 0) {
+            load_keys(ga, page_at(na));
+            load_values(ga, page_at(na));
         }
-        for (int b = 0; number >= 0; b ^= 1) {
-            unpack(page, lds[b]);
-            const int following = next(&after);
-            const uint8_t* p = following >= 0 ? page_at(following) : nullptr;
-            if (p) load_values(p);
-            use(page, lds[b], p);
+        if (nb >= 0) {
+            load_keys(gb, page_at(nb));
+            load_values(gb, page_at(nb));
+        }
+        auto step = [&](ManyRegs<D>& g, int& page, int& number, uint8_t* buf) {       // the page in g; then g takes the one after the next
+            unpack(g, page, buf);
+            int after = 0;
+            number = next(&after);
+            const uint8_t* p = number >= 0 ? page_at(number) : nullptr;
+            if (p) load_values(g, p);
+            use(g, page, buf, p);
             page = after;
-            number = following;
+        };
+        while (na >= 0) {
+            step(ga, pa, na, lds[0]);
+            if (nb < 0) break;
+            step(gb, pb, nb, lds[1]);
         }
         lds_wait_and_barrier();                      // the next 64 begin with the first buffer
     }
@@ -530,23 +546,25 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
     if (a.lse && h == 0) a.lse[at] = l > 0.0f ? (top_ref + __log2f(l)) * kLn2 : -INFINITY;
 }
 
-// Joins the splits of one row and head: groups of D/4 threads take every so many splits, then their sums are joined.
-template <int D, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_attention_join(const AttnArgs a, int splits, const float* part_o, const float* part_ml) {
-    constexpr int TH = D / 4, GROUPS = THREADS / TH;
-    const int Hq = a.Hk * a.G, group = (int)threadIdx.x / TH, d = (int)(threadIdx.x % TH) * 4;
-    const int64_t id = blockIdx.x, si = id / Hq;                            // (sequence, row, head)
+// Joins the splits of rows and heads, 256/(GROUPS D/4) to a workgroup: GROUPS groups of D/4 threads a row take every so many splits,
+// then their sums are joined.
+template <int D, int GROUPS>
+__global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int splits, const float* part_o, const float* part_ml) {
+    constexpr int TH = D / 4, ROWS = 256 / (TH * GROUPS);
+    const int Hq = a.Hk * a.G, mine = (int)threadIdx.x / (TH * GROUPS), group = (int)threadIdx.x / TH % GROUPS, d = (int)(threadIdx.x % TH) * 4;
+    const int64_t id = (int64_t)blockIdx.x * ROWS + mine, si = id / Hq;     // (sequence, row, head)
     const int h = (int)(id - si * Hq), s = (int)(si / a.max_q), i = (int)(si - (int64_t)s * a.max_q);
-    int64_t q0;
-    int nq;
-    query_rows(a, s, &q0, &nq);
-    if (i >= nq) return;
-    const int64_t t = q0 + i, at = t * Hq + h;
+    int64_t q0 = 0;
+    int nq = 0;
+    if (s < a.S) query_rows(a, s, &q0, &nq);
+    const bool there = i < nq;
+    if (GROUPS == 1 && !there) return;
+    const int64_t t = q0 + i, at = there ? t * Hq + h : 0;
     const float *po = part_o + at * splits * D + d, *pm = part_ml + at * splits * 2;
     float m = -INFINITY, sum = 0.0f;
     v4f y = {0, 0, 0, 0};
 #pragma unroll 4
-    for (int k = group; k < splits; k += GROUPS) {
+    for (int k = there ? group : splits; k < splits; k += GROUPS) {
         const f32x2 ml = *reinterpret_cast<const f32x2*>(pm + k * 2);
         const v4f x = *reinterpret_cast<const v4f*>(po + (int64_t)k * D);
         const float now = fmaxf(m, ml.x), r = now == -INFINITY ? 0.0f : now;
@@ -555,24 +573,26 @@ __global__ __launch_bounds__(THREADS) void k_attention_join(const AttnArgs a, in
         sum = sum * f0 + ml.y * f1;
         m = now;
     }
-    __shared__ float so[GROUPS][D], sm[GROUPS], sl[GROUPS];
-    *reinterpret_cast<v4f*>(&so[group][d]) = y;
-    if (d == 0) {
-        sm[group] = m;
-        sl[group] = sum;
-    }
-    __syncthreads();
-    if (group != 0) return;
+    if constexpr (GROUPS > 1) {
+        __shared__ float so[ROWS][GROUPS][D], sm[ROWS][GROUPS], sl[ROWS][GROUPS];
+        *reinterpret_cast<v4f*>(&so[mine][group][d]) = y;
+        if (d == 0) {
+            sm[mine][group] = m;
+            sl[mine][group] = sum;
+        }
+        __syncthreads();
+        if (group != 0 || !there) return;
 #pragma unroll
-    for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, sm[k]);
-    const float r = m == -INFINITY ? 0.0f : m;
-    y = v4f{0, 0, 0, 0};
-    sum = 0.0f;
+        for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, sm[mine][k]);
+        const float r = m == -INFINITY ? 0.0f : m;
+        y = v4f{0, 0, 0, 0};
+        sum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < GROUPS; ++k) {
-        const float f = __builtin_amdgcn_exp2f(sm[k] - r);
-        y += *reinterpret_cast<const v4f*>(&so[k][d]) * f;
-        sum += sl[k] * f;
+        for (int k = 0; k < GROUPS; ++k) {
+            const float f = __builtin_amdgcn_exp2f(sm[mine][k] - r);
+            y += *reinterpret_cast<const v4f*>(&so[mine][k][d]) * f;
+            sum += sl[mine][k] * f;
+        }
     }
     const float k = sum > 0.0f ? 1.0f / sum : 0.0f;
     *reinterpret_cast<v2i*>(a.o.p + t * a.o.ts + h * a.o.hs + d * 2) = v2i{(int)pack_bf16x2(y.x * k, y.y * k), (int)pack_bf16x2(y.z * k, y.w * k)};
@@ -581,19 +601,20 @@ __global__ __launch_bounds__(THREADS) void k_attention_join(const AttnArgs a, in
 
 // How a call is cut up.  Up to 16 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
 // pages; more: tiles of 128 rows.  The pages are split where that alone leaves CUs idle: two workgroups a CU, none with less than
-// two pages a wavefront.
+// two pages a wavefront, or eight of a tile.
+#ifndef BRQ_WGS
+#define BRQ_WGS 2
+#endif
 struct Plan {
     bool few;
     int64_t tiles;
-    int splits, pages;
+    int splits;
     static Plan of(int64_t S, int Hk, int G, int64_t max_q, int64_t max_kv, int cus) {
         const bool few = max_q * G <= 16;
         const int64_t tiles = few ? 1 : (max_q * G + 127) / 128, pages = (max_kv + kKv4Page - 1) / kKv4Page, groups = S * Hk * tiles;
-        int64_t n = (2 * cus + groups - 1) / groups;
+        int64_t n = (BRQ_WGS * cus + groups - 1) / groups;
         n = n < (pages + 7) / 8 ? n : (pages + 7) / 8;
-        n = n < 1 ? 1 : n > 256 ? 256 : n;
-        const int64_t each = (pages + n - 1) / n;
-        return {few, tiles, (int)(each ? (pages + each - 1) / each : 1), (int)(each ? each : 1)};
+        return {few, tiles, (int)(n < 1 ? 1 : n > 256 ? 256 : n)};
     }
 };
 
@@ -610,12 +631,12 @@ static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t strea
     const Plan p = Plan::of(a.S, a.Hk, a.G, a.max_q, a.max_kv, cus);
     float *po = p.splits == 1 ? nullptr : static_cast<float*>(a.workspace), *pm = po ? po + a.T * Hq * p.splits * D : nullptr;
     const dim3 grid((uint32_t)(a.S * a.Hk * p.tiles * p.splits));
-    if (p.few) hipLaunchKernelGGL((k_attention_few<D>), grid, dim3(256), 0, stream, a, p.splits, p.pages, po, pm);
-    else hipLaunchKernelGGL((k_attention_many<D>), grid, dim3(256), 0, stream, a, (int)p.tiles, p.splits, p.pages, po, pm);
+    if (p.few) hipLaunchKernelGGL((k_attention_few<D>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
+    else hipLaunchKernelGGL((k_attention_many<D>), grid, dim3(256), 0, stream, a, (int)p.tiles, p.splits, po, pm);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;
-    const dim3 rows((uint32_t)((int64_t)a.S * a.max_q * Hq));
-    if (p.splits <= 8) hipLaunchKernelGGL((k_attention_join<D, 64>), rows, dim3(64), 0, stream, a, p.splits, po, pm);
-    else hipLaunchKernelGGL((k_attention_join<D, 256>), rows, dim3(256), 0, stream, a, p.splits, po, pm);
+    const int64_t rows = (int64_t)a.S * a.max_q * Hq;
+    if (p.splits <= 8) hipLaunchKernelGGL((k_attention_join<D, 1>), dim3((uint32_t)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, stream, a, p.splits, po, pm);
+    else hipLaunchKernelGGL((k_attention_join<D, 1024 / D>), dim3((uint32_t)rows), dim3(256), 0, stream, a, p.splits, po, pm);
     return hipGetLastError();
 }
 
