@@ -13,6 +13,9 @@
 #include "brq_launch.h"
 #include "mfma_fp4.h"
 
+#ifndef BRQ_OCC
+#define BRQ_OCC 2
+#endif
 namespace brq {
 namespace {
 
@@ -37,13 +40,20 @@ __device__ __forceinline__ bf16x8 eight_values(uint32_t w, uint32_t scale) {
     return __builtin_bit_cast(bf16x8, x);
 }
 
+// A load that is known to be from global memory.  The compiler loses sight of that behind uniform_ptr, and what it takes instead
+// counts as an access of LDS too: every wait for LDS, one in front of each barrier, would wait for the pages on their way.
+template <class T>
+__device__ __forceinline__ T load(const uint8_t* p) {
+    return *reinterpret_cast<const __attribute__((address_space(1))) T*>(reinterpret_cast<uintptr_t>(p));
+}
+
 template <int N>
 __device__ __forceinline__ void load_words(uint32_t (&r)[N], const uint8_t* p) {
     if constexpr (N == 4) {
-        const v4i x = *reinterpret_cast<const v4i*>(p);
+        const v4i x = load<v4i>(p);
         r[0] = (uint32_t)x.x; r[1] = (uint32_t)x.y; r[2] = (uint32_t)x.z; r[3] = (uint32_t)x.w;
     } else {
-        const v2i x = *reinterpret_cast<const v2i*>(p);
+        const v2i x = load<v2i>(p);
         r[0] = (uint32_t)x.x; r[1] = (uint32_t)x.y;
     }
 }
@@ -81,7 +91,7 @@ struct PageRegs {
 
 // Workgroup: sequence, cache head, split.  Wavefront w goes through pages first + w, first + w + 4, ...
 template <int D>
-__global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int splits, float* part_o, float* part_ml) {
+__global__ __launch_bounds__(256, BRQ_OCC) void k_attention_few(const AttnArgs a, int splits, float* part_o, float* part_ml) {
     constexpr int MT = D / 16, HB = kv4_head_bytes(D);
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int split = (int)blockIdx.x % splits, sh = (int)blockIdx.x / splits, s = sh / a.Hk, kvh = sh - s * a.Hk;
@@ -131,14 +141,14 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     float l = 0.0f, ref = 0.0f, top_ref = -INFINITY;      // ref: what is subtracted; top_ref: the same, -inf before any token
 
     const int32_t* row = a.table + (int64_t)s * a.table_cols;
-    auto load = [&](PageRegs<D>& r, int number) {
+    auto fetch = [&](PageRegs<D>& r, int number) {
         const uint8_t* h = uniform_ptr(a.pool + ((int64_t)number * a.Hk + kvh) * HB);
 #pragma unroll
         for (int u = 0; u < 4; ++u) load_words<D / 32>(r.k[u], h + (u * 64 + n * 4 + g) * (D / 8));
-        r.ks = *reinterpret_cast<const uint32_t*>(h + 32 * D + (g * D / 128 * 16 + n) * 4);
+        r.ks = load<uint32_t>(h + 32 * D + (g * D / 128 * 16 + n) * 4);
 #pragma unroll
         for (int u = 0; u < 4; ++u) load_words<D / 32>(r.v[u], h + 34 * D + (u * 64 + lane) * (D / 8));
-        r.vs = *reinterpret_cast<const v4i*>(h + 66 * D + (g * (D / 32) + n * D / 512) * 16);
+        r.vs = load<v4i>(h + 66 * D + (g * (D / 32) + n * D / 512) * 16);
     };
     auto use = [&](PageRegs<D>& r, int page) {
         const int t0 = page * kKv4Page;
@@ -245,14 +255,14 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
         };
         PageRegs<D> ra, rb;
         int pa = 0, pb = 0, na = next(&pa), nb;
-        if (na >= 0) load(ra, na);
+        if (na >= 0) fetch(ra, na);
         while (na >= 0) {
             nb = next(&pb);
-            if (nb >= 0) load(rb, nb);
+            if (nb >= 0) fetch(rb, nb);
             use(ra, pa);
             if (nb < 0) break;
             na = next(&pa);
-            if (na >= 0) load(ra, na);
+            if (na >= 0) fetch(ra, na);
             use(rb, pb);
         }
     }
@@ -385,11 +395,11 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
 #pragma unroll
             for (int k = 0; k < KS; ++k) load_words<4>(g.k[i][k], p + (i * 32 + n) * (D / 2) + k * 32 + h * 16);
 #pragma unroll
-        for (int k = 0; k < KS; ++k) g.ks[k] = *reinterpret_cast<const uint32_t*>(p + 32 * D + ((k * 2 + h) * 16 + (n & 15)) * 4);
+        for (int k = 0; k < KS; ++k) g.ks[k] = load<uint32_t>(p + 32 * D + ((k * 2 + h) * 16 + (n & 15)) * 4);
     };
     auto load_values = [&](ManyRegs<D>& g, const uint8_t* p) {
         load_words<D / 32>(g.v, p + 34 * D + (int)threadIdx.x * (D / 8));
-        g.vs = *reinterpret_cast<const uint32_t*>(p + 66 * D + ((vq & 3) * (D / 32) + vc * D / 512) * 16 + (vq >> 2) * 4);
+        g.vs = load<uint32_t>(p + 66 * D + ((vq & 3) * (D / 32) + vc * D / 512) * 16 + (vq >> 2) * 4);
     };
     auto unpack = [&](const ManyRegs<D>& g, int page, uint8_t* buf) {
         const int left = all - (page * kKv4Page + vq * 4);                            // tokens that are none: 0 times whatever they hold is to be 0
