@@ -7,7 +7,11 @@
 #include "brq_attn.h"
 #include "brq_device.h"
 #include "brq_launch.h"
+#include "mfma_fp4.h"
 
+#ifndef BRQ_WAVES
+#define BRQ_WAVES 8192
+#endif
 namespace brq {
 namespace {
 
@@ -116,11 +120,14 @@ __device__ __forceinline__ void store_chunk(uint8_t* p, const float (&v)[8]) {
 }
 
 __device__ __forceinline__ void load_weight(const float* w, uint32_t chunk, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 1.0f;
+    typedef float quad __attribute__((ext_vector_type(4), aligned(4)));          // (weights are aligned to 4 bytes, no more)
     if (w) {
+        const quad a = *reinterpret_cast<const quad*>(w + chunk * 8), b = *reinterpret_cast<const quad*>(w + chunk * 8 + 4);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = w[chunk * 8 + i];
+        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 1.0f;
     }
 }
 
@@ -134,83 +141,111 @@ __device__ __forceinline__ float sum_squares(const float (&v)[8]) {
     return a + b;
 }
 
-// One wavefront: token t, the groups part, part + splits, ... of 64/L heads; queries first, then keys, then values.
+// A lane's place in a wavefront's 64/L heads, and its walk over groups of that many heads of one token.
+template <int L>
+struct Walk {
+    const uint8_t* p;
+    int64_t step;
+    int h, n;                            // the lane's head, the number of heads
+    __device__ __forceinline__ Walk(const Heads& x, int64_t t, int group, uint32_t lane, uint32_t byte)
+        : p(x.p + t * x.ts + group * (64 / L) * x.hs + (int64_t)(lane / L) * x.hs + byte), step(x.hs * (64 / L)), h(group * (64 / L) + (int)(lane / L)), n(x.n) {}
+    __device__ __forceinline__ bool there() const { return h < n; }
+    // where to read: the last groups' lanes without a head read the first lane's, which there is
+    __device__ __forceinline__ const uint8_t* read(int64_t hs, uint32_t lane) const { return there() ? p : p - (int64_t)(lane / L) * hs; }
+    __device__ __forceinline__ void next() {
+        p += step;
+        h += 64 / L;
+    }
+};
+enum Kind { kQuery, kKey, kValue };
+
+// One wavefront: token t, `each` groups of 64/L heads from part * each on; groups are queries first, then keys, then values.
+// Everything but the lane's place is uniform and stays in scalar registers; the next group's load is under way while one is
+// worked on.
 template <int L, bool IN_BF16, bool OUT_BF16, bool APPEND>
-__global__ __launch_bounds__(256) void k_heads(const HeadsArgs a, int splits) {
+__global__ __launch_bounds__(256) void k_heads(const HeadsArgs a, int splits, int each) {
     constexpr int D = L * 8, HPW = 64 / L, ES = IN_BF16 ? 2 : 4, OS = OUT_BF16 ? 2 : 4;
     const uint32_t lane = threadIdx.x & 63u, l = lane & (L - 1), chunk = chunk_of_lane(l);
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t t = wave / splits;
     const int part = (int)(wave - t * splits);
     if (t >= a.T) return;
     const int nq = (a.q.n + HPW - 1) / HPW, nk = (a.k.n + HPW - 1) / HPW, nv = APPEND ? (a.v.n + HPW - 1) / HPW : 0;
+    const int begin = part * each, end = min(begin + each, nq + nk + nv);
     bool placed = true;
     Turn turn;
-    if (a.rope.rot) {
+    if (a.rope.rot && begin < nq + nk) {
         const int64_t row = a.rope.pos[t];
         placed = row >= 0 && row < a.rope.rows;
         turn.load(a.rope, placed ? row : 0, chunk, false);
     }
     int64_t slot = -1;
-    if constexpr (APPEND) slot = a.slots[t];
+    if constexpr (APPEND) {
+        slot = a.slots[t];
+        if (a.rope.rot && begin >= nq + nk) placed = a.rope.pos[t] >= 0 && a.rope.pos[t] < a.rope.rows;
+    }
     const bool write = placed && slot >= 0 && slot < a.num_slots;
     const int in_page = (int)(slot & (kKv4Page - 1));
-    for (int it = part; it < nq + nk + nv; it += splits) {
-        const bool is_q = it < nq, is_v = it >= nq + nk;
-        const Heads& src = is_q ? a.q : is_v ? a.v : a.k;
-        const int h = (it - (is_q ? 0 : is_v ? nq + nk : nq)) * HPW + (int)(lane / L);
-        const bool there = h < src.n;
-        float v[8];
-        load_chunk<IN_BF16>(src.p + t * src.ts + (there ? h : 0) * src.hs + chunk * 8 * ES, v);
-        if (!is_v) {
-            const float* wp = is_q ? a.wq : a.wk;
-            if (wp) {
-                float w[8];
-                load_weight(wp, chunk, w);
-                const float r = __builtin_amdgcn_rsqf(head_sum<L>(sum_squares(v)) * (1.0f / D) + a.eps);
+
+    auto segment = [&](auto kind, const Heads& src, const Heads& dst, const float* weight, int l2b, int g0, int g1) {
+        constexpr int K = decltype(kind)::value;
+        if (g0 >= g1) return;
+        constexpr bool STORE = !APPEND || K == kQuery;
+        Walk<L> in(src, t, g0, lane, chunk * 8 * ES), out(STORE ? dst : Heads{a.pool, 0, kv4_head_bytes(D), src.n}, STORE ? t : 0, g0, lane, STORE ? chunk * 8 * OS : 0);
+        if constexpr (!STORE) out.p += write ? slot / kKv4Page * a.Hk * kv4_head_bytes(D) : 0;
+        float w[8];
+        if (K != kValue && weight) load_weight(weight, chunk, w);
+        RawChunk<IN_BF16> raw = load_raw<IN_BF16>(in.read(src.hs, lane));
+        for (int it = g0; it < g1; ++it) {
+            float v[8];
+            widen<IN_BF16>(raw, v);
+            in.next();
+            if (it + 1 < g1) raw = load_raw<IN_BF16>(in.read(src.hs, lane));
+            if constexpr (K != kValue) {
+                if (weight) {
+                    const float r = __builtin_amdgcn_rsqf(head_sum<L>(sum_squares(v)) * (1.0f / D) + a.eps);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = v[i] * r * w[i];
+                    for (int i = 0; i < 8; ++i) v[i] = v[i] * r * w[i];
+                }
+                if (a.rope.rot) turn.apply<L>(v, a.rope, lane, chunk);
             }
-            if (a.rope.rot) turn.apply<L>(v, a.rope, lane, chunk);
-            rotate_block<L>(v, a.l2b, chunk);
-        } else {
-            rotate_block<L>(v, a.l2bv, chunk);
-        }
-        if (!APPEND || is_q) {
-            const Heads& dst = is_q ? a.qo : a.ko;
-            if (!placed) {
+            rotate_block<L>(v, l2b, chunk);
+            uint8_t* to = const_cast<uint8_t*>(out.p);
+            if constexpr (STORE) {
+                if (!placed) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = as_f32(0x7fc00000u);
-            }
-            if (there) store_chunk<OUT_BF16>(dst.p + t * dst.ts + h * dst.hs + chunk * 8 * OS, v);
-        }
-        if constexpr (APPEND) {
-            if (!is_q) {
+                    for (int i = 0; i < 8; ++i) v[i] = as_f32(0x7fc00000u);
+                }
+                if (out.there()) store_chunk<OUT_BF16>(to, v);
+            } else {
                 const uint32_t sb = e8m0_from_amax(quad_max(absmax8(v)));
                 const uint32_t codes = encode8_e2m1(v, sb);
-                if (write && there) {
-                    uint8_t* head = a.pool + ((slot / kKv4Page) * a.Hk + h) * kv4_head_bytes(D);
-                    if (!is_v) {
-                        *reinterpret_cast<uint32_t*>(head + kv4_key_code(D, in_page) + chunk * 4) = codes;
-                        if ((l & 3u) == 0) head[kv4_key_scale(D, in_page, (int)(chunk >> 2))] = (uint8_t)sb;
+                if (write && out.there()) {
+                    if constexpr (K == kKey) {
+                        *reinterpret_cast<uint32_t*>(to + kv4_key_code(D, in_page) + chunk * 4) = codes;
+                        if ((l & 3u) == 0) to[kv4_key_scale(D, in_page, (int)(chunk >> 2))] = (uint8_t)sb;
                     } else {
                         if constexpr (D == 128) {
-                            *reinterpret_cast<uint32_t*>(head + kv4_value_code(D, in_page, (int)chunk)) = codes;
+                            *reinterpret_cast<uint32_t*>(to + kv4_value_code(D, in_page, (int)chunk)) = codes;
                         } else {
-                            *reinterpret_cast<uint16_t*>(head + kv4_value_code(D, in_page, (int)chunk * 2)) = (uint16_t)codes;
-                            *reinterpret_cast<uint16_t*>(head + kv4_value_code(D, in_page, (int)chunk * 2 + 1)) = (uint16_t)(codes >> 16);
+                            *reinterpret_cast<uint16_t*>(to + kv4_value_code(D, in_page, (int)chunk * 2)) = (uint16_t)codes;
+                            *reinterpret_cast<uint16_t*>(to + kv4_value_code(D, in_page, (int)chunk * 2 + 1)) = (uint16_t)(codes >> 16);
                         }
-                        if ((l & 3u) == 0) head[kv4_value_scale(D, in_page, (int)(chunk >> 2))] = (uint8_t)sb;
+                        if ((l & 3u) == 0) to[kv4_value_scale(D, in_page, (int)(chunk >> 2))] = (uint8_t)sb;
                     }
                 }
             }
+            out.next();
         }
-    }
+    };
+    segment(IC<kQuery>{}, a.q, a.qo, a.wq, a.l2b, begin, min(end, nq));
+    segment(IC<kKey>{}, a.k, a.ko, a.wk, a.l2b, max(begin - nq, 0), min(end - nq, nk));
+    if constexpr (APPEND) segment(IC<kValue>{}, a.v, a.ko, nullptr, a.l2bv, max(begin - nq - nk, 0), end - nq - nk);
 }
 
 // Wavefronts of a launch: as many to a token as make about 8 for every SIMD together, at most one for each group of heads.
 int token_splits(int64_t T, int groups) {
-    const int64_t want = (8192 + T - 1) / T;
+    const int64_t want = (BRQ_WAVES + T - 1) / T;
     return (int)(want < groups ? want : groups);
 }
 
@@ -219,9 +254,9 @@ int token_splits(int64_t T, int groups) {
 hipError_t launch_heads(int D, bool in_bf16, bool out_bf16, bool append, const HeadsArgs& a, hipStream_t stream) {
     const int hpw = 512 / D;
     const int groups = (a.q.n + hpw - 1) / hpw + (a.k.n + hpw - 1) / hpw + (append ? (a.v.n + hpw - 1) / hpw : 0);
-    const int splits = token_splits(a.T, groups);
+    const int each = (groups + token_splits(a.T, groups) - 1) / token_splits(a.T, groups), splits = (groups + each - 1) / each;
     const dim3 grid((uint32_t)((a.T * splits + 3) / 4)), block(256);
-#define BRQ_HEADS(L_, IN, OUT, APP) hipLaunchKernelGGL((k_heads<L_, IN, OUT, APP>), grid, block, 0, stream, a, splits)
+#define BRQ_HEADS(L_, IN, OUT, APP) hipLaunchKernelGGL((k_heads<L_, IN, OUT, APP>), grid, block, 0, stream, a, splits, each)
 #define BRQ_HEADS_T(L_)                                                        \
     do {                                                                       \
         if (in_bf16 && out_bf16) BRQ_HEADS(L_, true, true, false);             \
@@ -245,15 +280,13 @@ namespace {
 // Backward.  A wavefront goes through (token, part) items with a stride and keeps both weights' gradients for its
 // lanes' channels in registers; a workgroup adds its wavefronts' up in LDS and writes one row of partial sums.
 template <int L, bool X_BF16, bool G_BF16>
-__global__ __launch_bounds__(256) void k_heads_backward(const HeadsArgs a, int splits) {
+__global__ __launch_bounds__(256) void k_heads_backward(const HeadsArgs a, int splits, int each) {
     constexpr int D = L * 8, HPW = 64 / L, ES = X_BF16 ? 2 : 4, GS = G_BF16 ? 2 : 4;
     const uint32_t lane = threadIdx.x & 63u, l = lane & (L - 1), chunk = chunk_of_lane(l);
     const int nq = (a.q.n + HPW - 1) / HPW, nk = (a.k.n + HPW - 1) / HPW;
-    float wq[8], wk[8], dw[2][8] = {};
-    load_weight(a.wq, chunk, wq);
-    load_weight(a.wk, chunk, wk);
+    float dw[2][8] = {};
     const int64_t items = a.T * splits;
-    for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
+    for (int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); item < items; item += (int64_t)gridDim.x * 4) {
         const int64_t t = item / splits;
         const int part = (int)(item - t * splits);
         Turn turn;
@@ -263,38 +296,54 @@ __global__ __launch_bounds__(256) void k_heads_backward(const HeadsArgs a, int s
             placed = row >= 0 && row < a.rope.rows;
             turn.load(a.rope, placed ? row : 0, chunk, true);
         }
-        for (int it = part; it < nq + nk; it += splits) {
-            const bool is_q = it < nq;
-            const Heads &src = is_q ? a.q : a.k, &gs = is_q ? a.gq : a.gk, &dst = is_q ? a.qo : a.ko;
-            const int h = (is_q ? it : it - nq) * HPW + (int)(lane / L);
-            const bool there = h < src.n;
-            float g[8];
-            load_chunk<G_BF16>(gs.p + t * gs.ts + (there ? h : 0) * gs.hs + chunk * 8 * GS, g);
-            rotate_block<L>(g, a.l2b, chunk);
-            if (a.rope.rot) turn.apply<L>(g, a.rope, lane, chunk);
-            if (!placed) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = as_f32(0x7fc00000u);
-            }
-            if (is_q ? a.wq != nullptr : a.wk != nullptr) {
-                float x[8], y[8];
-                load_chunk<X_BF16>(src.p + t * src.ts + (there ? h : 0) * src.hs + chunk * 8 * ES, x);
-                const float r = __builtin_amdgcn_rsqf(head_sum<L>(sum_squares(x)) * (1.0f / D) + a.eps);
-                float dot = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[i] *= r;                                                // u = x / rms
-                    y[i] = g[i] * (is_q ? wq[i] : wk[i]);
-                    dot = __builtin_fmaf(y[i], x[i], dot);
-                    const float gu = there ? g[i] * x[i] : 0.0f;
-                    if (is_q) dw[0][i] += gu; else dw[1][i] += gu;
+        const int begin = part * each, end = min(begin + each, nq + nk);
+        auto segment = [&](auto kind, const Heads& src, const Heads& grad, const Heads& dst, const float* weight, int g0, int g1) {
+            constexpr int K = decltype(kind)::value;
+            if (g0 >= g1) return;
+            Walk<L> in(src, t, g0, lane, chunk * 8 * ES), gr(grad, t, g0, lane, chunk * 8 * GS), out(dst, t, g0, lane, chunk * 8 * ES);
+            float w[8];
+            if (weight) load_weight(weight, chunk, w);
+            RawChunk<G_BF16> rg = load_raw<G_BF16>(gr.read(grad.hs, lane));
+            RawChunk<X_BF16> rx = {};
+            if (weight) rx = load_raw<X_BF16>(in.read(src.hs, lane));
+            for (int it = g0; it < g1; ++it) {
+                float g[8], x[8];
+                widen<G_BF16>(rg, g);
+                widen<X_BF16>(rx, x);
+                in.next();
+                gr.next();
+                if (it + 1 < g1) {
+                    rg = load_raw<G_BF16>(gr.read(grad.hs, lane));
+                    if (weight) rx = load_raw<X_BF16>(in.read(src.hs, lane));
                 }
-                const float mean = head_sum<L>(dot) * (1.0f / D);
+                rotate_block<L>(g, a.l2b, chunk);
+                if (a.rope.rot) turn.apply<L>(g, a.rope, lane, chunk);
+                if (!placed) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = r * (y[i] - x[i] * mean);
+                    for (int i = 0; i < 8; ++i) g[i] = as_f32(0x7fc00000u);
+                }
+                if (weight) {
+                    float y[8];
+                    const float r = __builtin_amdgcn_rsqf(head_sum<L>(sum_squares(x)) * (1.0f / D) + a.eps);
+                    float dot = 0.0f;
+                    const bool mine = out.there();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        x[i] *= r;                                            // u = x / rms
+                        y[i] = g[i] * w[i];
+                        dot = __builtin_fmaf(y[i], x[i], dot);
+                        dw[K][i] += mine ? g[i] * x[i] : 0.0f;
+                    }
+                    const float mean = head_sum<L>(dot) * (1.0f / D);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) g[i] = r * (y[i] - x[i] * mean);
+                }
+                if (out.there()) store_chunk<X_BF16>(const_cast<uint8_t*>(out.p), g);
+                out.next();
             }
-            if (there) store_chunk<X_BF16>(dst.p + t * dst.ts + h * dst.hs + chunk * 8 * ES, g);
-        }
+        };
+        segment(IC<kQuery>{}, a.q, a.gq, a.qo, a.wq, begin, min(end, nq));
+        segment(IC<kKey>{}, a.k, a.gk, a.ko, a.wk, max(begin - nq, 0), end - nq);
     }
     if (!a.partial) return;
     __shared__ float sum[4][2][D];
@@ -341,9 +390,9 @@ int64_t heads_backward_workgroups(int64_t T, int Hq, int Hk, int D) {
 
 hipError_t launch_heads_backward(int D, bool x_bf16, bool g_bf16, const HeadsArgs& a, hipStream_t stream) {
     const int hpw = 512 / D, groups = (a.q.n + hpw - 1) / hpw + (a.k.n + hpw - 1) / hpw;
-    const int splits = token_splits(a.T, groups);
+    const int each = (groups + token_splits(a.T, groups) - 1) / token_splits(a.T, groups), splits = (groups + each - 1) / each;
     const int wgs = (int)heads_backward_workgroups(a.T, a.q.n, a.k.n, D);
-#define BRQ_BACK(L_, X, G) hipLaunchKernelGGL((k_heads_backward<L_, X, G>), dim3(wgs), dim3(256), 0, stream, a, splits)
+#define BRQ_BACK(L_, X, G) hipLaunchKernelGGL((k_heads_backward<L_, X, G>), dim3(wgs), dim3(256), 0, stream, a, splits, each)
 #define BRQ_BACK_T(L_)                                          \
     do {                                                        \
         if (x_bf16 && g_bf16) BRQ_BACK(L_, true, true);         \
