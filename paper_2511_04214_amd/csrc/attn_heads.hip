@@ -9,9 +9,6 @@
 #include "brq_launch.h"
 #include "mfma_fp4.h"
 
-#ifndef BRQ_WAVES
-#define BRQ_WAVES 8192
-#endif
 namespace brq {
 namespace {
 
@@ -108,14 +105,20 @@ struct Turn {
     }
 };
 
-template <bool BF16>
+// STREAM: past the caches.  For the outputs of the forward and backward pass (8192 tokens, 168 MB of them: 97.2 -> 91.2 us one call after
+// the other, 101 -> 104 alone), not for queries on their way to attention (a step of 16 sequences 17.25 -> 17.45).
+template <bool STREAM, class T>
+__device__ __forceinline__ void store16(uint8_t* p, T x) {
+    if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<T*>(p));
+    else *reinterpret_cast<T*>(p) = x;
+}
+template <bool BF16, bool STREAM>
 __device__ __forceinline__ void store_chunk(uint8_t* p, const float (&v)[8]) {
     if constexpr (BF16) {
-        *reinterpret_cast<v4i*>(p) = v4i{(int)pack_bf16x2(v[0], v[1]), (int)pack_bf16x2(v[2], v[3]), (int)pack_bf16x2(v[4], v[5]),
-                                        (int)pack_bf16x2(v[6], v[7])};
+        store16<STREAM>(p, v4i{(int)pack_bf16x2(v[0], v[1]), (int)pack_bf16x2(v[2], v[3]), (int)pack_bf16x2(v[4], v[5]), (int)pack_bf16x2(v[6], v[7])});
     } else {
-        *reinterpret_cast<v4f*>(p) = v4f{v[0], v[1], v[2], v[3]};
-        *(reinterpret_cast<v4f*>(p) + 1) = v4f{v[4], v[5], v[6], v[7]};
+        store16<STREAM>(p, v4f{v[0], v[1], v[2], v[3]});
+        store16<STREAM>(p + 16, v4f{v[4], v[5], v[6], v[7]});
     }
 }
 
@@ -216,7 +219,7 @@ __global__ __launch_bounds__(256) void k_heads(const HeadsArgs a, int splits, in
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[i] = as_f32(0x7fc00000u);
                 }
-                if (out.there()) store_chunk<OUT_BF16>(to, v);
+                if (out.there()) store_chunk<OUT_BF16, !APPEND>(to, v);
             } else {
                 const uint32_t sb = e8m0_from_amax(quad_max(absmax8(v)));
                 const uint32_t codes = encode8_e2m1(v, sb);
@@ -245,7 +248,7 @@ __global__ __launch_bounds__(256) void k_heads(const HeadsArgs a, int splits, in
 
 // Wavefronts of a launch: as many to a token as make about 8 for every SIMD together, at most one for each group of heads.
 int token_splits(int64_t T, int groups) {
-    const int64_t want = (BRQ_WAVES + T - 1) / T;
+    const int64_t want = (8192 + T - 1) / T;
     return (int)(want < groups ? want : groups);
 }
 
@@ -280,7 +283,7 @@ namespace {
 // Backward.  A wavefront goes through (token, part) items with a stride and keeps both weights' gradients for its
 // lanes' channels in registers; a workgroup adds its wavefronts' up in LDS and writes one row of partial sums.
 template <int L, bool X_BF16, bool G_BF16>
-__global__ __launch_bounds__(256) void k_heads_backward(const HeadsArgs a, int splits, int each) {
+__global__ __launch_bounds__(256, 3) void k_heads_backward(const HeadsArgs a, int splits, int each) {
     constexpr int D = L * 8, HPW = 64 / L, ES = X_BF16 ? 2 : 4, GS = G_BF16 ? 2 : 4;
     const uint32_t lane = threadIdx.x & 63u, l = lane & (L - 1), chunk = chunk_of_lane(l);
     const int nq = (a.q.n + HPW - 1) / HPW, nk = (a.k.n + HPW - 1) / HPW;
@@ -338,7 +341,7 @@ __global__ __launch_bounds__(256) void k_heads_backward(const HeadsArgs a, int s
 #pragma unroll
                     for (int i = 0; i < 8; ++i) g[i] = r * (y[i] - x[i] * mean);
                 }
-                if (out.there()) store_chunk<X_BF16>(const_cast<uint8_t*>(out.p), g);
+                if (out.there()) store_chunk<X_BF16, true>(const_cast<uint8_t*>(out.p), g);
                 out.next();
             }
         };
@@ -363,18 +366,19 @@ __global__ __launch_bounds__(256) void k_heads_backward(const HeadsArgs a, int s
     }
 }
 
-// Sums of the partial sums' columns: 16 columns a workgroup, 16 threads each.
-__global__ __launch_bounds__(256) void k_heads_weight_grads(const float* partial, int rows, int D, float* dwq, float* dwk) {
-    __shared__ float sum[16][17];
+// Sums of the partial sums' columns: 16 columns a workgroup, 64 threads each.
+__global__ __launch_bounds__(1024) void k_heads_weight_grads(const float* partial, int rows, int D, float* dwq, float* dwk) {
+    __shared__ float sum[64][17];
     const int c = (int)blockIdx.x * 16 + (int)(threadIdx.x & 15u), r0 = (int)(threadIdx.x >> 4);
     float v = 0.0f;
-#pragma unroll 8
-    for (int r = r0; r < rows; r += 16) v += partial[(int64_t)r * (2 * D) + c];
+#pragma unroll 4
+    for (int r = r0; r < rows; r += 64) v += partial[(int64_t)r * (2 * D) + c];
     sum[r0][threadIdx.x & 15u] = v;
     __syncthreads();
     if (threadIdx.x < 16) {
         float s = 0.0f;
-        for (int i = 0; i < 16; ++i) s += sum[i][threadIdx.x];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) s += sum[i][threadIdx.x];
         float* out = c < D ? dwq : dwk;
         if (out) out[c < D ? c : c - D] = s;
     }
@@ -385,7 +389,7 @@ __global__ __launch_bounds__(256) void k_heads_weight_grads(const float* partial
 int64_t heads_backward_workgroups(int64_t T, int Hq, int Hk, int D) {
     const int hpw = 512 / D, groups = (Hq + hpw - 1) / hpw + (Hk + hpw - 1) / hpw;
     const int64_t n = (T * token_splits(T, groups) + 3) / 4;
-    return n < 1024 ? n : 1024;
+    return n < 768 ? n : 768;                        // three to a CU, as many as its registers hold
 }
 
 hipError_t launch_heads_backward(int D, bool x_bf16, bool g_bf16, const HeadsArgs& a, hipStream_t stream) {
@@ -410,7 +414,7 @@ hipError_t launch_heads_backward(int D, bool x_bf16, bool g_bf16, const HeadsArg
 }
 
 hipError_t launch_heads_weight_grads(const float* partial, int rows, int D, float* dwq, float* dwk, hipStream_t stream) {
-    hipLaunchKernelGGL(k_heads_weight_grads, dim3(2 * D / 16), dim3(256), 0, stream, partial, rows, D, dwq, dwk);
+    hipLaunchKernelGGL(k_heads_weight_grads, dim3(2 * D / 16), dim3(1024), 0, stream, partial, rows, D, dwq, dwk);
     return hipGetLastError();
 }
 
@@ -451,8 +455,8 @@ __global__ __launch_bounds__(256) void k_kv4_read(const uint8_t* pool, int64_t n
 #pragma unroll
         for (int j = 0; j < 16; ++j) x[j >> 3][j & 7] = as_f32(0x7fc00000u);
     }
-    store_chunk<OUT_BF16>(k.p + t * k.ts + h * k.hs + chunk * 8 * OS, x[0]);
-    store_chunk<OUT_BF16>(v.p + t * v.ts + h * v.hs + chunk * 8 * OS, x[1]);
+    store_chunk<OUT_BF16, false>(k.p + t * k.ts + h * k.hs + chunk * 8 * OS, x[0]);
+    store_chunk<OUT_BF16, false>(v.p + t * v.ts + h * v.hs + chunk * 8 * OS, x[1]);
 }
 
 }  // namespace
