@@ -12,21 +12,22 @@ namespace {
 constexpr int kScan = 1024;       // threads of the workgroup that counts
 constexpr int kPer = 16;          // page counts a thread and step
 
-// Sum of v over the workgroup's threads in front of this one; *total: over all.  lds: 17 ints, free on return after the next barrier.
-__device__ __forceinline__ int scan_before(int v, int* lds, int* total) {
+// Sum of v over the workgroup's threads in front of this one; *total: over all.  T: an integer, or two counts in one.
+template <class T>
+__device__ __forceinline__ T scan_before(T v, T* lds, T* total) {
     const int lane = (int)(threadIdx.x & 63u), w = (int)(threadIdx.x >> 6);
-    int x = v;
+    T x = v;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-        const int y = __shfl_up(x, d);
+        const T y = __shfl_up(x, d);
         if (lane >= d) x += y;
     }
     if (lane == 63) lds[w] = x;
     __syncthreads();
-    int before = 0, all = 0;
+    T before = 0, all = 0;
 #pragma unroll
     for (int i = 0; i < kScan / 64; ++i) {
-        const int n = lds[i];
+        const T n = lds[i];
         before += i < w ? n : 0;
         all += n;
     }
@@ -91,11 +92,43 @@ __device__ __forceinline__ int wanted(const PagesArgs& a, int i) {
     }
 }
 
-template <bool FORK>
+// A wavefront fills the empty columns of item i's row; `found`: how many pages there are for all.
+__device__ __forceinline__ void fill_row(const PagesArgs& a, const Found& f, int i, int found, int lane) {
+    const int s = a.a[i], tokens = a.b[i];
+    if (!in_range(s, a.S) || tokens <= 0) return;
+    const int cols = (tokens - 1) / kKv4Page + 1;
+    int32_t* row = a.table + (int64_t)s * a.cols;
+    bool failed = cols > a.cols;
+    int need = 0;
+    if (!failed) {
+        for (int c0 = 0; c0 < cols; c0 += 64) need += __popcll(__ballot(c0 + lane < cols && row[c0 + lane] < 0));
+        failed = need > 0 && (int64_t)f.first[i] + need > found;
+    }
+    if (failed) {
+        if (lane == 0) atomicAdd(a.result, 1);
+        return;
+    }
+    int at = f.first[i];
+    for (int c0 = 0; c0 < cols && need > 0; c0 += 64) {
+        const bool empty = c0 + lane < cols && row[c0 + lane] < 0;
+        const uint64_t m = __ballot(empty);
+        if (empty) {
+            const int page = f.pages[at + __popcll(m & ((1ull << lane) - 1))];
+            row[c0 + lane] = page;
+            a.refs[page] = 1;
+        }
+        at += __popcll(m);
+    }
+}
+
+// FILL: reservations of few sequences are made by the same workgroup, a wavefront a row (up to 64 of them: a launch saved is worth
+// four rounds of its 16 wavefronts).
+template <bool FORK, bool FILL>
 __global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
     __shared__ int lds[17];
     const Found f(a.workspace, a.n);
-    int want = 0, total;
+    int want = 0, total, r[kPer];
+    load_refs(a.refs, a.num_pages, (int)threadIdx.x * kPer, r);                   // (on their way while the wants are counted)
     for (int i0 = 0; i0 < a.n; i0 += kScan) {
         const int i = i0 + (int)threadIdx.x, w = i < a.n ? wanted<FORK>(a, i) : 0;
         const int before = scan_before(w > 0 ? w : 0, lds, &total);
@@ -104,9 +137,9 @@ __global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
     }
     int found = 0;
     for (int at = 0; at < a.num_pages && found < want; at += kScan * kPer) {
-        int r[kPer], n = 0;
+        int n = 0;
         const int mine = at + (int)threadIdx.x * kPer;
-        load_refs(a.refs, a.num_pages, mine, r);
+        if (at > 0) load_refs(a.refs, a.num_pages, mine, r);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) n += r[i] == 0;
         int rank = found + scan_before(n, lds, &total);
@@ -121,6 +154,10 @@ __global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
     if (threadIdx.x == 0) {
         f.count[0] = min(found, want);
         a.result[0] = 0;
+    }
+    if constexpr (FILL) {
+        __syncthreads();
+        for (int i = (int)(threadIdx.x >> 6); i < a.n; i += kScan / 64) fill_row(a, f, i, min(found, want), (int)(threadIdx.x & 63u));
     }
 }
 
@@ -159,35 +196,9 @@ __global__ __launch_bounds__(256) void k_fork(const PagesArgs a, int parts) {
     }
 }
 
-// A wavefront fills the empty columns of one row.
 __global__ __launch_bounds__(64) void k_reserve(const PagesArgs a) {
-    const int i = (int)blockIdx.x, lane = (int)threadIdx.x;
     const Found f(a.workspace, a.n);
-    const int s = a.a[i], tokens = a.b[i];
-    if (!in_range(s, a.S) || tokens <= 0) return;
-    const int cols = (tokens - 1) / kKv4Page + 1;
-    int32_t* row = a.table + (int64_t)s * a.cols;
-    bool failed = cols > a.cols;
-    int need = 0;
-    if (!failed) {
-        for (int c0 = 0; c0 < cols; c0 += 64) need += __popcll(__ballot(c0 + lane < cols && row[c0 + lane] < 0));
-        failed = need > 0 && (int64_t)f.first[i] + need > f.count[0];
-    }
-    if (failed) {
-        if (lane == 0) atomicAdd(a.result, 1);
-        return;
-    }
-    int at = f.first[i];
-    for (int c0 = 0; c0 < cols && need > 0; c0 += 64) {
-        const bool empty = c0 + lane < cols && row[c0 + lane] < 0;
-        const uint64_t m = __ballot(empty);
-        if (empty) {
-            const int page = f.pages[at + __popcll(m & ((1ull << lane) - 1))];
-            row[c0 + lane] = page;
-            a.refs[page] = 1;
-        }
-        at += __popcll(m);
-    }
+    fill_row(a, f, (int)blockIdx.x, f.count[0], (int)threadIdx.x);
 }
 
 // The entry is taken out by an exchange: a sequence named twice is given up once.
@@ -208,18 +219,20 @@ __global__ __launch_bounds__(256) void k_copy(const PagesArgs a, int parts) {
     if (in_range(s, a.num_pages) && in_range(d, a.num_pages) && s != d) move_page(a.pool, a.page_bytes, s, d, part, parts);
 }
 
-// ---- compaction.  Workspace: [0] moves, pairs from[N/2 + 1], to[N/2 + 1], then map[N].
+// ---- compaction.  Workspace: [0] moves, [1] live pages, from[N/2 + 1], to[N/2 + 1], then rank[N]: of the live pages above, which move theirs is.
 struct Moves {
-    int32_t *count, *from, *to, *map;
-    __host__ __device__ Moves(int32_t* w, int n) : count(w), from(w + 4), to(w + 4 + n / 2 + 1), map(w + 4 + 2 * (n / 2 + 1)) {}
+    int32_t *count, *from, *to, *rank;
+    __host__ __device__ Moves(int32_t* w, int n) : count(w), from(w + 4), to(w + 4 + n / 2 + 1), rank(w + 4 + 2 * (n / 2 + 1)) {}
 };
 
 __global__ __launch_bounds__(kScan) void k_plan_moves(const PagesArgs a) {
     __shared__ int lds[17];
+    __shared__ uint64_t lds2[17];
     const Moves v(a.workspace, a.num_pages);
-    int live = 0, total;
-    for (int at = 0; at < a.num_pages; at += kScan * kPer) {
-        int r[kPer], n = 0;
+    constexpr int kStep = kScan * kPer;
+    int live = 0, total, r[kPer];
+    for (int at = 0; at < a.num_pages; at += kStep) {
+        int n = 0;
         load_refs(a.refs, a.num_pages, at + (int)threadIdx.x * kPer, r);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) n += r[i] > 0;
@@ -228,28 +241,30 @@ __global__ __launch_bounds__(kScan) void k_plan_moves(const PagesArgs a) {
     }
     // free pages below `live` and live pages at or above it: as many of one as of the other
     int holes = 0, high = 0;
-    for (int at = 0; at < a.num_pages; at += kScan * kPer) {
-        int r[kPer], nh = 0, ns = 0;
+    for (int at = 0; at < a.num_pages; at += kStep) {
+        uint32_t nh = 0, ns = 0;
         const int mine = at + (int)threadIdx.x * kPer;
-        load_refs(a.refs, a.num_pages, mine, r);
+        if (a.num_pages > kStep) load_refs(a.refs, a.num_pages, mine, r);         // (otherwise they are still there)
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             nh += r[i] <= 0 && mine + i < live;
             ns += r[i] > 0 && mine + i >= live;
         }
-        int total_high;
-        int hole = holes + scan_before(nh, lds, &total), src = high + scan_before(ns, lds, &total_high);
+        uint64_t both;
+        const uint64_t before = scan_before((uint64_t)ns << 32 | nh, lds2, &both);
+        int hole = holes + (int)(uint32_t)before, src = high + (int)(before >> 32);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            if (r[i] <= 0 && mine + i < live) v.to[hole++] = mine + i;
-            if (r[i] > 0 && mine + i >= live) v.from[src++] = mine + i;
-            if (r[i] <= 0 && mine + i >= live && mine + i < a.num_pages) v.map[mine + i] = -1;       // an entry that names a free page
+            if (mine + i < live) {
+                if (r[i] <= 0) v.to[hole++] = mine + i;
+            } else if (mine + i < a.num_pages) {
+                v.rank[mine + i] = r[i] > 0 ? src : -1;                           // -1: an entry that names a free page
+                if (r[i] > 0) v.from[src++] = mine + i;
+            }
         }
-        holes += total;
-        high += total_high;
+        holes += (int)(uint32_t)both;
+        high += (int)(both >> 32);
     }
-    __syncthreads();
-    for (int k = (int)threadIdx.x; k < high; k += kScan) v.map[v.from[k]] = v.to[k];
     if (threadIdx.x == 0) {
         v.count[0] = high;
         v.count[1] = live;
@@ -271,7 +286,10 @@ __global__ __launch_bounds__(256) void k_move(const PagesArgs a, int parts) {
     const int64_t entries = (int64_t)a.S * a.cols;
     for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < entries; k += (int64_t)gridDim.x * 256) {
         const int e = a.table[k];
-        if (e >= live && e < a.num_pages) a.table[k] = v.map[e];
+        if (e >= live && e < a.num_pages) {
+            const int m = v.rank[e];
+            a.table[k] = m < 0 ? -1 : v.to[m];
+        }
     }
 }
 
@@ -287,7 +305,7 @@ hipError_t launch_pages_copy(const PagesArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL(k_find_free<true>, dim3(1), dim3(kScan), 0, stream, a);
+    hipLaunchKernelGGL((k_find_free<true, false>), dim3(1), dim3(kScan), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (a.n == 0) return hipSuccess;
     const int parts = parts_of(a.page_bytes);
@@ -301,9 +319,12 @@ hipError_t launch_pages_free(const PagesArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL(k_find_free<false>, dim3(1), dim3(kScan), 0, stream, a);
+    if (a.n <= 64) {
+        hipLaunchKernelGGL((k_find_free<false, true>), dim3(1), dim3(kScan), 0, stream, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((k_find_free<false, false>), dim3(1), dim3(kScan), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (a.n == 0) return hipSuccess;
     hipLaunchKernelGGL(k_reserve, dim3((uint32_t)a.n), dim3(64), 0, stream, a);
     return hipGetLastError();
 }

@@ -97,7 +97,7 @@ def ints(x):
     return torch.tensor(list(x), dtype=I32, device="cuda")
 
 
-@pytest.mark.parametrize("pages,seqs,cols,page_bytes,seed", [(40, 6, 5, 16, 0), (3000, 50, 20, 4352, 1), (20000, 40, 70, 32, 2), (33, 8, 3, 8704 * 3, 3), (200, 70, 4, 16400, 4)])
+@pytest.mark.parametrize("pages,seqs,cols,page_bytes,seed", [(40, 6, 5, 16, 0), (3000, 50, 20, 4352, 1), (20000, 40, 70, 32, 2), (33, 8, 3, 8704 * 3, 3), (200, 70, 4, 16400, 4), (40000, 400, 90, 16, 5)])
 def test_a_scheduler_s_day(pages, seqs, cols, page_bytes, seed):
     r = random.Random(seed)
     half = seqs // 2
