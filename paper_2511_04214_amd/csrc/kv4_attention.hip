@@ -13,6 +13,20 @@
 #include "brq_launch.h"
 #include "mfma_fp4.h"
 
+#ifndef BRQ_SCHED
+#define BRQ_SCHED 0
+#endif
+#if BRQ_SCHED == 0
+#define BRQ_SCHED1
+#define BRQ_SCHED2
+#else
+template <int N, int V>
+__device__ __forceinline__ void sched1() { if constexpr (N > 0) { __builtin_amdgcn_sched_group_barrier(0x2, V, 0); __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); sched1<N - 1, V>(); } }
+template <int N, int V>
+__device__ __forceinline__ void sched2() { if constexpr (N > 0) { __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, V, 0); __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); sched2<N - 1, V>(); } }
+#define BRQ_SCHED1 sched1<D / 16, BRQ_SCHED>();
+#define BRQ_SCHED2 sched2<2 * MT, 5>();
+#endif
 #ifndef BRQ_OCC
 #define BRQ_OCC 2
 #endif
@@ -40,20 +54,22 @@ __device__ __forceinline__ bf16x8 eight_values(uint32_t w, uint32_t scale) {
     return __builtin_bit_cast(bf16x8, x);
 }
 
-// A load that is known to be from global memory.  The compiler loses sight of that behind uniform_ptr, and what it takes instead
-// counts as an access of LDS too: every wait for LDS, one in front of each barrier, would wait for the pages on their way.
+// A load that is known to be from global memory, at a uniform address and a lane's 32-bit offset.  The compiler loses sight of the
+// first behind uniform_ptr, and what it takes instead counts as an access of LDS too: every wait for LDS, one in front of each
+// barrier, would wait for the pages on their way.
 template <class T>
-__device__ __forceinline__ T load(const uint8_t* p) {
-    return *reinterpret_cast<const __attribute__((address_space(1))) T*>(reinterpret_cast<uintptr_t>(p));
+__device__ __forceinline__ T load(const uint8_t* p, uint32_t off) {
+    typedef const __attribute__((address_space(1))) uint8_t* global;
+    return *reinterpret_cast<const __attribute__((address_space(1))) T*>(reinterpret_cast<global>(reinterpret_cast<uintptr_t>(p)) + off);
 }
 
 template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&r)[N], const uint8_t* p) {
+__device__ __forceinline__ void load_words(uint32_t (&r)[N], const uint8_t* p, uint32_t off) {
     if constexpr (N == 4) {
-        const v4i x = load<v4i>(p);
+        const v4i x = load<v4i>(p, off);
         r[0] = (uint32_t)x.x; r[1] = (uint32_t)x.y; r[2] = (uint32_t)x.z; r[3] = (uint32_t)x.w;
     } else {
-        const v2i x = load<v2i>(p);
+        const v2i x = load<v2i>(p, off);
         r[0] = (uint32_t)x.x; r[1] = (uint32_t)x.y;
     }
 }
@@ -75,6 +91,10 @@ __device__ __forceinline__ void query_rows(const AttnArgs& a, int s, int64_t* q0
     *q0 = b;
     *n = b < 0 || e > a.T || e <= b ? 0 : (int)min(e - b, (int64_t)a.max_q);
 }
+
+// A value that is the same in every lane, in a scalar register: an instruction with two vector operands issues in 2.8 cycles (two
+// wavefronts a SIMD), one with three in 4.6.
+__device__ __forceinline__ float uniform_f32(float v) { return as_f32(__builtin_amdgcn_readfirstlane(as_u32(v))); }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -133,7 +153,7 @@ __global__ __launch_bounds__(256, BRQ_OCC) void k_attention_few(const AttnArgs a
             q[k] = __builtin_bit_cast(bf16x8, n < rows ? x : zero);
         }
     }
-    const float c = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);
+    const float c = uniform_f32(fmaxf(fabsf(a.scale) * kLog2e, 1e-30f));
 
     v4f o[MT];
 #pragma unroll
@@ -144,11 +164,11 @@ __global__ __launch_bounds__(256, BRQ_OCC) void k_attention_few(const AttnArgs a
     auto fetch = [&](PageRegs<D>& r, int number) {
         const uint8_t* h = uniform_ptr(a.pool + ((int64_t)number * a.Hk + kvh) * HB);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load_words<D / 32>(r.k[u], h + (u * 64 + n * 4 + g) * (D / 8));
-        r.ks = load<uint32_t>(h + 32 * D + (g * D / 128 * 16 + n) * 4);
+        for (int u = 0; u < 4; ++u) load_words<D / 32>(r.k[u], h + u * 8 * D, (uint32_t)((n * 4 + g) * (D / 8)));
+        r.ks = load<uint32_t>(h + 32 * D, (uint32_t)((g * D / 128 * 16 + n) * 4));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load_words<D / 32>(r.v[u], h + 34 * D + (u * 64 + lane) * (D / 8));
-        r.vs = load<v4i>(h + 66 * D + (g * (D / 32) + n * D / 512) * 16);
+        for (int u = 0; u < 4; ++u) load_words<D / 32>(r.v[u], h + 34 * D + u * 8 * D, (uint32_t)(lane * (D / 8)));
+        r.vs = load<v4i>(h + 66 * D, (uint32_t)((g * (D / 32) + n * D / 512) * 16));
     };
     auto use = [&](PageRegs<D>& r, int page) {
         const int t0 = page * kKv4Page;
@@ -312,13 +332,15 @@ __global__ __launch_bounds__(256, BRQ_OCC) void k_attention_few(const AttnArgs a
 
 // ---- many query rows: prompts and chunks
 
-// A page of one head as a wavefront takes its keys (all 64 tokens, 32 x 32 x 64 products) and a thread its share of the values.
+// Keys of 32 tokens as a wavefront takes them: token lane % 32, channels 64 s + 32 (lane / 32) ...; and a thread's share of a page's
+// values, 4 tokens of a column.
 template <int D>
-struct ManyRegs {
-    uint32_t k[2][D / 64][4];    // tokens 32 i + lane % 32, channels 64 s + 32 (lane / 32) ...
-    uint32_t ks[D / 64];
-    uint32_t v[D / 32];          // 4 tokens of a column
-    uint32_t vs;
+struct Keys {
+    uint32_t k[D / 64][4], s[D / 64];
+};
+template <int D>
+struct Values {
+    uint32_t v[D / 32], s;
 };
 
 // Workgroup: 128 rows (query tokens x heads of a group) of a sequence and cache head, 32 to a wavefront, against the pages of a
@@ -346,22 +368,19 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
     const int len = a.kv_lens[s], all = min(len, min(a.max_kv, a.table_cols * kKv4Page));
     const int first = len - (a.cu_q ? (int)(a.cu_q[s + 1] - a.cu_q[s]) : 1);          // position of the sequence's first row
     const int r = r0 + w * 32 + n, rc = min(r, rows - 1), tok = rc / a.G, head = kvh * a.G + (rc - tok * a.G);
-    // tokens that a row of the workgroup sees; that every row of the wavefront sees, and any; that this lane's row sees
-    int begin = 0, end = all, begin_wg = 0, end_wg = all, begin_all = 0, end_all = all, begin_any = 0, end_any = all;
+    // tokens that a row of the workgroup sees; that every row of the wavefront sees; that this lane's row sees
+    int begin = 0, end = all, begin_wg = 0, end_wg = all, begin_all = 0, end_all = all;
     if (a.causal) {
         const int wa = min(r0 + w * 32, rows - 1) / a.G, wb = min(r0 + w * 32 + 31, rows - 1) / a.G, ga = r0 / a.G, gb = min(r0 + 127, rows - 1) / a.G;
         end = min(all, first + tok + 1);
         end_all = min(all, first + wa + 1);
-        end_any = min(all, first + wb + 1);
         end_wg = min(all, first + gb + 1);
         if (a.window) {
             begin = max(0, first + tok - a.window + 1);
             begin_all = max(0, first + wb - a.window + 1);
-            begin_any = max(0, first + wa - a.window + 1);
             begin_wg = max(0, first + ga - a.window + 1);
         }
     }
-    if (r0 + w * 32 >= rows) end_any = 0;                // a wavefront without rows only unpacks
     int page0, page1;
     split_pages(begin_wg / kKv4Page, (max(end_wg, 0) + kKv4Page - 1) / kKv4Page, split, splits, 1, &page0, &page1);
 
@@ -377,7 +396,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
                 q[k][j] = __builtin_bit_cast(bf16x8, x);
             }
     }
-    const float c = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);
+    const float c = uniform_f32(fmaxf(fabsf(a.scale) * kLog2e, 1e-30f));
 
     v16f o[MT];
 #pragma unroll
@@ -389,21 +408,20 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
     const int vq = (int)threadIdx.x >> 4, vc = (int)threadIdx.x & 15;                 // this thread's quad of tokens and column of the values
     const int vpos = ((vq & ~3) | ((vq & 1) << 1) | ((vq >> 1) & 1)) * 8;             // where the quad lies in a row of LDS
     auto page_at = [&](int number) { return uniform_ptr(a.pool + ((int64_t)number * a.Hk + kvh) * HB); };
-    auto load_keys = [&](ManyRegs<D>& g, const uint8_t* p) {
+    auto load_keys = [&](int half, Keys<D>& g, const uint8_t* p) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int k = 0; k < KS; ++k) load_words<4>(g.k[i][k], p + (i * 32 + n) * (D / 2) + k * 32 + h * 16);
-#pragma unroll
-        for (int k = 0; k < KS; ++k) g.ks[k] = load<uint32_t>(p + 32 * D + ((k * 2 + h) * 16 + (n & 15)) * 4);
+        for (int k = 0; k < KS; ++k) {
+            load_words<4>(g.k[k], p + half * 16 * D + k * 32, (uint32_t)(n * (D / 2) + h * 16));
+            g.s[k] = load<uint32_t>(p + 32 * D + k * 128, (uint32_t)((h * 16 + (n & 15)) * 4));
+        }
     };
-    auto load_values = [&](ManyRegs<D>& g, const uint8_t* p) {
-        load_words<D / 32>(g.v, p + 34 * D + (int)threadIdx.x * (D / 8));
-        g.vs = load<uint32_t>(p + 66 * D + ((vq & 3) * (D / 32) + vc * D / 512) * 16 + (vq >> 2) * 4);
+    auto load_values = [&](Values<D>& g, const uint8_t* p) {
+        load_words<D / 32>(g.v, p + 34 * D, threadIdx.x * (D / 8));
+        g.s = load<uint32_t>(p + 66 * D, (uint32_t)(((vq & 3) * (D / 32) + vc * D / 512) * 16 + (vq >> 2) * 4));
     };
-    auto unpack = [&](const ManyRegs<D>& g, int page, uint8_t* buf) {
+    auto unpack = [&](const Values<D>& g, int page, uint8_t* buf) {
         const int left = all - (page * kKv4Page + vq * 4);                            // tokens that are none: 0 times whatever they hold is to be 0
-        const uint32_t sb = left >= 4 ? g.vs : left <= 0 ? 0u : g.vs & ((1u << (8 * left)) - 1u);
+        const uint32_t sb = g.s & (uint32_t)((1ull << (8 * min(max(left, 0), 4))) - 1);
         const uint32_t sc[4] = {scale_of<0>(sb), scale_of<1>(sb), scale_of<2>(sb), scale_of<3>(sb)};
         static_for([&](auto ib) {
             constexpr int b = decltype(ib)::value;
@@ -423,106 +441,134 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
             *reinterpret_cast<v2i*>(buf + ((2 * b + 1) * 16 + vc) * ROW + vpos) = odd;
         }, IC<D / 32>{});
     };
-    auto use = [&](ManyRegs<D>& g, int page, const uint8_t* buf, const uint8_t* following) {      // following: whose keys come next into g, null: none
-        const int t0 = page * kKv4Page;
-        const bool mine = t0 < end_any && t0 + kKv4Page > begin_any;                  // some row of the wavefront sees some of it
-        v4i pw[4];
-        if (mine) {
-            v16f x[2];
-            static_for([&](auto ii) {
-                constexpr int i = decltype(ii)::value;
+    // of tokens 32 half ... 32 half + 31 of a page
+    auto scores = [&](auto half, const Keys<D>& g, v16f& x) {
+        v16f y = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[i][e] = 0.0f;
+        for (int k = 0; k < KS; ++k) {
+            const uint32_t sc = scale_of<2 * decltype(half)::value>(g.s[k] >> (n & 16 ? 8 : 0));
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const uint32_t sc = scale_of<2 * i>(g.ks[k] >> (n & 16 ? 8 : 0));
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_values(g.k[i][k][j], sc), q[k][j], x[i], 0, 0, 0);
-                }
-            }, IC<2>{});
-            if (following) load_keys(g, following);
-            if (t0 < begin_all || t0 + kKv4Page > end_all) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int t = t0 + i * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
-                        x[i][e] = t >= begin && t < end ? x[i][e] : -INFINITY;
-                    }
-            }
-            float top = fmaxf(x[0][0], x[1][0]);
-#pragma unroll
-            for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(top, x[0][e]), x[1][e]);
-            top *= c;
-            if (__any(top > top_ref + 8.0f)) {
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = fmaxf(top, top_ref), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top_ref - now);
-                top_ref = now;
-                ref = now == -INFINITY ? 0.0f : now;
-                l *= f;
-#pragma unroll
-                for (int j = 0; j < MT; ++j) o[j] *= f;
-            }
-#pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st >> 1][(st & 1) * 8 + e], c, -ref));
-                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st >> 1][(st & 1) * 8 + e + 1], c, -ref));
-                    l += e0 + e1;
-                    pw[st][e >> 1] = (int)pack_bf16x2(e0, e1);
-                }
-        } else if (following) {
-            load_keys(g, following);
+            for (int j = 0; j < 4; ++j) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_values(g.k[k][j], sc), q[k][j], y, 0, 0, 0);
         }
-        lds_wait_and_barrier();
-        if (mine) {
+        x = y;
+    };
+    // what is not seen
+    auto mask = [&](v16f& x, int t0) {
+        if (t0 < begin_all || t0 + 32 > end_all) {
+            asm volatile("");                            // (a branch: few pages need it, and without one all would pay for it)
 #pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll
-                for (int j = 0; j < MT; ++j) {
-                    const v4i vv = *reinterpret_cast<const v4i*>(buf + (j * 32 + n) * ROW + st * 32 + h * 16);
-                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vv), __builtin_bit_cast(bf16x8, pw[st]), o[j], 0, 0, 0);
-                }
+            for (int e = 0; e < 16; ++e) {
+                const int t = t0 + 8 * (e >> 2) + 4 * h + (e & 3);
+                x[e] = t >= begin && t < end ? x[e] : -INFINITY;
+            }
         }
     };
+    auto largest = [&](const v16f& x) {
+        float top = x[0];
+#pragma unroll
+        for (int e = 1; e < 15; e += 2) top = fmaxf(fmaxf(top, x[e]), x[e + 1]);
+        return fmaxf(top, x[15]) * c;
+    };
+    // a new reference where a score is 2^8 above the old one
+    auto settle = [&](float top) {
+        if (__any(top > top_ref + 8.0f)) {
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float now = fmaxf(top, top_ref), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top_ref - now);
+            top_ref = now;
+            ref = now == -INFINITY ? 0.0f : now;
+            l *= f;
+#pragma unroll
+            for (int j = 0; j < MT; ++j) o[j] *= f;
+        }
+    };
+    auto weights = [&](const v16f& x, v4i (&pw)[2]) {
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st * 8 + e], c, -ref));
+                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st * 8 + e + 1], c, -ref));
+                l += e0 + e1;
+                pw[st][e >> 1] = (int)pack_bf16x2(e0, e1);
+            }
+        asm volatile("" : "+v"(l));                      // (the compiler would add them up where l is next used, and keep them all until then)
+    };
+    auto add = [&](int half, const v4i (&pw)[2], const uint8_t* buf) {
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                const v4i vv = *reinterpret_cast<const v4i*>(buf + (j * 32 + n) * ROW + (half * 2 + st) * 32 + h * 16);
+                o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vv), __builtin_bit_cast(bf16x8, pw[st]), o[j], 0, 0, 0);
+            }
+    };
 
+    // pages in order, 64 numbers at a time, one a lane
     const int32_t* row = a.table + (int64_t)s * a.table_cols;
-    for (int chunk = page0; chunk < page1; chunk += 64) {
-        const int entry = chunk + lane < page1 ? row[chunk + lane] : -1;
-        uint64_t left = __ballot(entry >= 0 && entry < a.num_pages);
-        auto next = [&](int* page) {
-            if (left == 0) return -1;
-            const int i = __builtin_ctzll(left);
-            left &= left - 1;
-            *page = chunk + i;
-            return __builtin_amdgcn_readlane(entry, i);
-        };
-        ManyRegs<D> ga, gb;
-        int pa = 0, pb = 0, na = next(&pa), nb = next(&pb);
-        if (na >= 0) {
-            load_keys(ga, page_at(na));
-            load_values(ga, page_at(na));
+    int chunk = page0 - 64, entry = -1;
+    uint64_t left = 0;
+    auto next = [&](int* page) {                         // the next page that is one, or -1
+        while (left == 0) {
+            if (chunk + 64 >= page1) return -1;
+            chunk += 64;
+            entry = chunk + lane < page1 ? row[chunk + lane] : -1;
+            left = __ballot(entry >= 0 && entry < a.num_pages);
         }
-        if (nb >= 0) {
-            load_keys(gb, page_at(nb));
-            load_values(gb, page_at(nb));
+        const int i = __builtin_ctzll(left);
+        left &= left - 1;
+        *page = chunk + i;
+        return __builtin_amdgcn_readlane(entry, i);
+    };
+
+    // Halves of a page (32 tokens) in turn, x the first's scores and y the second's.  While one half's scores become weights the other's
+    // are made, the next page's values are unpacked while this one's are added up: the vector unit works in the shadow of the
+    // matrix instructions.
+    Keys<D> k0, k1;
+    Values<D> v;
+    v16f x, y;
+    v4i pw[2];
+    int page = 0, following = 0, number = next(&page);
+    if (number >= 0) {
+        const uint8_t* p = page_at(number);
+        load_keys(0, k0, p);
+        load_keys(1, k1, p);
+        load_values(v, p);
+        scores(IC<0>{}, k0, x);
+        unpack(v, page, lds[0]);
+        number = next(&following);
+        p = number >= 0 ? page_at(number) : p;           // (none: the same again, unused)
+        load_keys(0, k0, p);
+        load_values(v, p);
+        mask(x, page * kKv4Page);
+        settle(largest(x));
+        int b = 0;
+        for (;; b ^= 1) {
+            scores(IC<1>{}, k1, y);
+            weights(x, pw);
+            BRQ_SCHED1
+            load_keys(1, k1, p);
+            lds_wait_and_barrier();
+            mask(y, page * kKv4Page + 32);
+            const float top = largest(y);
+            add(0, pw, lds[b]);
+            settle(top);
+            if (number < 0) break;
+            page = following;
+            number = next(&following);
+            p = number >= 0 ? page_at(number) : p;
+            scores(IC<0>{}, k0, x);
+            weights(y, pw);
+            BRQ_SCHED1
+            load_keys(0, k0, p);
+            add(1, pw, lds[b]);
+            unpack(v, page, lds[b ^ 1]);
+            BRQ_SCHED2
+            load_values(v, p);
+            mask(x, page * kKv4Page);
+            settle(largest(x));
         }
-        auto step = [&](ManyRegs<D>& g, int& page, int& number, uint8_t* buf) {       // the page in g; then g takes the one after the next
-            unpack(g, page, buf);
-            int after = 0;
-            number = next(&after);
-            const uint8_t* p = number >= 0 ? page_at(number) : nullptr;
-            if (p) load_values(g, p);
-            use(g, page, buf, p);
-            page = after;
-        };
-        while (na >= 0) {
-            step(ga, pa, na, lds[0]);
-            if (nb < 0) break;
-            step(gb, pb, nb, lds[1]);
-        }
-        lds_wait_and_barrier();                      // the next 64 begin with the first buffer
+        weights(y, pw);
+        add(1, pw, lds[b]);
     }
 
     l += __shfl_xor(l, 32);
