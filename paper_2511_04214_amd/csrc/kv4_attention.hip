@@ -8,24 +8,21 @@
 // The products are made transposed, S^T = K Q^T and O^T = V^T P^T: a lane then holds one query row's scores for the very
 // tokens that it has to supply to the second product, and one row's output, so that weights go from the first product's
 // accumulators to the second's operand without leaving the lane and a row's rescaling is one factor a lane.
+#include <algorithm>
+
 #include "brq_attn.h"
 #include "brq_device.h"
 #include "brq_launch.h"
 #include "mfma_fp4.h"
 
-#ifndef BRQ_SCHED
-#define BRQ_SCHED 0
+#ifndef BRQ_AHEAD
+#define BRQ_AHEAD 4
 #endif
-#if BRQ_SCHED == 0
-#define BRQ_SCHED1
-#define BRQ_SCHED2
-#else
-template <int N, int V>
-__device__ __forceinline__ void sched1() { if constexpr (N > 0) { __builtin_amdgcn_sched_group_barrier(0x2, V, 0); __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); sched1<N - 1, V>(); } }
-template <int N, int V>
-__device__ __forceinline__ void sched2() { if constexpr (N > 0) { __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, V, 0); __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); sched2<N - 1, V>(); } }
-#define BRQ_SCHED1 sched1<D / 16, BRQ_SCHED>();
-#define BRQ_SCHED2 sched2<2 * MT, 5>();
+#ifndef BRQ_WGS
+#define BRQ_WGS 2
+#endif
+#ifndef BRQ_TWO
+#define BRQ_TWO 1
 #endif
 #ifndef BRQ_OCC
 #define BRQ_OCC 2
@@ -332,26 +329,26 @@ __global__ __launch_bounds__(256, BRQ_OCC) void k_attention_few(const AttnArgs a
 
 // ---- many query rows: prompts and chunks
 
-// Keys of 32 tokens as a wavefront takes them: token lane % 32, channels 64 s + 32 (lane / 32) ...; and a thread's share of a page's
-// values, 4 tokens of a column.
+// A thread's share of a page, on its way to LDS: D/4 channels of a token's keys, 4 tokens of a column of values.
 template <int D>
-struct Keys {
-    uint32_t k[D / 64][4], s[D / 64];
-};
-template <int D>
-struct Values {
-    uint32_t v[D / 32], s;
+struct Share {
+    uint32_t w[D / 32], s;
 };
 
-// Workgroup: 128 rows (query tokens x heads of a group) of a sequence and cache head, 32 to a wavefront, against the pages of a
-// split.  The keys go from memory to the wavefronts' registers as operands; the values are unpacked by the four wavefronts
-// together, a quarter each, into LDS: [channel][64 tokens] bf16, in the order in which a lane of the second product takes them:
-// quads of tokens 4 s + h and 4 s + 2 + h of its half h side by side.  Channel D/16 c + j is row 16 j + c, so that 16 columns'
-// writes fall on neighbouring rows, and a lane ends up with whole columns of the output.  Two buffers, one barrier a page.
-template <int D>
-__global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int tiles, int splits, float* part_o, float* part_ml) {
-    constexpr int MT = D / 32, KS = D / 64, HB = kv4_head_bytes(D), ROW = 64 * 2 + 16;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][D * ROW];
+// Workgroup: 128 rows (query tokens x heads of a group) of a sequence and cache head for each group of four wavefronts, 32 to a
+// wavefront, against the pages of a split.  Keys and values are unpacked to bf16 once a workgroup and lie in LDS in the order in
+// which a lane takes them: keys by token; values by channel, quads of tokens 4 s + h and 4 s + 2 + h of a lane's half h side by side
+// and channel D/16 c + j in row 16 j + c, so that 16 columns' writes fall on neighbouring rows and a lane ends up with whole
+// columns of the output.
+// A wavefront's matrix instructions hold up its own vector instructions (27 cycles each, measured) but not another wavefront's.  So
+// the two never mix: a page is a matrix phase (the last page's weights times its values, this page's scores) and a vector phase (scores to
+// weights, unpacking), and of two groups in a workgroup one is in the one while the other is in the other, a barrier between
+// phases.  With the phases of a wavefront interleaved instruction by instruction instead, and two independent workgroups on a CU,
+// the 8192-token prompt took 535 us.
+template <int D, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnArgs a, int tiles, int splits, float* part_o, float* part_ml) {
+    constexpr int MT = D / 32, KS = D / 64, HB = kv4_head_bytes(D), ROW = 64 * 2 + 16, KROW = D * 2 + 16, TILE = 128 * GROUPS;
+    __shared__ __attribute__((aligned(16))) uint8_t lds_v[2][D * ROW], lds_k[2][64 * KROW];
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
     // neighbouring workgroups take different heads (each XCD its own), the longest rows of a causal prompt first
     int id = (int)blockIdx.x;
@@ -363,7 +360,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
     int64_t q0;
     int nq;
     query_rows(a, s, &q0, &nq);
-    const int rows = nq * a.G, r0 = tile * 128;
+    const int rows = nq * a.G, r0 = tile * TILE;
     if (r0 >= rows) return;
     const int len = a.kv_lens[s], all = min(len, min(a.max_kv, a.table_cols * kKv4Page));
     const int first = len - (a.cu_q ? (int)(a.cu_q[s + 1] - a.cu_q[s]) : 1);          // position of the sequence's first row
@@ -371,7 +368,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
     // tokens that a row of the workgroup sees; that every row of the wavefront sees; that this lane's row sees
     int begin = 0, end = all, begin_wg = 0, end_wg = all, begin_all = 0, end_all = all;
     if (a.causal) {
-        const int wa = min(r0 + w * 32, rows - 1) / a.G, wb = min(r0 + w * 32 + 31, rows - 1) / a.G, ga = r0 / a.G, gb = min(r0 + 127, rows - 1) / a.G;
+        const int wa = min(r0 + w * 32, rows - 1) / a.G, wb = min(r0 + w * 32 + 31, rows - 1) / a.G, ga = r0 / a.G, gb = min(r0 + TILE - 1, rows - 1) / a.G;
         end = min(all, first + tok + 1);
         end_all = min(all, first + wa + 1);
         end_wg = min(all, first + gb + 1);
@@ -405,72 +402,71 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
         for (int i = 0; i < 16; ++i) o[j][i] = 0.0f;
     float l = 0.0f, ref = 0.0f, top_ref = -INFINITY;
 
-    const int vq = (int)threadIdx.x >> 4, vc = (int)threadIdx.x & 15;                 // this thread's quad of tokens and column of the values
+    const int group = w >> 2, thread = (int)threadIdx.x & 255;
+    const int vq = thread >> 4, vc = thread & 15;                                     // this thread's quad of tokens and column of the values
     const int vpos = ((vq & ~3) | ((vq & 1) << 1) | ((vq >> 1) & 1)) * 8;             // where the quad lies in a row of LDS
     auto page_at = [&](int number) { return uniform_ptr(a.pool + ((int64_t)number * a.Hk + kvh) * HB); };
-    auto load_keys = [&](int half, Keys<D>& g, const uint8_t* p) {
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            load_words<4>(g.k[k], p + half * 16 * D + k * 32, (uint32_t)(n * (D / 2) + h * 16));
-            g.s[k] = load<uint32_t>(p + 32 * D + k * 128, (uint32_t)((h * 16 + (n & 15)) * 4));
-        }
+    const int kt = thread >> 2, kb = thread & 3;                  // its token of the keys, and which quarter of the channels
+    auto load_keys = [&](Share<D>& g, const uint8_t* p) {
+        load_words<D / 32>(g.w, p, (uint32_t)(thread * (D / 8)));
+        g.s = load<uint8_t>(p + 32 * D, (uint32_t)((kb * D / 128 * 16 + (kt & 15)) * 4 + (kt >> 4)));
     };
-    auto load_values = [&](Values<D>& g, const uint8_t* p) {
-        load_words<D / 32>(g.v, p + 34 * D, threadIdx.x * (D / 8));
+    auto load_values = [&](Share<D>& g, const uint8_t* p) {
+        load_words<D / 32>(g.w, p + 34 * D, (uint32_t)(thread * (D / 8)));
         g.s = load<uint32_t>(p + 66 * D, (uint32_t)(((vq & 3) * (D / 32) + vc * D / 512) * 16 + (vq >> 2) * 4));
     };
-    auto unpack = [&](const Values<D>& g, int page, uint8_t* buf) {
-        const int left = all - (page * kKv4Page + vq * 4);                            // tokens that are none: 0 times whatever they hold is to be 0
-        const uint32_t sb = g.s & (uint32_t)((1ull << (8 * min(max(left, 0), 4))) - 1);
-        const uint32_t sc[4] = {scale_of<0>(sb), scale_of<1>(sb), scale_of<2>(sb), scale_of<3>(sb)};
-        static_for([&](auto ib) {
-            constexpr int b = decltype(ib)::value;
-            uint32_t y[4];
+    // Unpacking in pieces of about four vector instructions, D/32 of keys and D/16 of values.
+    auto unpack_keys = [&](auto piece, const Share<D>& g, uint8_t* buf) {
+        constexpr int i = decltype(piece)::value;
+        *reinterpret_cast<bf16x8*>(buf + kt * KROW + kb * (D / 2) + i * 16) = eight_values(g.w[i], g.s << 23);
+    };
+    uint32_t two[4];                                     // two channels of the quad's four tokens, between two pieces
+    auto unpack_values = [&](auto piece, const Share<D>& g, uint8_t* buf) {
+        constexpr int b = decltype(piece)::value / 2;
+        if constexpr (decltype(piece)::value % 2 == 0) {
             if constexpr (D == 128) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = two_values<b>(g.v[i], sc[i]);
+                two[0] = two_values<b>(g.w[0], scale_of<0>(g.s));
+                two[1] = two_values<b>(g.w[1], scale_of<1>(g.s));
+                two[2] = two_values<b>(g.w[2], scale_of<2>(g.s));
+                two[3] = two_values<b>(g.w[3], scale_of<3>(g.s));
             } else {
-                y[0] = two_values<b>(g.v[0], sc[0]);
-                y[1] = two_values<b + 2>(g.v[0], sc[1]);
-                y[2] = two_values<b>(g.v[1], sc[2]);
-                y[3] = two_values<b + 2>(g.v[1], sc[3]);
+                two[0] = two_values<b>(g.w[0], scale_of<0>(g.s));
+                two[1] = two_values<b + 2>(g.w[0], scale_of<1>(g.s));
+                two[2] = two_values<b>(g.w[1], scale_of<2>(g.s));
+                two[3] = two_values<b + 2>(g.w[1], scale_of<3>(g.s));
             }
-            const v2i even = {(int)__builtin_amdgcn_perm(y[1], y[0], 0x05040100u), (int)__builtin_amdgcn_perm(y[3], y[2], 0x05040100u)};
-            const v2i odd = {(int)__builtin_amdgcn_perm(y[1], y[0], 0x07060302u), (int)__builtin_amdgcn_perm(y[3], y[2], 0x07060302u)};
-            *reinterpret_cast<v2i*>(buf + ((2 * b) * 16 + vc) * ROW + vpos) = even;
-            *reinterpret_cast<v2i*>(buf + ((2 * b + 1) * 16 + vc) * ROW + vpos) = odd;
-        }, IC<D / 32>{});
-    };
-    // of tokens 32 half ... 32 half + 31 of a page
-    auto scores = [&](auto half, const Keys<D>& g, v16f& x) {
-        v16f y = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            const uint32_t sc = scale_of<2 * decltype(half)::value>(g.s[k] >> (n & 16 ? 8 : 0));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_values(g.k[k][j], sc), q[k][j], y, 0, 0, 0);
+        } else {
+            *reinterpret_cast<v2i*>(buf + ((2 * b) * 16 + vc) * ROW + vpos) =
+                v2i{(int)__builtin_amdgcn_perm(two[1], two[0], 0x05040100u), (int)__builtin_amdgcn_perm(two[3], two[2], 0x05040100u)};
+            *reinterpret_cast<v2i*>(buf + ((2 * b + 1) * 16 + vc) * ROW + vpos) =
+                v2i{(int)__builtin_amdgcn_perm(two[1], two[0], 0x07060302u), (int)__builtin_amdgcn_perm(two[3], two[2], 0x07060302u)};
         }
-        x = y;
     };
-    // what is not seen
-    auto mask = [&](v16f& x, int t0) {
-        if (t0 < begin_all || t0 + 32 > end_all) {
+    // scales of tokens that are none: 0 times whatever they hold is to be 0
+    auto real_scales = [&](Share<D>& g, int page) {
+        const int left = all - (page * kKv4Page + vq * 4);
+        g.s &= (uint32_t)((1ull << (8 * min(max(left, 0), 4))) - 1);
+    };
+    // what is not seen, then a new reference where a score is 2^8 above the old one
+    auto settle = [&](v16f (&x)[2], int page) {
+        const int t0 = page * kKv4Page;
+        if (t0 < begin_all || t0 + kKv4Page > end_all) {
             asm volatile("");                            // (a branch: few pages need it, and without one all would pay for it)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int t = t0 + 8 * (e >> 2) + 4 * h + (e & 3);
-                x[e] = t >= begin && t < end ? x[e] : -INFINITY;
-            }
-        }
-    };
-    auto largest = [&](const v16f& x) {
-        float top = x[0];
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 1; e < 15; e += 2) top = fmaxf(fmaxf(top, x[e]), x[e + 1]);
-        return fmaxf(top, x[15]) * c;
-    };
-    // a new reference where a score is 2^8 above the old one
-    auto settle = [&](float top) {
+                for (int e = 0; e < 16; ++e) {
+                    const int t = t0 + i * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
+                    x[i][e] = t >= begin && t < end ? x[i][e] : -INFINITY;
+                }
+        }
+        float t0x = x[0][0], t1x = x[1][0];
+#pragma unroll
+        for (int e = 1; e < 15; e += 2) {
+            t0x = fmaxf(fmaxf(t0x, x[0][e]), x[0][e + 1]);
+            t1x = fmaxf(fmaxf(t1x, x[1][e]), x[1][e + 1]);
+        }
+        float top = fmaxf(fmaxf(t0x, x[0][15]), fmaxf(t1x, x[1][15])) * c;
         if (__any(top > top_ref + 8.0f)) {
             top = fmaxf(top, __shfl_xor(top, 32));
             const float now = fmaxf(top, top_ref), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top_ref - now);
@@ -481,28 +477,22 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
             for (int j = 0; j < MT; ++j) o[j] *= f;
         }
     };
-    auto weights = [&](const v16f& x, v4i (&pw)[2]) {
+    auto weights = [&](const v16f (&x)[2], v4i (&pw)[4]) {
+        float l1 = 0.0f;
 #pragma unroll
-        for (int st = 0; st < 2; ++st)
+        for (int st = 0; st < 4; ++st)
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st * 8 + e], c, -ref));
-                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st * 8 + e + 1], c, -ref));
-                l += e0 + e1;
+                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st >> 1][(st & 1) * 8 + e], c, -ref));
+                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[st >> 1][(st & 1) * 8 + e + 1], c, -ref));
+                l += e0;
+                l1 += e1;
                 pw[st][e >> 1] = (int)pack_bf16x2(e0, e1);
             }
-        asm volatile("" : "+v"(l));                      // (the compiler would add them up where l is next used, and keep them all until then)
+        l += l1;
+        // (the compiler would add up and pack where the results are next used, and keep all weights in 32 bits until then)
+        asm volatile("" : "+v"(l), "+v"(pw[0]), "+v"(pw[1]), "+v"(pw[2]), "+v"(pw[3]));
     };
-    auto add = [&](int half, const v4i (&pw)[2], const uint8_t* buf) {
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-            for (int j = 0; j < MT; ++j) {
-                const v4i vv = *reinterpret_cast<const v4i*>(buf + (j * 32 + n) * ROW + (half * 2 + st) * 32 + h * 16);
-                o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vv), __builtin_bit_cast(bf16x8, pw[st]), o[j], 0, 0, 0);
-            }
-    };
-
     // pages in order, 64 numbers at a time, one a lane
     const int32_t* row = a.table + (int64_t)s * a.table_cols;
     int chunk = page0 - 64, entry = -1;
@@ -520,56 +510,91 @@ __global__ __launch_bounds__(256, 2) void k_attention_many(const AttnArgs a, int
         return __builtin_amdgcn_readlane(entry, i);
     };
 
-    // Halves of a page (32 tokens) in turn, x the first's scores and y the second's.  While one half's scores become weights the other's
-    // are made, the next page's values are unpacked while this one's are added up: the vector unit works in the shadow of the
-    // matrix instructions.
-    Keys<D> k0, k1;
-    Values<D> v;
-    v16f x, y;
-    v4i pw[2];
-    int page = 0, following = 0, number = next(&page);
-    if (number >= 0) {
-        const uint8_t* p = page_at(number);
-        load_keys(0, k0, p);
-        load_keys(1, k1, p);
-        load_values(v, p);
-        scores(IC<0>{}, k0, x);
-        unpack(v, page, lds[0]);
-        number = next(&following);
-        p = number >= 0 ? page_at(number) : p;           // (none: the same again, unused)
-        load_keys(0, k0, p);
-        load_values(v, p);
-        mask(x, page * kKv4Page);
-        settle(largest(x));
-        int b = 0;
-        for (;; b ^= 1) {
-            scores(IC<1>{}, k1, y);
-            weights(x, pw);
-            BRQ_SCHED1
-            load_keys(1, k1, p);
-            lds_wait_and_barrier();
-            mask(y, page * kKv4Page + 32);
-            const float top = largest(y);
-            add(0, pw, lds[b]);
-            settle(top);
-            if (number < 0) break;
-            page = following;
-            number = next(&following);
-            p = number >= 0 ? page_at(number) : p;
-            scores(IC<0>{}, k0, x);
-            weights(y, pw);
-            BRQ_SCHED1
-            load_keys(0, k0, p);
-            add(1, pw, lds[b]);
-            unpack(v, page, lds[b ^ 1]);
-            BRQ_SCHED2
-            load_values(v, p);
-            mask(x, page * kKv4Page);
-            settle(largest(x));
+    // Phases, with pages 0, 1, ... as they come (M: matrix, V: vector):
+    //     group 0          M0    V0    M1    V1    ...       unpacks the keys of page i + 1 in M_i
+    //     group 1          .     M0    V0    M1    V1 ...    unpacks the values of page i + 1 in V_i, of page 0 in its first phase
+    // with a barrier between any two.  (One group alone: the keys of i + 1 in M_i, the values of i in V_i, a barrier behind V_i.)  M_i reads the
+    // keys of page i and the values of page i - 1.  The keys of i + 1 replace those of i - 1, and the values of i + 1 those of i - 1 (one group:
+    // of i those of i - 2): both read last in M_{i-1} and M_i of group 1, a barrier before.
+    auto run = [&](auto role) {                          // 0: unpacks keys, 1: values, 2: both
+        constexpr bool KEYS = decltype(role)::value != 1, VALUES = decltype(role)::value != 0;
+        Share<D> sk, sv;
+        v16f x[2];
+        v4i pw[4];
+        int page = 0, next1 = 0, next2 = 0, n0 = next(&page);                             // numbers of this page and the next two, -1: none
+        if (n0 < 0) return;
+        int n1 = next(&next1), n2 = next(&next2);
+        auto there = [&](int number) { return page_at(number >= 0 ? number : n0); };     // (none: any page, unused)
+        if constexpr (VALUES) load_values(sv, page_at(n0));
+        if constexpr (KEYS) {
+            load_keys(sk, page_at(n0));
+            static_for([&](auto piece) { unpack_keys(piece, sk, lds_k[0]); }, IC<D / 32>{});
+            load_keys(sk, there(n1));
         }
-        weights(y, pw);
-        add(1, pw, lds[b]);
-    }
+        lds_wait_and_barrier();
+        auto values_of = [&](int which, uint8_t* buf, int following) {                   // page `which`; then the load of number `following`
+            real_scales(sv, which);
+            static_for([&](auto piece) { unpack_values(piece, sv, buf); }, IC<D / 16>{});
+            load_values(sv, there(following));
+        };
+        if constexpr (GROUPS == 2 && VALUES) {
+            values_of(page, lds_v[0], n1);
+            lds_wait_and_barrier();                      // one phase behind
+        }
+        int b = 0;                                       // of this page's keys
+        // A matrix phase, step by step as it is written: a product, the operand of the one kAhead steps on, a piece of unpacking.
+        // (Left to itself the compiler reads an operand, waits and multiplies.)
+        auto matrix = [&](auto from) {                   // from: 0, or NV without the values of a page in front
+            constexpr int NV = 4 * MT, NK = 8 * KS, FROM = decltype(from)::value, kAhead = BRQ_AHEAD;
+            const uint8_t *bv = lds_v[b ^ 1], *bk = lds_k[b];
+            auto operand = [&](int m) {
+                return m < NV ? *reinterpret_cast<const v4i*>(bv + (m % MT * 32 + n) * ROW + m / MT * 32 + h * 16)
+                              : *reinterpret_cast<const v4i*>(bk + ((m - NV) / (4 * KS) * 32 + n) * KROW + (m - NV) % (4 * KS) / 4 * 128 + h * 64 + (m - NV) % 4 * 16);
+            };
+            v4i f[kAhead];
+#pragma unroll
+            for (int m = 0; m < kAhead; ++m) f[(FROM + m) % kAhead] = operand(FROM + m);
+            __builtin_amdgcn_sched_barrier(0);
+            static_for([&](auto im) {
+                constexpr int m = FROM + decltype(im)::value;
+                const bf16x8 a8 = __builtin_bit_cast(bf16x8, f[m % kAhead]);
+                if constexpr (m < NV) {
+                    o[m % MT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a8, __builtin_bit_cast(bf16x8, pw[m / MT]), o[m % MT], 0, 0, 0);
+                } else {
+                    constexpr int i = (m - NV) / (4 * KS), k = (m - NV) % (4 * KS);
+                    const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+                    x[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a8, q[k / 4][k % 4], k == 0 ? zero : x[i], 0, 0, 0);
+                }
+                if constexpr (m + kAhead < NV + NK) f[m % kAhead] = operand(m + kAhead);
+                constexpr int step = m - FROM - 1;       // two steps to a piece, from the second on
+                if constexpr (KEYS && step >= 0 && step % 2 == 0 && step / 2 < D / 32) unpack_keys(IC<step / 2>{}, sk, lds_k[b ^ 1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }, IC<NV + NK - FROM>{});
+            if constexpr (KEYS) load_keys(sk, there(n2));
+        };
+        matrix(IC<4 * MT>{});
+        if constexpr (GROUPS == 2) lds_wait_and_barrier();
+        for (;;) {
+            settle(x, page);
+            weights(x, pw);
+            if constexpr (GROUPS == 1) values_of(page, lds_v[b], n1);
+            else if constexpr (VALUES) values_of(next1, lds_v[b ^ 1], n2);
+            lds_wait_and_barrier();
+            const bool more = n1 >= 0;
+            page = next1;
+            next1 = next2;
+            n1 = n2;
+            n2 = next(&next2);
+            b ^= 1;
+            matrix(IC<0>{});                             // (behind the last page the scores are of whatever is there, unused)
+            if (!more) break;
+            if constexpr (GROUPS == 2) lds_wait_and_barrier();
+        }
+        if constexpr (GROUPS == 2 && KEYS) lds_wait_and_barrier();
+    };
+    if constexpr (GROUPS == 1) run(IC<2>{});
+    else if (group == 0) run(IC<0>{});
+    else run(IC<1>{});
 
     l += __shfl_xor(l, 32);
     if (r >= rows) return;
@@ -656,39 +681,42 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 }
 
 // How a call is cut up.  Up to 16 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
-// pages; more: tiles of 128 rows.  The pages are split where that alone leaves CUs idle: two workgroups a CU, none with less than
-// two pages a wavefront, or eight of a tile.
-#ifndef BRQ_WGS
-#define BRQ_WGS 2
-#endif
+// pages.  More: tiles of 256 rows where there is one for every CU, else of 128.  The pages are split where that alone leaves CUs
+// idle: two workgroups a CU, none with less than two pages a wavefront, or eight of a tile.
 struct Plan {
     bool few;
+    int groups;                  // of 128 rows in a tile
     int64_t tiles;
     int splits;
-    static Plan of(int64_t S, int Hk, int G, int64_t max_q, int64_t max_kv, int cus) {
+    static Plan of(int64_t T, int64_t S, int Hk, int G, int64_t max_q, int64_t max_kv, int cus) {
         const bool few = max_q * G <= 16;
-        const int64_t tiles = few ? 1 : (max_q * G + 127) / 128, pages = (max_kv + kKv4Page - 1) / kKv4Page, groups = S * Hk * tiles;
-        int64_t n = (BRQ_WGS * cus + groups - 1) / groups;
-        n = n < (pages + 7) / 8 ? n : (pages + 7) / 8;
-        return {few, tiles, (int)(n < 1 ? 1 : n > 256 ? 256 : n)};
+        const int64_t pages = (max_kv + kKv4Page - 1) / kKv4Page;
+        // tiles that a call of T rows can have, whatever the longest sequence's
+        auto most = [&](int64_t rows) { return std::min(S * ((max_q * G + rows - 1) / rows), T * G / rows + S); };
+        const int groups = !few && Hk * most(256) >= BRQ_TWO * cus ? 2 : 1;
+        const int64_t tiles = few ? 1 : (max_q * G + 128 * groups - 1) / (128 * groups), wgs = Hk * (few ? S : most(128 * groups));
+        int64_t n = (BRQ_WGS * cus + wgs - 1) / wgs;
+        n = std::min(n, (pages + 7) / 8);
+        return {few, groups, tiles, groups == 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
     }
 };
 
 }  // namespace
 
 int64_t kv4_attention_workspace(int64_t T, int64_t S, int Hq, int Hk, int D, int64_t max_q, int64_t max_kv, int cus) {
-    const Plan p = Plan::of(S, Hk, Hq / Hk, max_q, max_kv, cus);
+    const Plan p = Plan::of(T, S, Hk, Hq / Hk, max_q, max_kv, cus);
     return p.splits == 1 ? 0 : T * Hq * p.splits * (D + 2) * 4;
 }
 
 template <int D>
 static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t stream) {
     const int Hq = a.Hk * a.G;
-    const Plan p = Plan::of(a.S, a.Hk, a.G, a.max_q, a.max_kv, cus);
+    const Plan p = Plan::of(a.T, a.S, a.Hk, a.G, a.max_q, a.max_kv, cus);
     float *po = p.splits == 1 ? nullptr : static_cast<float*>(a.workspace), *pm = po ? po + a.T * Hq * p.splits * D : nullptr;
     const dim3 grid((uint32_t)(a.S * a.Hk * p.tiles * p.splits));
     if (p.few) hipLaunchKernelGGL((k_attention_few<D>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
-    else hipLaunchKernelGGL((k_attention_many<D>), grid, dim3(256), 0, stream, a, (int)p.tiles, p.splits, po, pm);
+    else if (p.groups == 2) hipLaunchKernelGGL((k_attention_many<D, 2>), grid, dim3(512), 0, stream, a, (int)p.tiles, p.splits, po, pm);
+    else hipLaunchKernelGGL((k_attention_many<D, 1>), grid, dim3(256), 0, stream, a, (int)p.tiles, p.splits, po, pm);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;
     const int64_t rows = (int64_t)a.S * a.max_q * Hq;
     if (p.splits <= 8) hipLaunchKernelGGL((k_attention_join<D, 1>), dim3((uint32_t)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, stream, a, p.splits, po, pm);
