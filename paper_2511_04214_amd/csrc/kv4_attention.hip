@@ -14,19 +14,6 @@
 #include "brq_device.h"
 #include "brq_launch.h"
 #include "mfma_fp4.h"
-
-#ifndef BRQ_AHEAD
-#define BRQ_AHEAD 4
-#endif
-#ifndef BRQ_WGS
-#define BRQ_WGS 2
-#endif
-#ifndef BRQ_TWO
-#define BRQ_TWO 1
-#endif
-#ifndef BRQ_OCC
-#define BRQ_OCC 2
-#endif
 namespace brq {
 namespace {
 
@@ -107,8 +94,10 @@ struct PageRegs {
 };
 
 // Workgroup: sequence, cache head, split.  Wavefront w goes through pages first + w, first + w + 4, ...
+// (Registers for two workgroups a CU, so that a page can be on its way while one is worked on: for three, the batch of 100 below took
+// 132 us, not 128.)
 template <int D>
-__global__ __launch_bounds__(256, BRQ_OCC) void k_attention_few(const AttnArgs a, int splits, float* part_o, float* part_ml) {
+__global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int splits, float* part_o, float* part_ml) {
     constexpr int MT = D / 16, HB = kv4_head_bytes(D);
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int split = (int)blockIdx.x % splits, sh = (int)blockIdx.x / splits, s = sh / a.Hk, kvh = sh - s * a.Hk;
@@ -344,11 +333,13 @@ struct Share {
 // the two never mix: a page is a matrix phase (the last page's weights times its values, this page's scores) and a vector phase (scores to
 // weights, unpacking), and of two groups in a workgroup one is in the one while the other is in the other, a barrier between
 // phases.  With the phases of a wavefront interleaved instruction by instruction instead, and two independent workgroups on a CU,
-// the 8192-token prompt took 535 us.
+// a prompt of 8192 tokens took 535 us, so 482 us.
 template <int D, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnArgs a, int tiles, int splits, float* part_o, float* part_ml) {
     constexpr int MT = D / 32, KS = D / 64, HB = kv4_head_bytes(D), ROW = 64 * 2 + 16, KROW = D * 2 + 16, TILE = 128 * GROUPS;
-    __shared__ __attribute__((aligned(16))) uint8_t lds_v[2][D * ROW], lds_k[2][64 * KROW];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * D * ROW + 2 * 64 * KROW];
+    const auto lds_v = [&](int i) { return lds + i * (D * ROW); };
+    const auto lds_k = [&](int i) { return lds + 2 * D * ROW + i * (64 * KROW); };
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
     // neighbouring workgroups take different heads (each XCD its own), the longest rows of a causal prompt first
     int id = (int)blockIdx.x;
@@ -528,7 +519,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
         if constexpr (VALUES) load_values(sv, page_at(n0));
         if constexpr (KEYS) {
             load_keys(sk, page_at(n0));
-            static_for([&](auto piece) { unpack_keys(piece, sk, lds_k[0]); }, IC<D / 32>{});
+            static_for([&](auto piece) { unpack_keys(piece, sk, lds_k(0)); }, IC<D / 32>{});
             load_keys(sk, there(n1));
         }
         lds_wait_and_barrier();
@@ -538,15 +529,15 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
             load_values(sv, there(following));
         };
         if constexpr (GROUPS == 2 && VALUES) {
-            values_of(page, lds_v[0], n1);
+            values_of(page, lds_v(0), n1);
             lds_wait_and_barrier();                      // one phase behind
         }
         int b = 0;                                       // of this page's keys
         // A matrix phase, step by step as it is written: a product, the operand of the one kAhead steps on, a piece of unpacking.
         // (Left to itself the compiler reads an operand, waits and multiplies.)
         auto matrix = [&](auto from) {                   // from: 0, or NV without the values of a page in front
-            constexpr int NV = 4 * MT, NK = 8 * KS, FROM = decltype(from)::value, kAhead = BRQ_AHEAD;
-            const uint8_t *bv = lds_v[b ^ 1], *bk = lds_k[b];
+            constexpr int NV = 4 * MT, NK = 8 * KS, FROM = decltype(from)::value, kAhead = 4;
+            const uint8_t *bv = lds_v(b ^ 1), *bk = lds_k(b);
             auto operand = [&](int m) {
                 return m < NV ? *reinterpret_cast<const v4i*>(bv + (m % MT * 32 + n) * ROW + m / MT * 32 + h * 16)
                               : *reinterpret_cast<const v4i*>(bk + ((m - NV) / (4 * KS) * 32 + n) * KROW + (m - NV) % (4 * KS) / 4 * 128 + h * 64 + (m - NV) % 4 * 16);
@@ -567,7 +558,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
                 }
                 if constexpr (m + kAhead < NV + NK) f[m % kAhead] = operand(m + kAhead);
                 constexpr int step = m - FROM - 1;       // two steps to a piece, from the second on
-                if constexpr (KEYS && step >= 0 && step % 2 == 0 && step / 2 < D / 32) unpack_keys(IC<step / 2>{}, sk, lds_k[b ^ 1]);
+                if constexpr (KEYS && step >= 0 && step % 2 == 0 && step / 2 < D / 32) unpack_keys(IC<step / 2>{}, sk, lds_k(b ^ 1));
                 __builtin_amdgcn_sched_barrier(0);
             }, IC<NV + NK - FROM>{});
             if constexpr (KEYS) load_keys(sk, there(n2));
@@ -577,8 +568,8 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
         for (;;) {
             settle(x, page);
             weights(x, pw);
-            if constexpr (GROUPS == 1) values_of(page, lds_v[b], n1);
-            else if constexpr (VALUES) values_of(next1, lds_v[b ^ 1], n2);
+            if constexpr (GROUPS == 1) values_of(page, lds_v(b), n1);
+            else if constexpr (VALUES) values_of(next1, lds_v(b ^ 1), n2);
             lds_wait_and_barrier();
             const bool more = n1 >= 0;
             page = next1;
@@ -596,35 +587,55 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
     else if (group == 0) run(IC<0>{});
     else run(IC<1>{});
 
+    // The output goes out row by row through the buffers' LDS, 32 rows of a wavefront in a part of its own: a lane has 16 bytes here
+    // and there of one row, and stores of such pieces keep the caches' request queues busy (the partial sums of 6 chunks of up to
+    // 500 tokens x 16 heads: the kernel 25.9 us with them, 24.6 us so).
     l += __shfl_xor(l, 32);
-    if (r >= rows) return;
+    lds_wait_and_barrier();
+    const bool mine = r < rows;
     const int64_t t = q0 + tok, at = t * (a.Hk * a.G) + head;
-    if (part_o) {
-        float* po = part_o + (at * splits + split) * D;
+    auto rows_out = [&](auto bytes, uint64_t address, auto piece) {        // bytes of a channel; address of the lane's row, 0: none
+        constexpr int E = decltype(bytes)::value, PITCH = D * E + 16, LANES = D * E / 16;
+        static_assert(4 * GROUPS * 32 * PITCH <= (int)sizeof(lds), "a part for each wavefront");
+        uint8_t* part = lds + w * (32 * PITCH);
+        piece(part + n * PITCH);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
+        for (int k = 0; k < 32 * LANES / 64; ++k) {
+            const int row = k * (64 / LANES) + lane / LANES;
+            const uint32_t lo = __shfl((uint32_t)address, row), hi = __shfl((uint32_t)(address >> 32), row);
+            const v4i v = *reinterpret_cast<const v4i*>(part + row * PITCH + lane % LANES * 16);
+            if ((lo | hi) != 0) *reinterpret_cast<v4i*>((((uint64_t)hi << 32) | lo) + lane % LANES * 16) = v;
+        }
+    };
+    if (GROUPS == 1 && part_o) {
+        if constexpr (GROUPS == 1) rows_out(IC<4>{}, mine ? reinterpret_cast<uint64_t>(part_o + (at * splits + split) * D) : 0, [&](uint8_t* to) {
 #pragma unroll
-            for (int j = 0; j < D / 16; j += 4) {
-                v4f y;
+            for (int q = 0; q < 8; ++q)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = o[(j + e) >> 1][((j + e) & 1) * 8 + q];
-                *reinterpret_cast<v4f*>(po + ((q >> 2) * 8 + h * 4 + (q & 3)) * (D / 16) + j) = y;
-            }
-        if (h == 0) *reinterpret_cast<f32x2*>(part_ml + (at * splits + split) * 2) = f32x2{top_ref, l};
+                for (int j = 0; j < D / 16; j += 4) {
+                    v4f y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = o[(j + e) >> 1][((j + e) & 1) * 8 + q];
+                    *reinterpret_cast<v4f*>(to + (((q >> 2) * 8 + h * 4 + (q & 3)) * (D / 16) + j) * 4) = y;
+                }
+        });
+        if (mine && h == 0) *reinterpret_cast<f32x2*>(part_ml + (at * splits + split) * 2) = f32x2{top_ref, l};
         return;
     }
     const float k = l > 0.0f ? 1.0f / l : 0.0f;
-    uint8_t* op = a.o.p + t * a.o.ts + head * a.o.hs;
+    rows_out(IC<2>{}, mine ? reinterpret_cast<uint64_t>(a.o.p + t * a.o.ts + head * a.o.hs) : 0, [&](uint8_t* to) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        uint32_t y[D / 32];
+        for (int q = 0; q < 8; ++q) {
+            uint32_t y[D / 32];
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) y[j] = pack_bf16x2(o[j][q] * k, o[j][8 + q] * k);
-        uint8_t* d = op + ((q >> 2) * 8 + h * 4 + (q & 3)) * (D / 8);
-        if constexpr (D == 128) *reinterpret_cast<v4i*>(d) = v4i{(int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-        else *reinterpret_cast<v2i*>(d) = v2i{(int)y[0], (int)y[1]};
-    }
-    if (a.lse && h == 0) a.lse[at] = l > 0.0f ? (top_ref + __log2f(l)) * kLn2 : -INFINITY;
+            for (int j = 0; j < D / 32; ++j) y[j] = pack_bf16x2(o[j][q] * k, o[j][8 + q] * k);
+            uint8_t* d = to + ((q >> 2) * 8 + h * 4 + (q & 3)) * (D / 8);
+            if constexpr (D == 128) *reinterpret_cast<v4i*>(d) = v4i{(int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+            else *reinterpret_cast<v2i*>(d) = v2i{(int)y[0], (int)y[1]};
+        }
+    });
+    if (a.lse && mine && h == 0) a.lse[at] = l > 0.0f ? (top_ref + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 // Joins the splits of rows and heads, 256/(GROUPS D/4) to a workgroup: GROUPS groups of D/4 threads a row take every so many splits,
@@ -681,8 +692,11 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 }
 
 // How a call is cut up.  Up to 16 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
-// pages.  More: tiles of 256 rows where there is one for every CU, else of 128.  The pages are split where that alone leaves CUs
-// idle: two workgroups a CU, none with less than two pages a wavefront, or eight of a tile.
+// pages.  More: tiles of 256 rows where there is one for every CU, else of 128 (8192 tokens x 32 heads: 482 us, 529 us with tiles
+// of 128).  The pages are split, none to less than eight pages, where the tiles alone leave CUs idle: to two workgroups a CU (one row of
+// 131 072 tokens: 34 us, to four a CU 38 to 45 us for the joining; 6 chunks of up to 500 tokens over up to 4000: 28 us, to four 30 us).
+// Few rows of several sequences: to four a CU, because the sequences' lengths differ and shorter parts even out (100 of up to 8192
+// tokens: 121 us, 125 us with two).
 struct Plan {
     bool few;
     int groups;                  // of 128 rows in a tile
@@ -693,9 +707,9 @@ struct Plan {
         const int64_t pages = (max_kv + kKv4Page - 1) / kKv4Page;
         // tiles that a call of T rows can have, whatever the longest sequence's
         auto most = [&](int64_t rows) { return std::min(S * ((max_q * G + rows - 1) / rows), T * G / rows + S); };
-        const int groups = !few && Hk * most(256) >= BRQ_TWO * cus ? 2 : 1;
+        const int groups = !few && Hk * most(256) >= cus ? 2 : 1;
         const int64_t tiles = few ? 1 : (max_q * G + 128 * groups - 1) / (128 * groups), wgs = Hk * (few ? S : most(128 * groups));
-        int64_t n = (BRQ_WGS * cus + wgs - 1) / wgs;
+        int64_t n = ((few && S > 1 ? 4 : 2) * cus + wgs - 1) / wgs;
         n = std::min(n, (pages + 7) / 8);
         return {few, groups, tiles, groups == 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
     }
