@@ -538,6 +538,6 @@ def diag_mfma_ceiling(operands, iters, workgroups, sink=None, stream=None):
 
 
 from . import attention as _attention          # noqa: E402  (at the end: it uses what is above)
-from .attention import (kv4_append, kv4_attention, kv4_attention_workspace, kv4_page_bytes, kv4_pages_compact, kv4_pages_copy,  # noqa: E402,F401
-                        kv4_pages_fork, kv4_pages_free, kv4_pages_reserve, kv4_pages_workspace, kv4_read, qk_norm_rope,
+from .attention import (KV4_PAGE, kv4_append, kv4_attention, kv4_attention_workspace, kv4_page_bytes, kv4_pages_compact,  # noqa: E402,F401
+                        kv4_pages_copy, kv4_pages_fork, kv4_pages_free, kv4_pages_reserve, kv4_pages_workspace, kv4_read, qk_norm_rope,
                         qk_norm_rope_backward, qk_norm_rope_backward_workspace)

@@ -301,17 +301,18 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
         float m = -INFINITY, sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = fmaxf(m, sm[i][r]);
+        const float any = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += sm[i][r] == -INFINITY ? 0.0f : sl[i][r] * __builtin_amdgcn_exp2f(sm[i][r] - m);
+        for (int i = 0; i < 4; ++i) sum += sl[i][r] * __builtin_amdgcn_exp2f(sm[i][r] - any);
         const int tk = r / a.G;
         const int64_t t = q0 + tk, hq = kvh * a.G + (r - tk * a.G), at = t * (a.Hk * a.G) + hq;
         if (part_o) {
             *reinterpret_cast<v4f*>(part_o + (at * splits + split) * D + d) = y;
             if (d == 0) *reinterpret_cast<f32x2*>(part_ml + (at * splits + split) * 2) = f32x2{m, sum};
         } else {
-            const float k = sum > 0.0f ? 1.0f / sum : 0.0f;
+            const float k = sum == 0.0f ? 0.0f : 1.0f / sum;
             *reinterpret_cast<v2i*>(a.o.p + t * a.o.ts + hq * a.o.hs + d * 2) = v2i{(int)pack_bf16x2(y.x * k, y.y * k), (int)pack_bf16x2(y.z * k, y.w * k)};
-            if (a.lse && d == 0) a.lse[at] = sum > 0.0f ? (m + __log2f(sum)) * kLn2 : -INFINITY;
+            if (a.lse && d == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (m + __log2f(sum)) * kLn2;
         }
     }
 }
@@ -623,7 +624,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
         if (mine && h == 0) *reinterpret_cast<f32x2*>(part_ml + (at * splits + split) * 2) = f32x2{top_ref, l};
         return;
     }
-    const float k = l > 0.0f ? 1.0f / l : 0.0f;
+    const float k = l == 0.0f ? 0.0f : 1.0f / l;
     rows_out(IC<2>{}, mine ? reinterpret_cast<uint64_t>(a.o.p + t * a.o.ts + head * a.o.hs) : 0, [&](uint8_t* to) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
@@ -635,7 +636,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
             else *reinterpret_cast<v2i*>(d) = v2i{(int)y[0], (int)y[1]};
         }
     });
-    if (a.lse && mine && h == 0) a.lse[at] = l > 0.0f ? (top_ref + __log2f(l)) * kLn2 : -INFINITY;
+    if (a.lse && mine && h == 0) a.lse[at] = l == 0.0f ? -INFINITY : (top_ref + __log2f(l)) * kLn2;
 }
 
 // Joins the splits of rows and heads, 256/(GROUPS D/4) to a workgroup: GROUPS groups of D/4 threads a row take every so many splits,
@@ -686,9 +687,9 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
             sum += sl[mine][k] * f;
         }
     }
-    const float k = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const float k = sum == 0.0f ? 0.0f : 1.0f / sum;
     *reinterpret_cast<v2i*>(a.o.p + t * a.o.ts + h * a.o.hs + d * 2) = v2i{(int)pack_bf16x2(y.x * k, y.y * k), (int)pack_bf16x2(y.z * k, y.w * k)};
-    if (a.lse && d == 0) a.lse[at] = sum > 0.0f ? (m + __log2f(sum)) * kLn2 : -INFINITY;
+    if (a.lse && d == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (m + __log2f(sum)) * kLn2;
 }
 
 // How a call is cut up.  Up to 16 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
