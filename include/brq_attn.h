@@ -107,7 +107,7 @@ brq_status brq_kv4_read(const uint8_t* pool, int64_t num_pages, int64_t T, int64
 
 /*
  * Attention of T query rows of S sequences over the cache.  Sequence s has query rows cu_q[s] ... cu_q[s+1] - 1
- * (cu_q: [S + 1]; NULL: one row each, T = S) and the tokens 0 ... kv_lens[s] - 1, token j in page
+ * (cu_q: [S + 1], ascending, or a sequence may come out unwritten; NULL: one row each, T = S) and the tokens 0 ... kv_lens[s] - 1, token j in page
  * table[s * table_cols + j / 64].  Its queries are the last of them: row i of n stands at position
  * p = kv_lens[s] - n + i.  With Hk heads in the cache, q.heads a multiple of it, query head h reads head
  * h / (q.heads / Hk):

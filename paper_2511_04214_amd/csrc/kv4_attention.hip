@@ -76,6 +76,35 @@ __device__ __forceinline__ void query_rows(const AttnArgs& a, int s, int64_t* q0
     *n = b < 0 || e > a.T || e <= b ? 0 : (int)min(e - b, (int64_t)a.max_q);
 }
 
+// Tile number `id` of `size` rows, counted through the sequences, a sequence's last tile first; false behind the last one.  (A grid
+// of sequences times the longest one's tiles is mostly empty where lengths differ: 6 chunks of 38 to 500 tokens 592 of 1536
+// workgroups, and the empty ones load the offsets like the others.)
+__device__ __forceinline__ bool tile_of(const AttnArgs& a, int id, int size, int* s, int64_t* q0, int* nq, int* tile) {
+    const int lane = (int)threadIdx.x & 63;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+        int64_t b = 0;
+        int n = 0;
+        if (s0 + lane < a.S) query_rows(a, s0 + lane, &b, &n);
+        int upto = (n * a.G + size - 1) / size;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int x = __shfl_up(upto, d);
+            upto += lane >= d ? x : 0;
+        }
+        const uint64_t behind = __ballot(upto > id);
+        if (behind) {
+            const int i = __builtin_ctzll(behind);
+            *s = s0 + i;
+            *q0 = __builtin_amdgcn_readlane((int)b, i);
+            *nq = __builtin_amdgcn_readlane(n, i);
+            *tile = __builtin_amdgcn_readlane(upto, i) - 1 - id;
+            return true;
+        }
+        id -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
 // A value that is the same in every lane, in a scalar register: an instruction with two vector operands issues in 2.8 cycles (two
 // wavefronts a SIMD), one with three in 4.6.
 __device__ __forceinline__ float uniform_f32(float v) { return as_f32(__builtin_amdgcn_readfirstlane(as_u32(v))); }
@@ -325,42 +354,48 @@ struct Share {
     uint32_t w[D / 32], s;
 };
 
-// Workgroup: 128 rows (query tokens x heads of a group) of a sequence and cache head for each group of four wavefronts, 32 to a
-// wavefront, against the pages of a split.  Keys and values are unpacked to bf16 once a workgroup and lie in LDS in the order in
+// Workgroup: a tile of rows (query tokens x heads of a group) of a sequence and cache head, 32 rows to a wavefront, against the pages
+// of a split.  Keys and values are unpacked to bf16 once a workgroup and lie in LDS in the order in
 // which a lane takes them: keys by token; values by channel, quads of tokens 4 s + h and 4 s + 2 + h of a lane's half h side by side
 // and channel D/16 c + j in row 16 j + c, so that 16 columns' writes fall on neighbouring rows and a lane ends up with whole
 // columns of the output.
-// A wavefront's matrix instructions hold up its own vector instructions (27 cycles each, measured) but not another wavefront's.  So
-// the two never mix: a page is a matrix phase (the last page's weights times its values, this page's scores) and a vector phase (scores to
-// weights, unpacking), and of two groups in a workgroup one is in the one while the other is in the other, a barrier between
-// phases.  With the phases of a wavefront interleaved instruction by instruction instead, and two independent workgroups on a CU,
-// a prompt of 8192 tokens took 535 us, so 482 us.
-template <int D, int GROUPS>
-__global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnArgs a, int tiles, int splits, float* part_o, float* part_ml) {
-    constexpr int MT = D / 32, KS = D / 64, HB = kv4_head_bytes(D), ROW = 64 * 2 + 16, KROW = D * 2 + 16, TILE = 128 * GROUPS;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * D * ROW + 2 * 64 * KROW];
-    const auto lds_v = [&](int i) { return lds + i * (D * ROW); };
-    const auto lds_k = [&](int i) { return lds + 2 * D * ROW + i * (64 * KROW); };
-    const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+// kTall: 256 rows, two groups of four wavefronts.  A wavefront's matrix instructions hold up its own vector instructions (27 cycles
+// each, measured) but not another wavefront's.  So the two never mix: a page is a matrix phase (the last page's weights times its
+// values, this page's scores) and a vector phase (scores to weights, unpacking), and of the two groups one is in the one while the
+// other is in the other, a barrier between phases.  With the phases of a wavefront interleaved instruction by instruction instead,
+// and two independent workgroups on a CU, a prompt of 8192 tokens took 535 us, so 482 us.  For calls that fill the card with such tiles.
+// kPair: 128 rows; the two groups take every other page of them, each with buffers of its own, and add their sums up at the end.
+// For calls that do not: a page after another costs a lone group 1.4 us, whatever the rest of the card does, and partial sums
+// through memory cost more than they save there (1024 tokens, 32 heads of 128: 28 us; one group 38 us, tall tiles 41 us).
+// kOne: 128 rows, one group, for contexts of a few pages, where a second one is only more to start (64 tokens: 8.3 us, 11.3 us paired).
+enum { kOne, kPair, kTall };
+template <int D, int MODE>
+__global__ __launch_bounds__(MODE == kOne ? 256 : 512, MODE != kOne && D == 64 ? 4 : 2) void k_attention_many(const AttnArgs a, int splits, float* part_o, float* part_ml) {
+    constexpr int MT = D / 32, KS = D / 64, HB = kv4_head_bytes(D), ROW = 64 * 2 + 16, KROW = D * 2 + 16, TILE = MODE == kTall ? 256 : 128;
+    constexpr bool PAIR = MODE == kPair, TALL = MODE == kTall;
+    constexpr int BUFFERS = 2 * D * ROW + 2 * 64 * KROW;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[BUFFERS * (PAIR ? 2 : 1)];
+    const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 31, h = lane >> 5, group = w >> 2;
+    uint8_t* const own = lds + (PAIR ? group * BUFFERS : 0);
+    const auto lds_v = [&](int i) { return own + i * (D * ROW); };
+    const auto lds_k = [&](int i) { return own + 2 * D * ROW + i * (64 * KROW); };
     // neighbouring workgroups take different heads (each XCD its own), the longest rows of a causal prompt first
     int id = (int)blockIdx.x;
     const int kvh = id % a.Hk;
     id /= a.Hk;
     const int split = id % splits;
     id /= splits;
-    const int s = id % a.S, tile = tiles - 1 - id / a.S;
+    int s, nq, tile;
     int64_t q0;
-    int nq;
-    query_rows(a, s, &q0, &nq);
+    if (!tile_of(a, id, TILE, &s, &q0, &nq, &tile)) return;
     const int rows = nq * a.G, r0 = tile * TILE;
-    if (r0 >= rows) return;
     const int len = a.kv_lens[s], all = min(len, min(a.max_kv, a.table_cols * kKv4Page));
     const int first = len - (a.cu_q ? (int)(a.cu_q[s + 1] - a.cu_q[s]) : 1);          // position of the sequence's first row
-    const int r = r0 + w * 32 + n, rc = min(r, rows - 1), tok = rc / a.G, head = kvh * a.G + (rc - tok * a.G);
+    const int rw = r0 + (TALL ? w : w & 3) * 32, r = rw + n, rc = min(r, rows - 1), tok = rc / a.G, head = kvh * a.G + (rc - tok * a.G);
     // tokens that a row of the workgroup sees; that every row of the wavefront sees; that this lane's row sees
     int begin = 0, end = all, begin_wg = 0, end_wg = all, begin_all = 0, end_all = all;
     if (a.causal) {
-        const int wa = min(r0 + w * 32, rows - 1) / a.G, wb = min(r0 + w * 32 + 31, rows - 1) / a.G, ga = r0 / a.G, gb = min(r0 + TILE - 1, rows - 1) / a.G;
+        const int wa = min(rw, rows - 1) / a.G, wb = min(rw + 31, rows - 1) / a.G, ga = r0 / a.G, gb = min(r0 + TILE - 1, rows - 1) / a.G;
         end = min(all, first + tok + 1);
         end_all = min(all, first + wa + 1);
         end_wg = min(all, first + gb + 1);
@@ -394,7 +429,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
         for (int i = 0; i < 16; ++i) o[j][i] = 0.0f;
     float l = 0.0f, ref = 0.0f, top_ref = -INFINITY;
 
-    const int group = w >> 2, thread = (int)threadIdx.x & 255;
+    const int thread = (int)threadIdx.x & 255;
     const int vq = thread >> 4, vc = thread & 15;                                     // this thread's quad of tokens and column of the values
     const int vpos = ((vq & ~3) | ((vq & 1) << 1) | ((vq >> 1) & 1)) * 8;             // where the quad lies in a row of LDS
     auto page_at = [&](int number) { return uniform_ptr(a.pool + ((int64_t)number * a.Hk + kvh) * HB); };
@@ -436,7 +471,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
     };
     // scales of tokens that are none: 0 times whatever they hold is to be 0
     auto real_scales = [&](Share<D>& g, int page) {
-        const int left = all - (page * kKv4Page + vq * 4);
+        const int left = page < 0 ? 0 : all - (page * kKv4Page + vq * 4);
         g.s &= (uint32_t)((1ull << (8 * min(max(left, 0), 4))) - 1);
     };
     // what is not seen, then a new reference where a score is 2^8 above the old one
@@ -505,21 +540,35 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
     // Phases, with pages 0, 1, ... as they come (M: matrix, V: vector):
     //     group 0          M0    V0    M1    V1    ...       unpacks the keys of page i + 1 in M_i
     //     group 1          .     M0    V0    M1    V1 ...    unpacks the values of page i + 1 in V_i, of page 0 in its first phase
-    // with a barrier between any two.  (One group alone: the keys of i + 1 in M_i, the values of i in V_i, a barrier behind V_i.)  M_i reads the
-    // keys of page i and the values of page i - 1.  The keys of i + 1 replace those of i - 1, and the values of i + 1 those of i - 1 (one group:
-    // of i those of i - 2): both read last in M_{i-1} and M_i of group 1, a barrier before.
+    // with a barrier between any two.  (Groups with their own buffers: the keys of i + 1 in M_i, the values of i in V_i, a barrier behind
+    // V_i; half a page apart they were no faster.)  M_i reads the keys of page i and the values of page i - 1.  The keys of i + 1 replace
+    // those of i - 1, and the values of i + 1 those of i - 1 (own buffers: of i those of i - 2): both read last in M_{i-1} and M_i of
+    // group 1, a barrier before.
     auto run = [&](auto role) {                          // 0: unpacks keys, 1: values, 2: both
         constexpr bool KEYS = decltype(role)::value != 1, VALUES = decltype(role)::value != 0;
         Share<D> sk, sv;
         v16f x[2];
         v4i pw[4];
-        int page = 0, next1 = 0, next2 = 0, n0 = next(&page);                             // numbers of this page and the next two, -1: none
-        if (n0 < 0) return;
-        int n1 = next(&next1), n2 = next(&next2);
-        auto there = [&](int number) { return page_at(number >= 0 ? number : n0); };     // (none: any page, unused)
-        if constexpr (VALUES) load_values(sv, page_at(n0));
+        // numbers of this page and the next two, -1: none, of a pair -2: none for this group, whose page is then -1 and has no tokens
+        int page = 0, next1 = 0, next2 = 0, some = -1;
+        auto step = [&](int* at) {
+            const int number = next(at);
+            if constexpr (!PAIR) return number;
+            if (number < 0) return -1;
+            if (some < 0) some = number;
+            int second = 0, behind = next(&second);
+            if (group == 0) return number;
+            *at = behind >= 0 ? second : -1;
+            return behind >= 0 ? behind : -2;
+        };
+        const int n0 = step(&page);
+        if (n0 == -1) return;
+        if constexpr (!PAIR) some = n0;
+        int n1 = step(&next1), n2 = step(&next2);
+        auto there = [&](int number) { return page_at(number >= 0 ? number : some); };   // (none: any page, unused)
+        if constexpr (VALUES) load_values(sv, there(n0));
         if constexpr (KEYS) {
-            load_keys(sk, page_at(n0));
+            load_keys(sk, there(n0));
             static_for([&](auto piece) { unpack_keys(piece, sk, lds_k(0)); }, IC<D / 32>{});
             load_keys(sk, there(n1));
         }
@@ -529,7 +578,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
             static_for([&](auto piece) { unpack_values(piece, sv, buf); }, IC<D / 16>{});
             load_values(sv, there(following));
         };
-        if constexpr (GROUPS == 2 && VALUES) {
+        if constexpr (TALL && VALUES) {
             values_of(page, lds_v(0), n1);
             lds_wait_and_barrier();                      // one phase behind
         }
@@ -565,40 +614,67 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
             if constexpr (KEYS) load_keys(sk, there(n2));
         };
         matrix(IC<4 * MT>{});
-        if constexpr (GROUPS == 2) lds_wait_and_barrier();
+        if constexpr (TALL) lds_wait_and_barrier();
         for (;;) {
             settle(x, page);
             weights(x, pw);
-            if constexpr (GROUPS == 1) values_of(page, lds_v(b), n1);
+            if constexpr (!TALL) values_of(page, lds_v(b), n1);
             else if constexpr (VALUES) values_of(next1, lds_v(b ^ 1), n2);
             lds_wait_and_barrier();
-            const bool more = n1 >= 0;
+            const bool more = n1 != -1;
             page = next1;
             next1 = next2;
             n1 = n2;
-            n2 = next(&next2);
+            n2 = step(&next2);
             b ^= 1;
             matrix(IC<0>{});                             // (behind the last page the scores are of whatever is there, unused)
             if (!more) break;
-            if constexpr (GROUPS == 2) lds_wait_and_barrier();
+            if constexpr (TALL) lds_wait_and_barrier();
         }
-        if constexpr (GROUPS == 2 && KEYS) lds_wait_and_barrier();
+        if constexpr (TALL && KEYS) lds_wait_and_barrier();
     };
-    if constexpr (GROUPS == 1) run(IC<2>{});
+    if constexpr (!TALL) run(IC<2>{});
     else if (group == 0) run(IC<0>{});
     else run(IC<1>{});
 
     // The output goes out row by row through the buffers' LDS, 32 rows of a wavefront in a part of its own: a lane has 16 bytes here
-    // and there of one row, and stores of such pieces keep the caches' request queues busy (the partial sums of 6 chunks of up to
-    // 500 tokens x 16 heads: the kernel 25.9 us with them, 24.6 us so).
+    // and there of one row, and stores of such pieces keep the caches' request queues busy (6 chunks of up to 500 tokens x 16 heads in
+    // parts: the kernel 25.9 us with them, 24.6 us so).
+    constexpr int PART = 32 * (D * (PAIR ? 4 : 2) + 16);
+    uint8_t* const part = lds + (TALL ? w : w & 3) * PART;
     l += __shfl_xor(l, 32);
     lds_wait_and_barrier();
+    if constexpr (PAIR) {                                 // the second group's sums go to the first
+        static_assert(PART >= 64 * MT * 16 * 4 && 4 * PART + 4 * 64 * 8 <= (int)sizeof(lds), "sums of four wavefronts");
+        f32x2* const ml = reinterpret_cast<f32x2*>(lds + 4 * PART) + (w & 3) * 64 + lane;
+        v4f* const sums = reinterpret_cast<v4f*>(part) + lane;
+        if (group == 1) {
+#pragma unroll
+            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sums[(j * 4 + i) * 64] = v4f{o[j][i * 4], o[j][i * 4 + 1], o[j][i * 4 + 2], o[j][i * 4 + 3]};
+            *ml = f32x2{top_ref, l};
+        }
+        lds_wait_and_barrier();
+        if (group == 1) return;
+        const f32x2 its = *ml;
+        const float top = fmaxf(top_ref, its.x), any = top == -INFINITY ? 0.0f : top;
+        const float f0 = __builtin_amdgcn_exp2f(top_ref - any), f1 = __builtin_amdgcn_exp2f(its.x - any);
+        top_ref = top;
+        l = l * f0 + its.y * f1;
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const v4f x = sums[(j * 4 + i) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j][i * 4 + e] = o[j][i * 4 + e] * f0 + x[e] * f1;
+            }
+    }
     const bool mine = r < rows;
     const int64_t t = q0 + tok, at = t * (a.Hk * a.G) + head;
-    auto rows_out = [&](auto bytes, uint64_t address, auto piece) {        // bytes of a channel; address of the lane's row, 0: none
+    auto rows_out = [&](auto bytes, uint64_t address, auto piece) {         // bytes of a channel; address of the lane's row, 0: none
         constexpr int E = decltype(bytes)::value, PITCH = D * E + 16, LANES = D * E / 16;
-        static_assert(4 * GROUPS * 32 * PITCH <= (int)sizeof(lds), "a part for each wavefront");
-        uint8_t* part = lds + w * (32 * PITCH);
         piece(part + n * PITCH);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
@@ -609,8 +685,8 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_attention_many(const AttnAr
             if ((lo | hi) != 0) *reinterpret_cast<v4i*>((((uint64_t)hi << 32) | lo) + lane % LANES * 16) = v;
         }
     };
-    if (GROUPS == 1 && part_o) {
-        if constexpr (GROUPS == 1) rows_out(IC<4>{}, mine ? reinterpret_cast<uint64_t>(part_o + (at * splits + split) * D) : 0, [&](uint8_t* to) {
+    if (PAIR && part_o) {
+        rows_out(IC<4>{}, mine ? reinterpret_cast<uint64_t>(part_o + (at * splits + split) * D) : 0, [&](uint8_t* to) {
 #pragma unroll
             for (int q = 0; q < 8; ++q)
 #pragma unroll
@@ -645,14 +721,23 @@ template <int D, int GROUPS>
 __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int splits, const float* part_o, const float* part_ml) {
     constexpr int TH = D / 4, ROWS = 256 / (TH * GROUPS);
     const int Hq = a.Hk * a.G, mine = (int)threadIdx.x / (TH * GROUPS), group = (int)threadIdx.x / TH % GROUPS, d = (int)(threadIdx.x % TH) * 4;
-    const int64_t id = (int64_t)blockIdx.x * ROWS + mine, si = id / Hq;     // (sequence, row, head)
-    const int h = (int)(id - si * Hq), s = (int)(si / a.max_q), i = (int)(si - (int64_t)s * a.max_q);
-    int64_t q0 = 0;
-    int nq = 0;
-    if (s < a.S) query_rows(a, s, &q0, &nq);
-    const bool there = i < nq;
+    const int64_t at = (int64_t)blockIdx.x * ROWS + mine, t = at / Hq;      // (token, head)
+    const int h = (int)(at - t * Hq);
+    // is the row a sequence's? (of up to 64/TH rows in a wavefront)
+    bool there = false;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+        int64_t b = 0;
+        int n = 0;
+        if (s0 + (int)(threadIdx.x & 63) < a.S) query_rows(a, s0 + (int)(threadIdx.x & 63), &b, &n);
+        if (n == 0) b = a.T;
+#pragma unroll
+        for (int k = 0; k < 64 / TH; ++k) {
+            const int tk = __builtin_amdgcn_readlane((int)t, k * TH);
+            const bool its = __ballot(tk >= (int)b && tk < (int)b + n) != 0;
+            if ((int)(threadIdx.x & 63) / TH == k) there |= its;
+        }
+    }
     if (GROUPS == 1 && !there) return;
-    const int64_t t = q0 + i, at = there ? t * Hq + h : 0;
     const float *po = part_o + at * splits * D + d, *pm = part_ml + at * splits * 2;
     float m = -INFINITY, sum = 0.0f;
     v4f y = {0, 0, 0, 0};
@@ -693,47 +778,51 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 }
 
 // How a call is cut up.  Up to 16 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
-// pages.  More: tiles of 256 rows where there is one for every CU, else of 128 (8192 tokens x 32 heads: 482 us, 529 us with tiles
-// of 128).  The pages are split, none to less than eight pages, where the tiles alone leave CUs idle: to two workgroups a CU (one row of
-// 131 072 tokens: 34 us, to four a CU 38 to 45 us for the joining; 6 chunks of up to 500 tokens over up to 4000: 28 us, to four 30 us).
-// Few rows of several sequences: to four a CU, because the sequences' lengths differ and shorter parts even out (100 of up to 8192
-// tokens: 121 us, 125 us with two).
+// pages.  More: one group for contexts of up to 6 pages (350 tokens, 32 heads: 15.2 us, 15.8 us paired; 512: 18.3 either way); tall
+// tiles where tiles of 128 rows would be more than the CUs take at once, one a CU or with heads of 64 two, of which half is enough
+// (6 chunks of up to 500 tokens over up to 4000, 32 heads of 128: 39 us, 54 us paired; 4 of up to 1000 over 2000, 16 heads of 64: 48 us,
+// 42 us paired); else pairs.
+// The pages are split, none to less than eight, where the tiles alone leave CUs idle.  Many rows: to one workgroup a CU at most, since
+// every split writes and reads its rows' sums in 32 bits (256 tokens over 8192, 32 heads: 57 us, to two a CU 66 us, whole 132 us).  Few:
+// to two a CU (one row of 131 072 tokens: 34 us, to four a CU 38 to 45 us for the joining), of several sequences to four, because the
+// sequences' lengths differ and shorter parts even out (100 of up to 8192 tokens: 121 us, 125 us with two).
 struct Plan {
     bool few;
-    int groups;                  // of 128 rows in a tile
-    int64_t tiles;
+    int mode;                    // of the kernel for many rows
+    int64_t tiles;               // of a head of the cache (few: one a sequence)
     int splits;
-    static Plan of(int64_t T, int64_t S, int Hk, int G, int64_t max_q, int64_t max_kv, int cus) {
+    static Plan of(int64_t T, int64_t S, int Hk, int G, int D, int64_t max_q, int64_t max_kv, int cus) {
         const bool few = max_q * G <= 16;
         const int64_t pages = (max_kv + kKv4Page - 1) / kKv4Page;
         // tiles that a call of T rows can have, whatever the longest sequence's
         auto most = [&](int64_t rows) { return std::min(S * ((max_q * G + rows - 1) / rows), T * G / rows + S); };
-        const int groups = !few && Hk * most(256) >= cus ? 2 : 1;
-        const int64_t tiles = few ? 1 : (max_q * G + 128 * groups - 1) / (128 * groups), wgs = Hk * (few ? S : most(128 * groups));
-        int64_t n = ((few && S > 1 ? 4 : 2) * cus + wgs - 1) / wgs;
+        const int mode = few || pages <= 6 ? kOne : Hk * most(128) > cus * (D == 64 ? 3 : 2) / 2 ? kTall : kPair;
+        const int64_t tiles = few ? S : most(mode == kTall ? 256 : 128), wgs = Hk * tiles;
+        int64_t n = few ? ((S > 1 ? 4 : 2) * cus + wgs - 1) / wgs : mode == kPair ? cus / wgs : 1;
         n = std::min(n, (pages + 7) / 8);
-        return {few, groups, tiles, groups == 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
+        return {few, mode, tiles, (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
     }
 };
 
 }  // namespace
 
 int64_t kv4_attention_workspace(int64_t T, int64_t S, int Hq, int Hk, int D, int64_t max_q, int64_t max_kv, int cus) {
-    const Plan p = Plan::of(T, S, Hk, Hq / Hk, max_q, max_kv, cus);
+    const Plan p = Plan::of(T, S, Hk, Hq / Hk, D, max_q, max_kv, cus);
     return p.splits == 1 ? 0 : T * Hq * p.splits * (D + 2) * 4;
 }
 
 template <int D>
 static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t stream) {
     const int Hq = a.Hk * a.G;
-    const Plan p = Plan::of(a.T, a.S, a.Hk, a.G, a.max_q, a.max_kv, cus);
+    const Plan p = Plan::of(a.T, a.S, a.Hk, a.G, D, a.max_q, a.max_kv, cus);
     float *po = p.splits == 1 ? nullptr : static_cast<float*>(a.workspace), *pm = po ? po + a.T * Hq * p.splits * D : nullptr;
-    const dim3 grid((uint32_t)(a.S * a.Hk * p.tiles * p.splits));
+    const dim3 grid((uint32_t)(p.tiles * a.Hk * p.splits));
     if (p.few) hipLaunchKernelGGL((k_attention_few<D>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
-    else if (p.groups == 2) hipLaunchKernelGGL((k_attention_many<D, 2>), grid, dim3(512), 0, stream, a, (int)p.tiles, p.splits, po, pm);
-    else hipLaunchKernelGGL((k_attention_many<D, 1>), grid, dim3(256), 0, stream, a, (int)p.tiles, p.splits, po, pm);
+    else if (p.mode == kTall) hipLaunchKernelGGL((k_attention_many<D, kTall>), grid, dim3(512), 0, stream, a, 1, nullptr, nullptr);
+    else if (p.mode == kPair) hipLaunchKernelGGL((k_attention_many<D, kPair>), grid, dim3(512), 0, stream, a, p.splits, po, pm);
+    else hipLaunchKernelGGL((k_attention_many<D, kOne>), grid, dim3(256), 0, stream, a, 1, nullptr, nullptr);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;
-    const int64_t rows = (int64_t)a.S * a.max_q * Hq;
+    const int64_t rows = a.T * Hq;
     if (p.splits <= 8) hipLaunchKernelGGL((k_attention_join<D, 1>), dim3((uint32_t)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, stream, a, p.splits, po, pm);
     else hipLaunchKernelGGL((k_attention_join<D, 1024 / D>), dim3((uint32_t)rows), dim3(256), 0, stream, a, p.splits, po, pm);
     return hipGetLastError();

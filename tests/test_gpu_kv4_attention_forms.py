@@ -1,0 +1,129 @@
+"""Attention of many rows in each of the forms a call can take: one group of wavefronts a tile (contexts of up to 6 pages), two that
+share a tile's pages, tall tiles (where there are many).  The bound max_kv, not the lengths, says which, so the same small cases go
+through all."""
+import math
+
+import pytest
+import torch
+
+import attn_ref as ref
+import paper_2511_04214_amd as brq
+import test_gpu_kv4_attention as base
+
+pytestmark = pytest.mark.gpu
+# sequences, heads of the cache, max_kv
+FORMS = {"one": (12, 2, 384), "pair": (12, 2, 500), "pair in parts": (12, 2, 1000), "tall": (130, 4, 1000)}
+
+
+def lengths(S, seed):
+    g = torch.Generator().manual_seed(seed)
+    qs = torch.randint(1, 6, (S,), generator=g).tolist()
+    lens = [n + int(torch.randint(0, 200, (1,), generator=g)) for n in qs]
+    qs[3], lens[3] = 290, 290                            # a whole prompt, over more than one tile, an odd number of pages
+    qs[4], lens[4] = 130, 384                            # an even number
+    qs[5], lens[5] = 64, 64                              # one page
+    qs[6], lens[6] = 0, 70                               # no rows
+    qs[7], lens[7] = 5, 2                                # rows in front of the first token
+    qs[8], lens[8] = 3, 0                                # no tokens
+    qs[9], lens[9] = 20, 129                             # a token of the last page
+    return qs, lens
+
+
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 1), (True, 70), (False, 0)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_ragged(form, D, causal, window):
+    S, Hk, max_kv = FORMS[form]
+    base.run(S, *lengths(S, D), Hk, Hk, D, causal, window, seed=31, max_kv=max_kv)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_heads_in_groups(form, D):
+    S, Hk, max_kv = FORMS[form]
+    base.run(S, *lengths(S, 32), 3 * Hk, Hk, D, seed=32, sharp=4.0, max_kv=max_kv)
+    base.run(S, *lengths(S, 33), 2 * Hk, Hk, D, seed=33, spread=6, max_kv=max_kv)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_pages_that_are_none_and_bytes_behind_the_end(form, D):
+    """First, middle, last and all pages missing; what stands behind a context's end changes nothing."""
+    g = torch.Generator().manual_seed(34)
+    S, Hk, max_kv = FORMS[form]
+    pool = base.cache(g, 40, Hk, D)
+    table = torch.randint(0, 39, (S, 5), generator=g).to(torch.int32)
+    table[0, 0], table[1, 1], table[2, 3], table[3], table[4, :3], table[6, 1:4] = -1, 40, 1 << 30, -1, -7, -1
+    table[5] = torch.tensor([1, 2, 39, 0, 3])            # page 39: its one token, and what is behind it
+    lens, qs = [256, 250, 320, 200, 256, 129, 320] + [100] * (S - 7), [70, 3, 90, 20, 5, 129, 140] + [2] * (S - 7)
+    cu = torch.tensor([0] + qs).cumsum(0).to(torch.int32)
+    q = torch.randn((sum(qs), Hk, D), generator=g).to(torch.bfloat16)
+    a = (table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda())
+    kw = dict(cu_q=cu.cuda(), max_q=140, max_kv=max_kv, want_lse=True)
+    out, lse = brq.kv4_attention(q.cuda(), pool.cuda(), *a, **kw)
+    base.check(out, ref.attention(q, ref.cache_values(pool, Hk, D), table, lens, D ** -0.5, True, 0, cu, 140, max_kv), lse)
+    bad = pool.clone().view(40, Hk, 68 * D)
+    kc, ks, vc, vs = ref.page_index(D)
+    for at, fill in ((kc, 0x77), (vc, 0xff), (ks, 0xff), (vs, 0xff)):
+        bad[39][:, at[1:].flatten()] = fill
+    again, l2 = brq.kv4_attention(q.cuda(), bad.view(40, -1).cuda(), *a, **kw)
+    assert torch.equal(out, again) and torch.equal(lse, l2)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_repeats_strides_streams_and_graphs(form, D):
+    S, Hk, max_kv = FORMS[form]
+    qs, lens = lengths(S, 7)
+    q, pool, table, cu, out, lse = base.run(S, qs, lens, 2 * Hk, Hk, D, seed=35, max_kv=max_kv)
+    dev = [t.cuda() for t in (q, pool, table)] + [torch.tensor(lens, dtype=torch.int32).cuda()]
+    a = dict(cu_q=cu.cuda(), max_q=max(qs), max_kv=max_kv, want_lse=True)
+    wide = torch.zeros((q.shape[0], 2 * Hk + 3, D + 8), dtype=torch.bfloat16, device="cuda")
+    wide[:, 1: 2 * Hk + 1, :D] = dev[0]
+    got, l2 = brq.kv4_attention(wide[:, 1: 2 * Hk + 1, :D], *dev[1:], out=torch.empty((2 * Hk, q.shape[0], D), dtype=torch.bfloat16, device="cuda").transpose(0, 1), **a)
+    assert torch.equal(got, out) and torch.equal(l2, lse)
+    y, z = torch.zeros_like(out), torch.zeros_like(lse)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        brq.kv4_attention(*dev, out=y, lse=z, **a)
+    for _ in range(3):
+        y.zero_(), z.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, out) and torch.equal(z, lse)
+
+
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 128, 500])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_a_nan_in_a_query_is_its_rows_alone(form, D, n):
+    g = torch.Generator().manual_seed(36)
+    S, Hk, max_kv = FORMS[form]
+    q, cols = 20, -(-n // 64)
+    pool = base.cache(g, 10, Hk, D)
+    table = torch.randint(0, 10, (S, cols), generator=g).to(torch.int32)
+    x = torch.randn((S * q, Hk, D), generator=g).to(torch.bfloat16)
+    a = (pool.cuda(), table.cuda(), torch.full((S,), n, dtype=torch.int32).cuda())
+    kw = dict(cu_q=torch.arange(0, S * q + 1, q, dtype=torch.int32).cuda(), max_q=q, max_kv=max_kv, causal=False, want_lse=True)
+    out, lse = brq.kv4_attention(x.cuda(), *a, **kw)
+    assert not torch.isnan(out).any() and not torch.isnan(lse).any()
+    t = S * q // 2
+    x[t, 1, 7] = math.nan
+    got, l2 = brq.kv4_attention(x.cuda(), *a, **kw)
+    assert torch.isnan(got[t, 1]).all() and torch.isnan(l2[t, 1])
+    keep = torch.ones((S * q, Hk), dtype=torch.bool, device="cuda")
+    keep[t, 1] = False
+    assert torch.equal(got[keep], out[keep]) and torch.equal(l2[keep], lse[keep])
+
+
+def test_few_long_sequences_among_many_short():
+    """A grid sized by the rows, not by sequences times the longest: every tile of every sequence is reached, in more than 64 sequences."""
+    S = 150
+    qs, lens = [0] * S, [10] * S
+    for s, n in ((0, 3), (63, 200), (64, 1), (65, 129), (149, 300)):
+        qs[s], lens[s] = n, n + 30
+    for max_kv in (384, 1000):
+        base.run(S, qs, lens, 4, 2, 64, seed=37, max_kv=max_kv)
+        base.run(S, qs, lens, 4, 2, 128, seed=37, max_kv=max_kv, window=100)
