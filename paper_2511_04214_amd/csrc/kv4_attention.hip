@@ -784,8 +784,9 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 // 42 us paired); else pairs.
 // The pages are split, none to less than eight, where the tiles alone leave CUs idle.  Many rows: to one workgroup a CU at most, since
 // every split writes and reads its rows' sums in 32 bits (256 tokens over 8192, 32 heads: 57 us, to two a CU 66 us, whole 132 us).  Few:
-// to two a CU (one row of 131 072 tokens: 34 us, to four a CU 38 to 45 us for the joining), of several sequences to four, because the
-// sequences' lengths differ and shorter parts even out (100 of up to 8192 tokens: 121 us, 125 us with two).
+// to one a CU (one row of 131 072 tokens in a cache: 29 us, to two a CU 31 us), of several sequences to four if that leaves 32 pages to a
+// split, because the sequences' lengths differ and shorter parts even out (72 of up to 8192 tokens: 95 us, 106 us to one a CU; 64 of up
+// to 2000, which it leaves whole: 22 us, 27 us to four a CU).
 struct Plan {
     bool few;
     int mode;                    // of the kernel for many rows
@@ -798,7 +799,8 @@ struct Plan {
         auto most = [&](int64_t rows) { return std::min(S * ((max_q * G + rows - 1) / rows), T * G / rows + S); };
         const int mode = few || pages <= 6 ? kOne : Hk * most(128) > cus * (D == 64 ? 3 : 2) / 2 ? kTall : kPair;
         const int64_t tiles = few ? S : most(mode == kTall ? 256 : 128), wgs = Hk * tiles;
-        int64_t n = few ? ((S > 1 ? 4 : 2) * cus + wgs - 1) / wgs : mode == kPair ? cus / wgs : 1;
+        int64_t n = few ? (cus + wgs - 1) / wgs : mode == kPair ? cus / wgs : 1;
+        if (few && S > 1) n = std::max(n, std::min((4 * cus + wgs - 1) / wgs, (pages + 16) / 32));
         n = std::min(n, (pages + 7) / 8);
         return {few, mode, tiles, (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
     }
