@@ -72,7 +72,7 @@ struct Found {
 };
 
 // Pages that item i wants: FORK: one where its parent's last page is not full; reserve: its row's columns below the wanted
-// length that have no page, or -1 where the table has too few columns.
+// length that have no page, none where the table has too few columns.
 template <bool FORK>
 __device__ __forceinline__ int wanted(const PagesArgs& a, int i) {
     if constexpr (FORK) {
@@ -85,57 +85,54 @@ __device__ __forceinline__ int wanted(const PagesArgs& a, int i) {
         const int s = a.a[i], tokens = a.b[i];
         if (!in_range(s, a.S) || tokens <= 0) return 0;
         const int cols = (tokens - 1) / kKv4Page + 1;
-        if (cols > a.cols) return -1;
+        if (cols > a.cols) return 0;
         int n = 0;
         for (int c = 0; c < cols; ++c) n += a.table[(int64_t)s * a.cols + c] < 0;
         return n;
     }
 }
 
-// A wavefront fills the empty columns of item i's row; `found`: how many pages there are for all.
-__device__ __forceinline__ void fill_row(const PagesArgs& a, const Found& f, int i, int found, int lane) {
-    const int s = a.a[i], tokens = a.b[i];
-    if (!in_range(s, a.S) || tokens <= 0) return;
-    const int cols = (tokens - 1) / kKv4Page + 1;
-    int32_t* row = a.table + (int64_t)s * a.cols;
-    bool failed = cols > a.cols;
-    int need = 0;
-    if (!failed) {
-        for (int c0 = 0; c0 < cols; c0 += 64) need += __popcll(__ballot(c0 + lane < cols && row[c0 + lane] < 0));
-        failed = need > 0 && (int64_t)f.first[i] + need > found;
+// A row of the table that is to get pages, LANES lanes to it.
+template <int LANES>
+struct Row {
+    int32_t* at = nullptr;
+    int cols = 0, need = 0;
+    bool none = false;           // too few columns
+    __device__ static uint64_t bits(bool b) {
+        return LANES == 64 ? __ballot(b) : __ballot(b) >> (threadIdx.x & (64u - LANES)) & ((1ull << (LANES & 63)) - 1);
     }
-    if (failed) {
-        if (lane == 0) atomicAdd(a.result, 1);
-        return;
-    }
-    int at = f.first[i];
-    for (int c0 = 0; c0 < cols && need > 0; c0 += 64) {
-        const bool empty = c0 + lane < cols && row[c0 + lane] < 0;
-        const uint64_t m = __ballot(empty);
-        if (empty) {
-            const int page = f.pages[at + __popcll(m & ((1ull << lane) - 1))];
-            row[c0 + lane] = page;
-            a.refs[page] = 1;
+    __device__ Row(const PagesArgs& a, int i, int lane) {
+        if (i < a.n && in_range(a.a[i], a.S) && a.b[i] > 0) {
+            cols = (a.b[i] - 1) / kKv4Page + 1;
+            at = a.table + (int64_t)a.a[i] * a.cols;
+            none = cols > a.cols;
+            if (none) cols = 0;
         }
-        at += __popcll(m);
+        for (int c0 = 0; __any(c0 < cols); c0 += LANES) need += __popcll(bits(c0 + lane < cols && at[c0 + lane] < 0));
     }
-}
+    // `first`: its first page of those found, `found` of them.
+    __device__ void fill(const PagesArgs& a, const int32_t* pages, int first, int found, int lane) {
+        if (none || (need > 0 && (int64_t)first + need > found)) {
+            if (lane == 0) atomicAdd(a.result, 1);
+            cols = 0;
+        }
+        if (need == 0) cols = 0;
+        for (int c0 = 0; __any(c0 < cols); c0 += LANES) {
+            const bool empty = c0 + lane < cols && at[c0 + lane] < 0;
+            const uint64_t m = bits(empty);
+            if (empty) {
+                const int page = pages[first + __popcll(m & ((1ull << lane) - 1))];
+                at[c0 + lane] = page;
+                a.refs[page] = 1;
+            }
+            first += __popcll(m);
+        }
+    }
+};
 
-// FILL: reservations of few sequences are made by the same workgroup, a wavefront a row (up to 64 of them: a launch saved is worth
-// four rounds of its 16 wavefronts).
-template <bool FORK, bool FILL>
-__global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
-    __shared__ int lds[17];
-    const Found f(a.workspace, a.n);
-    int want = 0, total, r[kPer];
-    load_refs(a.refs, a.num_pages, (int)threadIdx.x * kPer, r);                   // (on their way while the wants are counted)
-    for (int i0 = 0; i0 < a.n; i0 += kScan) {
-        const int i = i0 + (int)threadIdx.x, w = i < a.n ? wanted<FORK>(a, i) : 0;
-        const int before = scan_before(w > 0 ? w : 0, lds, &total);
-        if (i < a.n) f.first[i] = min(want + before, a.num_pages);               // (more than there are is as good as any more)
-        want = min(want + total, a.num_pages);
-    }
-    int found = 0;
+// The first `want` free pages, lowest first, by a workgroup; r: the thread's counts, of the first step already there.  Returns how many.
+__device__ __forceinline__ int find_free(const PagesArgs& a, int32_t* pages, int want, int (&r)[kPer], int* lds) {
+    int found = 0, total;
     for (int at = 0; at < a.num_pages && found < want; at += kScan * kPer) {
         int n = 0;
         const int mine = at + (int)threadIdx.x * kPer;
@@ -146,19 +143,47 @@ __global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
             if (r[i] == 0) {
-                if (rank < want) f.pages[rank] = mine + i;
+                if (rank < want) pages[rank] = mine + i;
                 ++rank;
             }
         found += total;
     }
+    return min(found, want);
+}
+
+template <bool FORK>
+__global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
+    __shared__ int lds[17];
+    const Found f(a.workspace, a.n);
+    int want = 0, total, r[kPer];
+    load_refs(a.refs, a.num_pages, (int)threadIdx.x * kPer, r);                   // (on their way while the wants are counted)
+    for (int i0 = 0; i0 < a.n; i0 += kScan) {
+        const int i = i0 + (int)threadIdx.x, w = i < a.n ? wanted<FORK>(a, i) : 0;
+        const int before = scan_before(w, lds, &total);
+        if (i < a.n) f.first[i] = min(want + before, a.num_pages);               // (more than there are is as good as any more)
+        want = min(want + total, a.num_pages);
+    }
+    const int found = find_free(a, f.pages, want, r, lds);
     if (threadIdx.x == 0) {
-        f.count[0] = min(found, want);
+        f.count[0] = found;
         a.result[0] = 0;
     }
-    if constexpr (FILL) {
-        __syncthreads();
-        for (int i = (int)(threadIdx.x >> 6); i < a.n; i += kScan / 64) fill_row(a, f, i, min(found, want), (int)(threadIdx.x & 63u));
-    }
+}
+
+// Reservations of up to 64 sequences in one launch, 16 lanes a row: 48 of 1000 tokens each 5.5 us; with a lane a row to count and a
+// wavefront a row to fill, a launch apart or not, 8.4 us.
+__global__ __launch_bounds__(kScan) void k_reserve_few(const PagesArgs a) {
+    __shared__ int lds[17];
+    const Found f(a.workspace, a.n);
+    const int lane = (int)threadIdx.x & 15;
+    int total, r[kPer];
+    load_refs(a.refs, a.num_pages, (int)threadIdx.x * kPer, r);
+    Row<16> row(a, (int)threadIdx.x >> 4, lane);
+    if (threadIdx.x == 0) a.result[0] = 0;
+    const int first = __shfl(scan_before(lane == 0 ? row.need : 0, lds, &total), (int)threadIdx.x & 48);
+    const int found = find_free(a, f.pages, min(total, a.num_pages), r, lds);
+    __syncthreads();
+    row.fill(a, f.pages, first, found, lane);
 }
 
 // Pairs (parent, child): `parts` workgroups copy the last page's bytes, the first of them also writes the child's row.
@@ -198,7 +223,8 @@ __global__ __launch_bounds__(256) void k_fork(const PagesArgs a, int parts) {
 
 __global__ __launch_bounds__(64) void k_reserve(const PagesArgs a) {
     const Found f(a.workspace, a.n);
-    fill_row(a, f, (int)blockIdx.x, f.count[0], (int)threadIdx.x);
+    const int i = (int)blockIdx.x, lane = (int)threadIdx.x;
+    Row<64>(a, i, lane).fill(a, f.pages, f.first[i], f.count[0], lane);
 }
 
 // The entry is taken out by an exchange: a sequence named twice is given up once.
@@ -305,7 +331,7 @@ hipError_t launch_pages_copy(const PagesArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((k_find_free<true, false>), dim3(1), dim3(kScan), 0, stream, a);
+    hipLaunchKernelGGL((k_find_free<true>), dim3(1), dim3(kScan), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (a.n == 0) return hipSuccess;
     const int parts = parts_of(a.page_bytes);
@@ -320,10 +346,10 @@ hipError_t launch_pages_free(const PagesArgs& a, hipStream_t stream) {
 
 hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream) {
     if (a.n <= 64) {
-        hipLaunchKernelGGL((k_find_free<false, true>), dim3(1), dim3(kScan), 0, stream, a);
+        hipLaunchKernelGGL(k_reserve_few, dim3(1), dim3(kScan), 0, stream, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((k_find_free<false, false>), dim3(1), dim3(kScan), 0, stream, a);
+    hipLaunchKernelGGL((k_find_free<false>), dim3(1), dim3(kScan), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(k_reserve, dim3((uint32_t)a.n), dim3(64), 0, stream, a);
     return hipGetLastError();
