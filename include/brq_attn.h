@@ -107,14 +107,15 @@ brq_status brq_kv4_read(const uint8_t* pool, int64_t num_pages, int64_t T, int64
 
 /*
  * Attention of T query rows of S sequences over the cache.  Sequence s has query rows cu_q[s] ... cu_q[s+1] - 1
- * (cu_q: [S + 1], ascending, or a sequence may come out unwritten; NULL: one row each, T = S) and the tokens 0 ... kv_lens[s] - 1, token j in page
- * table[s * table_cols + j / 64].  Its queries are the last of them: row i of n stands at position
- * p = kv_lens[s] - n + i.  With Hk heads in the cache, q.heads a multiple of it, query head h reads head
- * h / (q.heads / Hk):
+ * (cu_q: [S + 1], ascending, or rows may be left unwritten; NULL: one row each, T = S) and the tokens
+ * 0 ... kv_lens[s] - 1, token j in page table[s * table_cols + j / 64].  Its queries are the last of them: row i
+ * of n stands at position p = kv_lens[s] - n + i.  With Hk heads in the cache, q.heads a multiple of it, query
+ * head h reads head h / (q.heads / Hk):
  *     a_j = scale * q . k_j  for the j that the row sees,   o = sum_j exp(a_j) v_j / sum_j exp(a_j),
  *     lse = log sum_j exp(a_j)
  * The row sees j < kv_lens[s]; with `causal` j <= p, and with window > 0 (causal only) j > p - window.  A row
- * that sees nothing has o = 0, lse = -infinity; a NaN in a query makes its row NaN and no other.  Tokens whose page number is outside the cache are not seen.
+ * that sees nothing has o = 0, lse = -infinity; a NaN in a query makes its row NaN and no other.  Tokens whose
+ * page number is outside the cache are not seen.
  * q and out are BRQ_BF16; lse [T][q.heads] fp32 or NULL.  Arithmetic: products exact, summed in the matrix
  * cores' fp32, softmax in fp32, its weights rounded to bf16 in front of the product with the values.
  * max_q, max_kv: what the host knows of the longest query and context; rows beyond max_q of a sequence, and rows
