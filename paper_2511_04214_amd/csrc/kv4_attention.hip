@@ -785,7 +785,8 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 // tiles where tiles of 128 rows would be more than the CUs take at once, one a CU or with heads of 64 two, of which half is enough
 // (6 chunks of up to 500 tokens over up to 4000, 32 heads of 128: 39 us, 54 us paired; 4 of up to 1000 over 2000, 16 heads of 64: 48 us,
 // 42 us paired); else pairs.
-// The pages are split, none to less than eight, where the tiles alone leave CUs idle.  Many rows: to one workgroup a CU at most, since
+// The pages are split, to no less than eight, where the tiles alone leave CUs idle; up to 16 of few rows never, which the join takes
+// longer for than they do (1000 tokens: 8.1 us, 8.9 us in halves; 1300 9.7 and 9.2).  Many rows: to one workgroup a CU at most, since
 // every split writes and reads its rows' sums in 32 bits (256 tokens over 8192, 32 heads: 57 us, to two a CU 66 us, whole 132 us).  Few:
 // to one a CU (one row of 131 072 tokens in a cache: 29 us, to two a CU 31 us), of several sequences to four if that leaves 32 pages to a
 // split, because the sequences' lengths differ and shorter parts even out (72 of up to 8192 tokens: 95 us, 106 us to one a CU; 64 of up
@@ -795,16 +796,17 @@ struct Plan {
     int mode;                    // of the kernel for many rows
     int64_t tiles;               // of a head of the cache (few: one a sequence)
     int splits;
-    static Plan of(int64_t T, int64_t S, int Hk, int G, int D, int64_t max_q, int64_t max_kv, int cus) {
+    static Plan of(int64_t T, int64_t S, int Hk, int G, int D, int64_t max_q, int64_t max_kv, int window, int cus) {
         const bool few = max_q * G <= 16;
-        const int64_t pages = (max_kv + kKv4Page - 1) / kKv4Page;
+        // what a sequence's rows can see (a window makes parts fewer, never more: the workspace is sized without one)
+        const int64_t seen = window ? std::min<int64_t>(max_kv, window + max_q + 2 * kKv4Page) : max_kv, pages = (seen + kKv4Page - 1) / kKv4Page;
         // tiles that a call of T rows can have, whatever the longest sequence's
         auto most = [&](int64_t rows) { return std::min(S * ((max_q * G + rows - 1) / rows), T * G / rows + S); };
         const int mode = few || pages <= 6 ? kOne : Hk * most(128) > cus * (D == 64 ? 3 : 2) / 2 ? kTall : kPair;
         const int64_t tiles = few ? S : most(mode == kTall ? 256 : 128), wgs = Hk * tiles;
         int64_t n = few ? (cus + wgs - 1) / wgs : mode == kPair ? cus / wgs : 1;
         if (few && S > 1) n = std::max(n, std::min((4 * cus + wgs - 1) / wgs, (pages + 16) / 32));
-        n = std::min(n, (pages + 7) / 8);
+        n = few && pages <= 16 ? 1 : std::min(n, (pages + 7) / 8);
         return {few, mode, tiles, (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
     }
 };
@@ -812,14 +814,14 @@ struct Plan {
 }  // namespace
 
 int64_t kv4_attention_workspace(int64_t T, int64_t S, int Hq, int Hk, int D, int64_t max_q, int64_t max_kv, int cus) {
-    const Plan p = Plan::of(T, S, Hk, Hq / Hk, D, max_q, max_kv, cus);
+    const Plan p = Plan::of(T, S, Hk, Hq / Hk, D, max_q, max_kv, 0, cus);
     return p.splits == 1 ? 0 : T * Hq * p.splits * (D + 2) * 4;
 }
 
 template <int D>
 static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t stream) {
     const int Hq = a.Hk * a.G;
-    const Plan p = Plan::of(a.T, a.S, a.Hk, a.G, D, a.max_q, a.max_kv, cus);
+    const Plan p = Plan::of(a.T, a.S, a.Hk, a.G, D, a.max_q, a.max_kv, a.causal ? a.window : 0, cus);
     float *po = p.splits == 1 ? nullptr : static_cast<float*>(a.workspace), *pm = po ? po + a.T * Hq * p.splits * D : nullptr;
     const dim3 grid((uint32_t)(p.tiles * a.Hk * p.splits));
     if (p.few) hipLaunchKernelGGL((k_attention_few<D>), grid, dim3(256), 0, stream, a, p.splits, po, pm);

@@ -319,13 +319,16 @@ __global__ __launch_bounds__(256) void k_move(const PagesArgs a, int parts) {
     }
 }
 
-// Workgroups to a page: 16 KB each.
-int parts_of(int64_t page_bytes) { return (int)((page_bytes + 16383) / 16384); }
+// Workgroups to each of n pages: 16 KB a piece, and no more than a grid can have.
+int parts_of(int64_t page_bytes, int64_t n) {
+    const int64_t parts = (page_bytes + 16383) / 16384, most = (int64_t(1) << 23) / n;
+    return (int)(parts < most ? parts : most > 1 ? most : 1);
+}
 
 }  // namespace
 
 hipError_t launch_pages_copy(const PagesArgs& a, hipStream_t stream) {
-    const int parts = parts_of(a.page_bytes);
+    const int parts = parts_of(a.page_bytes, a.n);
     hipLaunchKernelGGL(k_copy, dim3((uint32_t)a.n * parts), dim3(256), 0, stream, a, parts);
     return hipGetLastError();
 }
@@ -334,7 +337,7 @@ hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((k_find_free<true>), dim3(1), dim3(kScan), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (a.n == 0) return hipSuccess;
-    const int parts = parts_of(a.page_bytes);
+    const int parts = parts_of(a.page_bytes, a.n);
     hipLaunchKernelGGL(k_fork, dim3((uint32_t)a.n * parts), dim3(256), 0, stream, a, parts);
     return hipGetLastError();
 }
@@ -358,7 +361,7 @@ hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream) {
 hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(k_plan_moves, dim3(1), dim3(kScan), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_move, dim3(2048), dim3(256), 0, stream, a, parts_of(a.page_bytes));
+    hipLaunchKernelGGL(k_move, dim3(2048), dim3(256), 0, stream, a, parts_of(a.page_bytes, 1));
     return hipGetLastError();
 }
 

@@ -127,3 +127,13 @@ def test_few_long_sequences_among_many_short():
     for max_kv in (384, 1000):
         base.run(S, qs, lens, 4, 2, 64, seed=37, max_kv=max_kv)
         base.run(S, qs, lens, 4, 2, 128, seed=37, max_kv=max_kv, window=100)
+
+
+@pytest.mark.parametrize("window", [1, 300, 1000, 3000])
+@pytest.mark.parametrize("D", [64, 128])
+def test_windows_in_long_contexts(D, window):
+    """Parts are counted by what a window shows; it stands anywhere in a context."""
+    base.run(1, [1], [5000], 8, 2, D, window=window, seed=38)
+    base.run(3, [1, 1, 1], [5000, 700, 64], 8, 2, D, window=window, seed=39)
+    base.run(3, [4, 1, 0], [3000, 1100, 0], 8, 2, D, window=window, seed=40)
+    base.run(2, [40, 3], [3000, 1100], 4, 1, D, window=window, seed=41)
