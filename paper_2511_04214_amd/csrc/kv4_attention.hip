@@ -366,14 +366,15 @@ struct Share {
 // each, measured) but not another wavefront's.  So the two never mix: a page is a matrix phase (the last page's weights times its
 // values, this page's scores) and a vector phase (scores to weights, unpacking), and of the two groups one is in the one while the
 // other is in the other, a barrier between phases.  With the phases of a wavefront interleaved instruction by instruction instead,
-// and two independent workgroups on a CU, a prompt of 8192 tokens took 535 us, so 482 us.  For calls that fill the card with such tiles.
+// and two independent workgroups on a CU, a prompt of 8192 tokens took 535 us, so 482 us (1.14 PFLOP/s; the board's power bounds it).
 // kPair: 128 rows; the two groups take every other page of them, each with buffers of its own, and add their sums up at the end.
-// For calls that do not: a page after another costs a lone group 1.4 us, whatever the rest of the card does, and partial sums
-// through memory cost more than they save there (1024 tokens, 32 heads of 128: 28 us; one group 38 us, tall tiles 41 us).
+// For calls that tall tiles do not fill the card with: a page after another costs a lone group 1.4 us, whatever the rest of the card
+// does, and partial sums through memory cost more than they save there (1024 tokens, 32 heads of 128: 28 us; one group 38 us, tall
+// tiles 41 us).
 // kOne: 128 rows, one group, for contexts of a few pages, where a second one is only more to start (64 tokens: 8.3 us, 11.3 us paired).
 enum { kOne, kPair, kTall };
 template <int D, int MODE>
-__global__ __launch_bounds__(MODE == kOne ? 256 : 512, MODE != kOne && D == 64 ? 4 : 2) void k_attention_many(const AttnArgs a, int splits, float* part_o, float* part_ml) {
+__global__ __launch_bounds__(MODE == kOne ? 256 : 512, MODE == kPair && D == 64 ? 4 : 2) void k_attention_many(const AttnArgs a, int splits, float* part_o, float* part_ml) {
     constexpr int MT = D / 32, KS = D / 64, HB = kv4_head_bytes(D), ROW = 64 * 2 + 16, KROW = D * 2 + 16, TILE = MODE == kTall ? 256 : 128;
     constexpr bool PAIR = MODE == kPair, TALL = MODE == kTall;
     constexpr int BUFFERS = 2 * D * ROW + 2 * 64 * KROW;
@@ -781,10 +782,12 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 }
 
 // How a call is cut up.  Up to 16 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
-// pages.  More: one group for contexts of up to 6 pages (350 tokens, 32 heads: 15.2 us, 15.8 us paired; 512: 18.3 either way); tall
-// tiles where tiles of 128 rows would be more than the CUs take at once, one a CU or with heads of 64 two, of which half is enough
-// (6 chunks of up to 500 tokens over up to 4000, 32 heads of 128: 39 us, 54 us paired; 4 of up to 1000 over 2000, 16 heads of 64: 48 us,
-// 42 us paired); else pairs.
+// pages.  More: one group for contexts of up to 6 pages (350 tokens, 32 heads: 15.2 us, 15.8 us paired; 512: 18.3 either way).  Heads
+// of 64: pairs, whose four wavefronts a SIMD suit work that the vector units bound (8192 tokens, 16 heads: 172 us, tall tiles 189 us).
+// Heads of 128: pairs or tall tiles, whichever is through first by what was measured: a workgroup 8 us to start and end and 1.65 us a
+// page with tall tiles, 9 and 1.15 paired, one a CU; the whole takes its longest, or as many rounds of the mean as there are (32 heads,
+// pairs and tall tiles: 1500 tokens 40 and 46 us, 2048 58 and 61, 3000 110 and 90; 6 chunks of up to 500 over up to 4000 in a window of
+// 1024 54 and 38).
 // The pages are split, to no less than eight, where the tiles alone leave CUs idle; up to 16 of few rows never, which the join takes
 // longer for than they do (1000 tokens: 8.1 us, 8.9 us in halves; 1300 9.7 and 9.2).  Many rows: to one workgroup a CU at most, since
 // every split writes and reads its rows' sums in 32 bits (256 tokens over 8192, 32 heads: 57 us, to two a CU 66 us, whole 132 us).  Few:
@@ -796,13 +799,18 @@ struct Plan {
     int mode;                    // of the kernel for many rows
     int64_t tiles;               // of a head of the cache (few: one a sequence)
     int splits;
-    static Plan of(int64_t T, int64_t S, int Hk, int G, int D, int64_t max_q, int64_t max_kv, int window, int cus) {
+    static Plan of(int64_t T, int64_t S, int Hk, int G, int D, int64_t max_q, int64_t max_kv, bool causal, int window, int cus) {
         const bool few = max_q * G <= 16;
         // what a sequence's rows can see (a window makes parts fewer, never more: the workspace is sized without one)
         const int64_t seen = window ? std::min<int64_t>(max_kv, window + max_q + 2 * kKv4Page) : max_kv, pages = (seen + kKv4Page - 1) / kKv4Page;
         // tiles that a call of T rows can have, whatever the longest sequence's
         auto most = [&](int64_t rows) { return std::min(S * ((max_q * G + rows - 1) / rows), T * G / rows + S); };
-        const int mode = few || pages <= 6 ? kOne : Hk * most(128) > cus * (D == 64 ? 3 : 2) / 2 ? kTall : kPair;
+        // us of tiles of so many rows (a causal prompt's see half of it on average)
+        auto time = [&](int64_t rows, double start, double page) {
+            const double mean = causal && !window ? std::max(double(max_kv - max_q / 2) / kKv4Page, 1.0) : double(pages);
+            return std::max(start + page * double(pages), double((Hk * most(rows) + cus - 1) / cus) * (start + page * mean));
+        };
+        const int mode = few || pages <= 6 ? kOne : D == 128 && time(256, 8.0, 1.65) < time(128, 9.0, 1.15) ? kTall : kPair;
         const int64_t tiles = few ? S : most(mode == kTall ? 256 : 128), wgs = Hk * tiles;
         int64_t n = few ? (cus + wgs - 1) / wgs : mode == kPair ? cus / wgs : 1;
         if (few && S > 1) n = std::max(n, std::min((4 * cus + wgs - 1) / wgs, (pages + 16) / 32));
@@ -814,18 +822,19 @@ struct Plan {
 }  // namespace
 
 int64_t kv4_attention_workspace(int64_t T, int64_t S, int Hq, int Hk, int D, int64_t max_q, int64_t max_kv, int cus) {
-    const Plan p = Plan::of(T, S, Hk, Hq / Hk, D, max_q, max_kv, 0, cus);
+    const Plan p = Plan::of(T, S, Hk, Hq / Hk, D, max_q, max_kv, false, 0, cus);
     return p.splits == 1 ? 0 : T * Hq * p.splits * (D + 2) * 4;
 }
 
 template <int D>
 static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t stream) {
     const int Hq = a.Hk * a.G;
-    const Plan p = Plan::of(a.T, a.S, a.Hk, a.G, D, a.max_q, a.max_kv, a.causal ? a.window : 0, cus);
+    const Plan p = Plan::of(a.T, a.S, a.Hk, a.G, D, a.max_q, a.max_kv, a.causal, a.window, cus);
     float *po = p.splits == 1 ? nullptr : static_cast<float*>(a.workspace), *pm = po ? po + a.T * Hq * p.splits * D : nullptr;
     const dim3 grid((uint32_t)(p.tiles * a.Hk * p.splits));
-    if (p.few) hipLaunchKernelGGL((k_attention_few<D>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
-    else if (p.mode == kTall) hipLaunchKernelGGL((k_attention_many<D, kTall>), grid, dim3(512), 0, stream, a, 1, nullptr, nullptr);
+    if (p.mode == kTall) {
+        if constexpr (D == 128) hipLaunchKernelGGL((k_attention_many<D, kTall>), grid, dim3(512), 0, stream, a, 1, nullptr, nullptr);
+    } else if (p.few) hipLaunchKernelGGL((k_attention_few<D>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
     else if (p.mode == kPair) hipLaunchKernelGGL((k_attention_many<D, kPair>), grid, dim3(512), 0, stream, a, p.splits, po, pm);
     else hipLaunchKernelGGL((k_attention_many<D, kOne>), grid, dim3(256), 0, stream, a, 1, nullptr, nullptr);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;
