@@ -791,7 +791,8 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 // The pages are split, to no less than eight, where the tiles alone leave CUs idle; up to 16 of few rows never, which the join takes
 // longer for than they do (1000 tokens: 8.1 us, 8.9 us in halves; 1300 9.7 and 9.2).  Many rows: to one workgroup a CU at most, since
 // every split writes and reads its rows' sums in 32 bits (256 tokens over 8192, 32 heads: 57 us, to two a CU 66 us, whole 132 us).  Few:
-// to one a CU (one row of 131 072 tokens in a cache: 29 us, to two a CU 31 us), of several sequences to four if that leaves 32 pages to a
+// to one a CU at most (one row of 131 072 tokens in a cache: 29 us, to two a CU 31 us; 24 of up to 2000, 8 heads of the cache: 13.9 us whole,
+// 15.8 in halves), of several sequences to four if that leaves 32 pages to a
 // split, because the sequences' lengths differ and shorter parts even out (72 of up to 8192 tokens: 95 us, 106 us to one a CU; 64 of up
 // to 2000, which it leaves whole: 22 us, 27 us to four a CU).
 struct Plan {
@@ -812,7 +813,7 @@ struct Plan {
         };
         const int mode = few || pages <= 6 ? kOne : D == 128 && time(256, 8.0, 1.65) < time(128, 9.0, 1.15) ? kTall : kPair;
         const int64_t tiles = few ? S : most(mode == kTall ? 256 : 128), wgs = Hk * tiles;
-        int64_t n = few ? (cus + wgs - 1) / wgs : mode == kPair ? cus / wgs : 1;
+        int64_t n = few || mode == kPair ? cus / wgs : 1;
         if (few && S > 1) n = std::max(n, std::min((4 * cus + wgs - 1) / wgs, (pages + 16) / 32));
         n = few && pages <= 16 ? 1 : std::min(n, (pages + 7) / 8);
         return {few, mode, tiles, (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
