@@ -111,7 +111,7 @@ __device__ __forceinline__ float uniform_f32(float v) { return as_f32(__builtin_
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// ---- up to 16 query rows (tokens x heads of a group) against a range of pages: decoding
+// ---- up to 32 query rows (tokens x heads of a group) against a range of pages: decoding
 
 // A page of one head as a lane takes it: 4 subtiles of 16 tokens.
 template <int D>
@@ -124,11 +124,12 @@ struct PageRegs {
 
 // Workgroup: sequence, cache head, split.  Wavefront w goes through pages first + w, first + w + 4, ...
 // Bound by the cache's bytes: one row of 131 072 tokens, 143 MB, 26 us (5.4 TB/s); 100 of up to 8192, 609 MB, 115 us.  16 rows of the
-// matrix instruction take all heads of a group, so that a page is read once for them; each wavefront unpacks its own pages in
-// registers, the next one's loads under way.
+// matrix instruction, RT times, take all heads of a group, so that a page is read once for them; each wavefront unpacks its own pages in
+// registers, the next one's loads under way.  (17 to 32 rows here and not in tiles of 128: 8 sequences of 4 rows x 8 heads over up to
+// 4000 tokens 13.9 us, 21.8 us in tiles.)
 // (Registers for two workgroups a CU, so that a page can be on its way while one is worked on: for three, the batch of 100 below took
 // 132 us, not 128.)
-template <int D>
+template <int D, int RT>
 __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int splits, float* part_o, float* part_ml) {
     constexpr int MT = D / 16, HB = kv4_head_bytes(D);
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -138,16 +139,28 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     query_rows(a, s, &q0, &nq);
     if (nq == 0) return;
     const int rows = nq * a.G, len = a.kv_lens[s], all = min(len, min(a.max_kv, a.table_cols * kKv4Page));
-    // the tokens of this lane's row, and of any row
-    const int tok = n < rows ? n / a.G : 0, head = kvh * a.G + (n < rows ? n - tok * a.G : 0), p = len - (a.cu_q ? (int)(a.cu_q[s + 1] - a.cu_q[s]) : 1) + tok;
-    int end = all, begin = 0, end_any = all, begin_any = 0, end_all = all, begin_all = 0;
+    // the tokens of this lane's rows, of any row, of all
+    const int p0 = len - (a.cu_q ? (int)(a.cu_q[s + 1] - a.cu_q[s]) : 1), p1 = p0 + nq - 1;
+    int end[RT], begin[RT], end_any = all, begin_any = 0, end_all = all, begin_all = 0;
+    bf16x8 q[RT][D / 32];                                 // channels D/4 g + 8 j of the rows
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = rt * 16 + n, tok = r < rows ? r / a.G : 0, head = kvh * a.G + (r < rows ? r - tok * a.G : 0), p = p0 + tok;
+        end[rt] = a.causal ? min(all, p + 1) : all;
+        begin[rt] = a.causal && a.window ? max(0, p - a.window + 1) : 0;
+        const uint8_t* qp = a.q.p + (q0 + tok) * a.q.ts + head * a.q.hs;
+        const int flip = a.scale < 0.0f ? (int)0x80008000u : 0;
+        const v4i zero = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            const v4i x = *reinterpret_cast<const v4i*>(qp + (g * (D / 4) + k * 8) * 2) ^ flip;
+            q[rt][k] = __builtin_bit_cast(bf16x8, r < rows ? x : zero);
+        }
+    }
     if (a.causal) {
-        const int p0 = p - tok, p1 = p0 + nq - 1;
-        end = min(all, p + 1);
         end_any = min(all, p1 + 1);
         end_all = min(all, p0 + 1);
         if (a.window) {
-            begin = max(0, p - a.window + 1);
             begin_any = max(0, p0 - a.window + 1);
             begin_all = max(0, p1 - a.window + 1);
         }
@@ -159,24 +172,17 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     int page0, page1;
     split_pages(begin_any / kKv4Page, (max(end_any, 0) + kKv4Page - 1) / kKv4Page, split, splits, 4, &page0, &page1);
 
-    // queries: channels D/4 g + 8 j of the lane's row
-    bf16x8 q[D / 32];
-    {
-        const uint8_t* qp = a.q.p + (q0 + tok) * a.q.ts + head * a.q.hs;
-        const int flip = a.scale < 0.0f ? (int)0x80008000u : 0;
-        const v4i zero = {0, 0, 0, 0};
-#pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            const v4i x = *reinterpret_cast<const v4i*>(qp + (g * (D / 4) + k * 8) * 2) ^ flip;
-            q[k] = __builtin_bit_cast(bf16x8, n < rows ? x : zero);
-        }
-    }
     const float c = uniform_f32(fmaxf(fabsf(a.scale) * kLog2e, 1e-30f));
 
-    v4f o[MT];
+    v4f o[RT][MT];
+    float l[RT], ref[RT], top_ref[RT];                    // ref: what is subtracted; top_ref: the same, -inf before any token
 #pragma unroll
-    for (int j = 0; j < MT; ++j) o[j] = v4f{0, 0, 0, 0};
-    float l = 0.0f, ref = 0.0f, top_ref = -INFINITY;      // ref: what is subtracted; top_ref: the same, -inf before any token
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int j = 0; j < MT; ++j) o[rt][j] = v4f{0, 0, 0, 0};
+        l[rt] = ref[rt] = 0.0f;
+        top_ref[rt] = -INFINITY;
+    }
 
     const int32_t* row = a.table + (int64_t)s * a.table_cols;
     auto fetch = [&](PageRegs<D>& r, int number) {
@@ -190,22 +196,28 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     };
     auto use = [&](PageRegs<D>& r, int page) {
         const int t0 = page * kKv4Page;
-        v4f x[4];
+        v4f x[RT][4];
         static_for([&](auto iu) {
             constexpr int u = decltype(iu)::value;
-            x[u] = v4f{0, 0, 0, 0};
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k)
-                x[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_values(r.k[u][k], scale_of<u>(r.ks)), q[k], x[u], 0, 0, 0);
+            for (int rt = 0; rt < RT; ++rt) x[rt][u] = v4f{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                const bf16x8 keys = eight_values(r.k[u][k], scale_of<u>(r.ks));
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) x[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(keys, q[rt][k], x[rt][u], 0, 0, 0);
+            }
         }, IC<4>{});
         if (t0 < begin_all || t0 + kKv4Page > end_all) {               // some row does not see some token
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = t0 + u * 16 + g * 4 + i;
-                    x[u][i] = t >= begin && t < end ? x[u][i] : -INFINITY;
-                }
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = t0 + u * 16 + g * 4 + i;
+                        x[rt][u][i] = t >= begin[rt] && t < end[rt] ? x[rt][u][i] : -INFINITY;
+                    }
             if (t0 + kKv4Page > all) {                                 // tokens that are none: whatever their scales say, 0 times them is to be 0
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
@@ -214,32 +226,35 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
                 }
             }
         }
-        float top = -INFINITY;
+        bf16x8 pw[RT][2];
+        static_for([&](auto irt) {
+            constexpr int rt = decltype(irt)::value;
+            float top = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) top = fmaxf(fmaxf(fmaxf(top, x[u][0]), fmaxf(x[u][1], x[u][2])), x[u][3]);
-        top *= c;
-        if (__any(top > top_ref + 8.0f)) {       // weights stay below 2^8 without a new reference
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(top, top_ref), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top_ref - now);
-            top_ref = now;
-            ref = now == -INFINITY ? 0.0f : now;
-            l *= f;
+            for (int u = 0; u < 4; ++u) top = fmaxf(fmaxf(fmaxf(top, x[rt][u][0]), fmaxf(x[rt][u][1], x[rt][u][2])), x[rt][u][3]);
+            top *= c;
+            if (__any(top > top_ref[rt] + 8.0f)) {       // weights stay below 2^8 without a new reference
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float now = fmaxf(top, top_ref[rt]), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top_ref[rt] - now);
+                top_ref[rt] = now;
+                ref[rt] = now == -INFINITY ? 0.0f : now;
+                l[rt] *= f;
 #pragma unroll
-            for (int j = 0; j < MT; ++j) o[j] *= f;
-        }
-        bf16x8 pw[2];
+                for (int j = 0; j < MT; ++j) o[rt][j] *= f;
+            }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            float e[4];
+            for (int u = 0; u < 4; ++u) {
+                float e[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][i], c, -ref));
-            l += (e[0] + e[1]) + (e[2] + e[3]);
-            const uint32_t w0 = pack_bf16x2(e[0], e[1]), w1 = pack_bf16x2(e[2], e[3]);
-            v4i& d = reinterpret_cast<v4i&>(pw[u >> 1]);
-            d[(u & 1) * 2] = (int)w0;
-            d[(u & 1) * 2 + 1] = (int)w1;
-        }
+                for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][u][i], c, -ref[rt]));
+                l[rt] += (e[0] + e[1]) + (e[2] + e[3]);
+                const uint32_t w0 = pack_bf16x2(e[0], e[1]), w1 = pack_bf16x2(e[2], e[3]);
+                v4i& d = reinterpret_cast<v4i&>(pw[rt][u >> 1]);
+                d[(u & 1) * 2] = (int)w0;
+                d[(u & 1) * 2 + 1] = (int)w1;
+            }
+        }, IC<RT>{});
         static_for([&](auto ih) {                // tokens 32 h ... 32 h + 31: subtiles 2 h and 2 h + 1
             constexpr int h = decltype(ih)::value;
             uint32_t sc[2][4];
@@ -274,8 +289,11 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
                         even[u * 2 + i] = (int)__builtin_amdgcn_perm(y[u][2 * i + 1], y[u][2 * i], 0x05040100u);
                         odd[u * 2 + i] = (int)__builtin_amdgcn_perm(y[u][2 * i + 1], y[u][2 * i], 0x07060302u);
                     }
-                o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pw[h], o[2 * b], 0, 0, 0);
-                o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pw[h], o[2 * b + 1], 0, 0, 0);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    o[rt][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pw[rt][h], o[rt][2 * b], 0, 0, 0);
+                    o[rt][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pw[rt][h], o[rt][2 * b + 1], 0, 0, 0);
+                }
             }, IC<D / 32>{});
         }, IC<2>{});
     };
@@ -306,23 +324,30 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     }
 
     // the four wavefronts' sums, brought to one reference, added up
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    __shared__ float so[4][16][D + 4], sm[4][16], sl[4][16];
-    if (g == 0) {
-        sm[w][n] = top_ref;
-        sl[w][n] = l;
+    __shared__ float so[4][16 * RT][D + 4], sm[4][16 * RT], sl[4][16 * RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += __shfl_xor(l[rt], 16);
+        l[rt] += __shfl_xor(l[rt], 32);
+        if (g == 0) {
+            sm[w][rt * 16 + n] = top_ref[rt];
+            sl[w][rt * 16 + n] = l[rt];
+        }
     }
     __syncthreads();
-    float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i][n]);
-    const float f = top_ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top_ref - top);
-    if (n < rows) {
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = rt * 16 + n;
+        float top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i][r]);
+        const float f = top_ref[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top_ref[rt] - top);
+        if (r < rows) {
 #pragma unroll
-            for (int j = 0; j < MT; ++j) so[w][n][(g * 4 + i) * MT + j] = o[j][i] * f;
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) so[w][r][(g * 4 + i) * MT + j] = o[rt][j][i] * f;
+        }
     }
     __syncthreads();
     for (int e = (int)threadIdx.x; e < rows * (D / 4); e += 256) {
@@ -781,7 +806,7 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
     if (a.lse && d == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (m + __log2f(sum)) * kLn2;
 }
 
-// How a call is cut up.  Up to 16 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
+// How a call is cut up.  Up to 32 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
 // pages.  More: one group for contexts of up to 6 pages (350 tokens, 32 heads: 15.2 us, 15.8 us paired; 512: 18.3 either way).  Heads
 // of 64: pairs, whose four wavefronts a SIMD suit work that the vector units bound (8192 tokens, 16 heads: 172 us, tall tiles 189 us).
 // Heads of 128: pairs or tall tiles, whichever is through first by what was measured: a workgroup 8 us to start and end and 1.65 us a
@@ -801,7 +826,7 @@ struct Plan {
     int64_t tiles;               // of a head of the cache (few: one a sequence)
     int splits;
     static Plan of(int64_t T, int64_t S, int Hk, int G, int D, int64_t max_q, int64_t max_kv, bool causal, int window, int cus) {
-        const bool few = max_q * G <= 16;
+        const bool few = max_q * G <= 32;
         // what a sequence's rows can see (a window makes parts fewer, never more: the workspace is sized without one)
         const int64_t seen = window ? std::min<int64_t>(max_kv, window + max_q + 2 * kKv4Page) : max_kv, pages = (seen + kKv4Page - 1) / kKv4Page;
         // tiles that a call of T rows can have, whatever the longest sequence's
@@ -835,7 +860,8 @@ static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t strea
     const dim3 grid((uint32_t)(p.tiles * a.Hk * p.splits));
     if (p.mode == kTall) {
         if constexpr (D == 128) hipLaunchKernelGGL((k_attention_many<D, kTall>), grid, dim3(512), 0, stream, a, 1, nullptr, nullptr);
-    } else if (p.few) hipLaunchKernelGGL((k_attention_few<D>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
+    } else if (p.few && a.max_q * a.G > 16) hipLaunchKernelGGL((k_attention_few<D, 2>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
+    else if (p.few) hipLaunchKernelGGL((k_attention_few<D, 1>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
     else if (p.mode == kPair) hipLaunchKernelGGL((k_attention_many<D, kPair>), grid, dim3(512), 0, stream, a, p.splits, po, pm);
     else hipLaunchKernelGGL((k_attention_many<D, kOne>), grid, dim3(256), 0, stream, a, 1, nullptr, nullptr);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;

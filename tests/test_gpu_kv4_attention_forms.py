@@ -137,3 +137,32 @@ def test_windows_in_long_contexts(D, window):
     base.run(3, [1, 1, 1], [5000, 700, 64], 8, 2, D, window=window, seed=39)
     base.run(3, [4, 1, 0], [3000, 1100, 0], 8, 2, D, window=window, seed=40)
     base.run(2, [40, 3], [3000, 1100], 4, 1, D, window=window, seed=41)
+
+
+@pytest.mark.parametrize("q,G", [(1, 17), (1, 32), (4, 8), (31, 1), (32, 1), (2, 16), (5, 6), (3, 8)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_two_tiles_of_16_rows(D, q, G):
+    """17 to 32 rows of a sequence; sequences with fewer, none, more than tokens; whole and in parts; in windows."""
+    qs = [q, max(q - 1, 0), 1, 0, q, q, q, q]
+    lens = [700, 65, 1, 30, max(q - 3, 0), 64, 0, 1800]
+    base.run(8, qs, lens, 2 * G, 2, D, seed=42, sharp=2.0)
+    base.run(8, qs, lens, 2 * G, 2, D, seed=43, window=100)
+    base.run(8, qs, lens, 2 * G, 2, D, seed=44, causal=False, max_kv=1000)
+
+
+@pytest.mark.parametrize("q,n", [(4, 200), (3, 3000)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_nan_in_one_of_32_rows(D, q, n):
+    g = torch.Generator().manual_seed(45)
+    pool = base.cache(g, 50, 1, D)
+    table = torch.randint(0, 50, (2, -(-n // 64)), generator=g).to(torch.int32)
+    x = torch.randn((2 * q, 8, D), generator=g).to(torch.bfloat16)
+    a = (pool.cuda(), table.cuda(), torch.full((2,), n, dtype=torch.int32).cuda())
+    kw = dict(cu_q=torch.tensor([0, q, 2 * q], dtype=torch.int32).cuda(), max_q=q, want_lse=True)
+    out, lse = brq.kv4_attention(x.cuda(), *a, **kw)
+    x[q - 1, 3, 7] = math.nan
+    got, l2 = brq.kv4_attention(x.cuda(), *a, **kw)
+    assert torch.isnan(got[q - 1, 3]).all() and torch.isnan(l2[q - 1, 3])
+    keep = torch.ones((2 * q, 8), dtype=torch.bool, device="cuda")
+    keep[q - 1, 3] = False
+    assert torch.equal(got[keep], out[keep]) and torch.equal(l2[keep], lse[keep])
