@@ -122,6 +122,34 @@ struct PageRegs {
     v4i vs;                      // byte i of element u: scale of token 16 u + 4 g + i
 };
 
+// The sequence that is number r by its pages, the longest first: the largest count that more than r sequences have is found bit by bit.
+// `top`: the highest bit of a count.  S <= 256.
+__device__ __forceinline__ int by_length(const AttnArgs& a, int r, int top) {
+    const int lane = (int)threadIdx.x & 63, most = min(a.max_kv, a.table_cols * kKv4Page);
+    int pages[4], v = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int s = i * 64 + lane;
+        pages[i] = s < a.S ? (min(max(a.kv_lens[s], 0), most) + kKv4Page - 1) / kKv4Page : -1;
+    }
+    for (int bit = top; bit > 0; bit >>= 1) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += __popcll(__ballot(pages[i] >= (v | bit)));
+        if (n > r) v |= bit;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r -= __popcll(__ballot(pages[i] > v));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t m = __ballot(pages[i] == v);
+        const int n = __popcll(m);
+        if (r < n) return i * 64 + __builtin_ctzll(__ballot((m >> lane & 1) != 0 && __popcll(m & ((1ull << lane) - 1)) == r));
+        r -= n;
+    }
+    return 0;
+}
+
 // Workgroup: sequence, cache head, split.  Wavefront w goes through pages first + w, first + w + 4, ...
 // Bound by the cache's bytes: one row of 131 072 tokens, 143 MB, 26 us (5.4 TB/s); 100 of up to 8192, 609 MB, 115 us.  16 rows of the
 // matrix instruction, RT times, take all heads of a group, so that a page is read once for them; each wavefront unpacks its own pages in
@@ -130,10 +158,11 @@ struct PageRegs {
 // (Registers for two workgroups a CU, so that a page can be on its way while one is worked on: for three, the batch of 100 below took
 // 132 us, not 128.)
 template <int D, int RT>
-__global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int splits, float* part_o, float* part_ml) {
+__global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int splits, int order, float* part_o, float* part_ml) {
     constexpr int MT = D / 16, HB = kv4_head_bytes(D);
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-    const int split = (int)blockIdx.x % splits, sh = (int)blockIdx.x / splits, s = sh / a.Hk, kvh = sh - s * a.Hk;
+    const int split = (int)blockIdx.x % splits, sh = (int)blockIdx.x / splits, number = sh / a.Hk, kvh = sh - number * a.Hk;
+    const int s = order ? by_length(a, number, order) : number;
     int64_t q0;
     int nq;
     query_rows(a, s, &q0, &nq);
@@ -818,7 +847,7 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 // every split writes and reads its rows' sums in 32 bits (256 tokens over 8192, 32 heads: 57 us, to two a CU 66 us, whole 132 us).  Few:
 // to one a CU at most (one row of 131 072 tokens in a cache: 29 us, to two a CU 31 us; 24 of up to 2000, 8 heads of the cache: 13.9 us whole,
 // 15.8 in halves), of several sequences to four if that leaves 32 pages to a
-// split, because the sequences' lengths differ and shorter parts even out (72 of up to 8192 tokens: 95 us, 106 us to one a CU; 64 of up
+// split, because the sequences' lengths differ and shorter parts even out (72 of up to 8192 tokens: 93 us, 106 us to one a CU; 64 of up
 // to 2000, which it leaves whole: 22 us, 27 us to four a CU).
 struct Plan {
     bool few;
@@ -858,10 +887,15 @@ static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t strea
     const Plan p = Plan::of(a.T, a.S, a.Hk, a.G, D, a.max_q, a.max_kv, a.causal, a.window, cus);
     float *po = p.splits == 1 ? nullptr : static_cast<float*>(a.workspace), *pm = po ? po + a.T * Hq * p.splits * D : nullptr;
     const dim3 grid((uint32_t)(p.tiles * a.Hk * p.splits));
+    const int pages = (std::min(a.max_kv, a.table_cols * kKv4Page) + kKv4Page - 1) / kKv4Page;
+    // more workgroups than there is room for: the longest sequences first, so that no long one is left at the end (100 of up to 8192 tokens:
+    // 118 us, 122 us as they come; from 48 pages on, since it takes a workgroup 0.5 us to know: 100 of up to 2000 32 us, 31 us as they come)
+    const bool sorted = p.few && a.S > 1 && a.S <= 256 && !a.window && pages >= 48 && (int64_t)a.S * a.Hk * p.splits > 2 * cus;
+    const int order = sorted ? 1 << (31 - __builtin_clz(pages)) : 0;
     if (p.mode == kTall) {
         if constexpr (D == 128) hipLaunchKernelGGL((k_attention_many<D, kTall>), grid, dim3(512), 0, stream, a, 1, nullptr, nullptr);
-    } else if (p.few && a.max_q * a.G > 16) hipLaunchKernelGGL((k_attention_few<D, 2>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
-    else if (p.few) hipLaunchKernelGGL((k_attention_few<D, 1>), grid, dim3(256), 0, stream, a, p.splits, po, pm);
+    } else if (p.few && a.max_q * a.G > 16) hipLaunchKernelGGL((k_attention_few<D, 2>), grid, dim3(256), 0, stream, a, p.splits, order, po, pm);
+    else if (p.few) hipLaunchKernelGGL((k_attention_few<D, 1>), grid, dim3(256), 0, stream, a, p.splits, order, po, pm);
     else if (p.mode == kPair) hipLaunchKernelGGL((k_attention_many<D, kPair>), grid, dim3(512), 0, stream, a, p.splits, po, pm);
     else hipLaunchKernelGGL((k_attention_many<D, kOne>), grid, dim3(256), 0, stream, a, 1, nullptr, nullptr);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;

@@ -166,3 +166,14 @@ def test_a_nan_in_one_of_32_rows(D, q, n):
     keep = torch.ones((2 * q, 8), dtype=torch.bool, device="cuda")
     keep[q - 1, 3] = False
     assert torch.equal(got[keep], out[keep]) and torch.equal(l2[keep], lse[keep])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("S,q,Hk", [(70, 1, 8), (256, 1, 3), (100, 3, 8), (257, 1, 3), (65, 1, 16)])
+def test_the_longest_sequences_first(S, q, Hk, D):
+    """More sequences than fit at once, in the order of their lengths: equal lengths, none, less than none, more than the table has."""
+    g = torch.Generator().manual_seed(46)
+    lens = torch.randint(1, 200, (S,), generator=g).tolist()
+    lens[:8] = [0, 3100, 64, 64, 64, 65, 63, 1]
+    lens[10:14] = [-5, 3100, 3099, 128]
+    base.run(S, [q] * S, lens, 2 * Hk if q == 1 else Hk, Hk, D, seed=47, max_kv=3500)
