@@ -842,9 +842,11 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 // page with tall tiles, 9 and 1.15 paired, one a CU; the whole takes its longest, or as many rounds of the mean as there are (32 heads,
 // pairs and tall tiles: 1500 tokens 40 and 46 us, 2048 58 and 61, 3000 110 and 90; 6 chunks of up to 500 over up to 4000 in a window of
 // 1024 54 and 38).
-// The pages are split, to no less than eight, where the tiles alone leave CUs idle; up to 16 of few rows never, which the join takes
-// longer for than they do (1000 tokens: 8.1 us, 8.9 us in halves; 1300 9.7 and 9.2).  Many rows: to one workgroup a CU at most, since
-// every split writes and reads its rows' sums in 32 bits (256 tokens over 8192, 32 heads: 57 us, to two a CU 66 us, whole 132 us).  Few:
+// The pages are split where the tiles alone leave CUs idle, except so few that joining takes longer than they do.  Few rows: more than
+// 16, to no less than 8 (1000 tokens: 8.1 us, 8.9 us in halves; 1300 9.7 and 9.2).  Many: more than 8, to no less than 4 (64 tokens over
+// 1500, 8 heads on 2 of 128: 17.5 us, 21.0 us to no less than 8; 500 over 500, 32 heads: 18 us, 28 us in halves), and to one workgroup a
+// CU at most, since every split writes and reads its rows' sums in 32 bits (256 tokens over 8192, 32 heads: 57 us, to two a CU 66 us, whole
+// 132 us).  Few:
 // to one a CU at most (one row of 131 072 tokens in a cache: 29 us, to two a CU 31 us; 24 of up to 2000, 8 heads of the cache: 13.9 us whole,
 // 15.8 in halves), of several sequences to four if that leaves 32 pages to a
 // split, because the sequences' lengths differ and shorter parts even out (72 of up to 8192 tokens: 93 us, 106 us to one a CU; 64 of up
@@ -869,7 +871,7 @@ struct Plan {
         const int64_t tiles = few ? S : most(mode == kTall ? 256 : 128), wgs = Hk * tiles;
         int64_t n = few || mode == kPair ? cus / wgs : 1;
         if (few && S > 1) n = std::max(n, std::min((4 * cus + wgs - 1) / wgs, (pages + 16) / 32));
-        n = few && pages <= 16 ? 1 : std::min(n, (pages + 7) / 8);
+        n = pages <= (few ? 16 : 8) ? 1 : std::min(n, few ? (pages + 7) / 8 : (pages + 3) / 4);
         return {few, mode, tiles, (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
     }
 };
