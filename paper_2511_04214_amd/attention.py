@@ -267,10 +267,6 @@ def kv4_attention(q, pool, table, kv_lens, scale=None, causal=True, window=0, cu
     table int32 [S, columns], kv_lens int32 [S]; cu_q int32 [S + 1] says which rows are whose (None: one row a sequence,
     T = S).  max_q: the longest sequence's rows (None: 1 without cu_q, else T); max_kv: the longest context (None: what the
     table has room for).  scale: None for D ** -0.5.  Returns out, or (out, lse) where lse is given or wanted."""
-    if q.dim() == 3 and table.dim() == 2:
-        max_q = (1 if cu_q is None else max(1, q.shape[0])) if max_q is None else max_q
-        max_kv = table.shape[1] * KV4_PAGE if max_kv is None else max_kv
-        scale = q.shape[2] ** -0.5 if scale is None and q.shape[2] else scale
     r = _native("kv4_attention", stream, q, pool, table, kv_lens, scale, causal, window, cu_q, max_q, max_kv, out, lse, want_lse, workspace)
     if r is not None:
         return r
@@ -285,7 +281,10 @@ def kv4_attention(q, pool, table, kv_lens, scale=None, causal=True, window=0, cu
     pl, pc = _array(kv_lens, "kv_lens", torch.int32, (S,)), _array(cu_q, "cu_q", torch.int32, (S + 1,), True)
     if cu_q is None and T != S:
         raise ValueError("cu_q must be given where the number of rows is not that of the sequences")
+    max_q = (1 if cu_q is None else max(1, T)) if max_q is None else max_q
+    max_kv = cols * KV4_PAGE if max_kv is None else max_kv
     need = kv4_attention_workspace(T, S, Hq, Hk, D, max_q, max_kv)
+    scale = D ** -0.5 if scale is None else scale
     with _on(stream):
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
         if lse is None and want_lse:

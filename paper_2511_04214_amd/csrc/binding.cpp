@@ -8,6 +8,9 @@
 // as it always did.  Otherwise a call returns the library's status, 0 or not, or the result tensor.
 #include <Python.h>
 
+#include <algorithm>
+#include <cmath>
+
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/_foreach_zero.h>
 #include <ATen/ops/empty.h>
@@ -676,20 +679,24 @@ PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// kv4_attention(q, pool, table, kv_lens, scale, causal, window, cu_q, max_q, max_kv, out, lse, want_lse, workspace)
+// kv4_attention(q, pool, table, kv_lens, scale, causal, window, cu_q, max_q, max_kv, out, lse, want_lse, workspace); scale, max_q and max_kv may be None
 PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     Call c;
     HeadSet q, out;
     at::Tensor pool, table, lens, cu, lse, space;
     double scale = 0.0;
-    int64_t Hk = -1, window, max_q, max_kv, need = 0;
+    int64_t Hk = -1, window, max_q = 0, max_kv = 0, need = 0;
     if (n != 14 || !g_attention || !quiet() || !head_set(c, a[0], &q) || q.dt != BRQ_BF16 || !cache(c, a[1], q.D, &Hk, &pool) || !array_of(c, a[2], at::kInt, {-1, -1}, &table) ||
         !array_of(c, a[3], at::kInt, {table.size(0)}, &lens) || !array_of(c, a[7], at::kInt, {table.size(0) + 1}, &cu, true) || (!cu.defined() && q.T != table.size(0)) ||
-        !number(a[4], &scale) || !PyBool_Check(a[5]) || !integer(a[6], &window) || !integer(a[8], &max_q) || !integer(a[9], &max_kv) ||
+        (a[4] != Py_None && !number(a[4], &scale)) || !PyBool_Check(a[5]) || !integer(a[6], &window) || (a[8] != Py_None && !integer(a[8], &max_q)) ||
+        (a[9] != Py_None && !integer(a[9], &max_kv)) ||
         !head_out(c, a[10], q, at::kBFloat16, &out) || !array_of(c, a[11], at::kFloat, {q.T, q.h.heads}, &lse, true) || !PyBool_Check(a[12]) ||
         !array_of(c, a[13], at::kByte, {-1}, &space, true)) Py_RETURN_NONE;
     const int64_t S = table.size(0);
+    if (a[4] == Py_None) scale = 1.0 / std::sqrt((double)q.D);
+    if (a[8] == Py_None) max_q = cu.defined() ? std::max<int64_t>(1, q.T) : 1;
+    if (a[9] == Py_None) max_kv = table.size(1) * BRQ_KV4_PAGE;
     if (const brq_status r = f_attention_space(q.T, S, q.h.heads, Hk, q.D, max_q, max_kv, &need); r != BRQ_OK) return status(r);
     if (!make_heads(c, q, at::kBFloat16, &out) || (a[12] == Py_True && !make(c, {q.T, q.h.heads}, at::kFloat, &lse)) || (need && !make(c, {need}, at::kByte, &space))) Py_RETURN_NONE;
     void* st = current_stream();
