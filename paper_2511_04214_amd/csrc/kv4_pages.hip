@@ -1,7 +1,8 @@
 // Pages of the MXFP4 cache: copied, shared, given up, reserved and made dense, on the device (include/brq_attn.h).
 //
 // What moves pages is bound by HBM; what finds them (counts of free and live pages in page order, so that results do not
-// depend on the schedule) is one workgroup that goes through the counts 16 at a time and thread, 16384 a step.
+// depend on the schedule) is one workgroup that goes through the counts, 16 a thread and step, 16384 a step; of caches of up to 4096 pages 4 a
+// thread, in one step (a compaction of 96 sequences' pages 36.2 -> 34.0 us).
 #include "brq_attn.h"
 #include "brq_device.h"
 #include "brq_launch.h"
@@ -10,7 +11,7 @@ namespace brq {
 namespace {
 
 constexpr int kScan = 1024;       // threads of the workgroup that counts
-constexpr int kPer = 16;          // page counts a thread and step
+constexpr int kSmall = kScan * 4; // pages of a cache whose counts are taken 4 a thread, 16 otherwise
 
 // Sum of v over the workgroup's threads in front of this one; *total: over all.  T: an integer, or two counts in one.
 template <class T>
@@ -36,17 +37,18 @@ __device__ __forceinline__ T scan_before(T v, T* lds, T* total) {
     return before + x - v;
 }
 
-// The counts of 16 pages of a thread: -1 past the end.
-__device__ __forceinline__ void load_refs(const int32_t* refs, int n, int at, int (&r)[kPer]) {
-    if (at + kPer <= n && (reinterpret_cast<uintptr_t>(refs) & 15u) == 0) {
+// The counts of a thread's pages: -1 past the end.
+template <int PER>
+__device__ __forceinline__ void load_refs(const int32_t* refs, int n, int at, int (&r)[PER]) {
+    if (at + PER <= n && (reinterpret_cast<uintptr_t>(refs) & 15u) == 0) {
 #pragma unroll
-        for (int i = 0; i < kPer; i += 4) {
+        for (int i = 0; i < PER; i += 4) {
             const v4i v = *reinterpret_cast<const v4i*>(refs + at + i);
             r[i] = v.x; r[i + 1] = v.y; r[i + 2] = v.z; r[i + 3] = v.w;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) r[i] = at + i < n ? refs[at + i] : -1;
+        for (int i = 0; i < PER; ++i) r[i] = at + i < n ? refs[at + i] : -1;
     }
 }
 
@@ -131,17 +133,18 @@ struct Row {
 };
 
 // The first `want` free pages, lowest first, by a workgroup; r: the thread's counts, of the first step already there.  Returns how many.
-__device__ __forceinline__ int find_free(const PagesArgs& a, int32_t* pages, int want, int (&r)[kPer], int* lds) {
+template <int PER>
+__device__ __forceinline__ int find_free(const PagesArgs& a, int32_t* pages, int want, int (&r)[PER], int* lds) {
     int found = 0, total;
-    for (int at = 0; at < a.num_pages && found < want; at += kScan * kPer) {
+    for (int at = 0; at < a.num_pages && found < want; at += kScan * PER) {
         int n = 0;
-        const int mine = at + (int)threadIdx.x * kPer;
+        const int mine = at + (int)threadIdx.x * PER;
         if (at > 0) load_refs(a.refs, a.num_pages, mine, r);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) n += r[i] == 0;
+        for (int i = 0; i < PER; ++i) n += r[i] == 0;
         int rank = found + scan_before(n, lds, &total);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
+        for (int i = 0; i < PER; ++i)
             if (r[i] == 0) {
                 if (rank < want) pages[rank] = mine + i;
                 ++rank;
@@ -151,12 +154,12 @@ __device__ __forceinline__ int find_free(const PagesArgs& a, int32_t* pages, int
     return min(found, want);
 }
 
-template <bool FORK>
+template <bool FORK, int PER>
 __global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
     __shared__ int lds[17];
     const Found f(a.workspace, a.n);
-    int want = 0, total, r[kPer];
-    load_refs(a.refs, a.num_pages, (int)threadIdx.x * kPer, r);                   // (on their way while the wants are counted)
+    int want = 0, total, r[PER];
+    load_refs(a.refs, a.num_pages, (int)threadIdx.x * PER, r);                   // (on their way while the wants are counted)
     for (int i0 = 0; i0 < a.n; i0 += kScan) {
         const int i = i0 + (int)threadIdx.x, w = i < a.n ? wanted<FORK>(a, i) : 0;
         const int before = scan_before(w, lds, &total);
@@ -170,14 +173,15 @@ __global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
     }
 }
 
-// Reservations of up to 64 sequences in one launch, 16 lanes a row: 48 of 1000 tokens each 5.5 us; with a lane a row to count and a
+// Reservations of up to 64 sequences in one launch, 16 lanes a row: 48 of 1000 tokens each 4.4 us; with a lane a row to count and a
 // wavefront a row to fill, a launch apart or not, 8.4 us.
+template <int PER>
 __global__ __launch_bounds__(kScan) void k_reserve_few(const PagesArgs a) {
     __shared__ int lds[17];
     const Found f(a.workspace, a.n);
     const int lane = (int)threadIdx.x & 15;
-    int total, r[kPer];
-    load_refs(a.refs, a.num_pages, (int)threadIdx.x * kPer, r);
+    int total, r[PER];
+    load_refs(a.refs, a.num_pages, (int)threadIdx.x * PER, r);
     Row<16> row(a, (int)threadIdx.x >> 4, lane);
     if (threadIdx.x == 0) a.result[0] = 0;
     const int first = __shfl(scan_before(lane == 0 ? row.need : 0, lds, &total), (int)threadIdx.x & 48);
@@ -251,17 +255,18 @@ struct Moves {
     __host__ __device__ Moves(int32_t* w, int n) : count(w), from(w + 4), to(w + 4 + n / 2 + 1), rank(w + 4 + 2 * (n / 2 + 1)) {}
 };
 
+template <int PER>
 __global__ __launch_bounds__(kScan) void k_plan_moves(const PagesArgs a) {
     __shared__ int lds[17];
     __shared__ uint64_t lds2[17];
     const Moves v(a.workspace, a.num_pages);
-    constexpr int kStep = kScan * kPer;
-    int live = 0, total, r[kPer];
+    constexpr int kStep = kScan * PER;
+    int live = 0, total, r[PER];
     for (int at = 0; at < a.num_pages; at += kStep) {
         int n = 0;
-        load_refs(a.refs, a.num_pages, at + (int)threadIdx.x * kPer, r);
+        load_refs(a.refs, a.num_pages, at + (int)threadIdx.x * PER, r);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) n += r[i] > 0;
+        for (int i = 0; i < PER; ++i) n += r[i] > 0;
         scan_before(n, lds, &total);
         live += total;
     }
@@ -269,10 +274,10 @@ __global__ __launch_bounds__(kScan) void k_plan_moves(const PagesArgs a) {
     int holes = 0, high = 0;
     for (int at = 0; at < a.num_pages; at += kStep) {
         uint32_t nh = 0, ns = 0;
-        const int mine = at + (int)threadIdx.x * kPer;
+        const int mine = at + (int)threadIdx.x * PER;
         if (a.num_pages > kStep) load_refs(a.refs, a.num_pages, mine, r);         // (otherwise they are still there)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
+        for (int i = 0; i < PER; ++i) {
             nh += r[i] <= 0 && mine + i < live;
             ns += r[i] > 0 && mine + i >= live;
         }
@@ -280,7 +285,7 @@ __global__ __launch_bounds__(kScan) void k_plan_moves(const PagesArgs a) {
         const uint64_t before = scan_before((uint64_t)ns << 32 | nh, lds2, &both);
         int hole = holes + (int)(uint32_t)before, src = high + (int)(before >> 32);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
+        for (int i = 0; i < PER; ++i) {
             if (mine + i < live) {
                 if (r[i] <= 0) v.to[hole++] = mine + i;
             } else if (mine + i < a.num_pages) {
@@ -334,7 +339,8 @@ hipError_t launch_pages_copy(const PagesArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((k_find_free<true>), dim3(1), dim3(kScan), 0, stream, a);
+    if (a.num_pages <= kSmall) hipLaunchKernelGGL((k_find_free<true, 4>), dim3(1), dim3(kScan), 0, stream, a);
+    else hipLaunchKernelGGL((k_find_free<true, 16>), dim3(1), dim3(kScan), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (a.n == 0) return hipSuccess;
     const int parts = parts_of(a.page_bytes, a.n);
@@ -349,17 +355,20 @@ hipError_t launch_pages_free(const PagesArgs& a, hipStream_t stream) {
 
 hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream) {
     if (a.n <= 64) {
-        hipLaunchKernelGGL(k_reserve_few, dim3(1), dim3(kScan), 0, stream, a);
+        if (a.num_pages <= kSmall) hipLaunchKernelGGL((k_reserve_few<4>), dim3(1), dim3(kScan), 0, stream, a);
+        else hipLaunchKernelGGL((k_reserve_few<16>), dim3(1), dim3(kScan), 0, stream, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((k_find_free<false>), dim3(1), dim3(kScan), 0, stream, a);
+    if (a.num_pages <= kSmall) hipLaunchKernelGGL((k_find_free<false, 4>), dim3(1), dim3(kScan), 0, stream, a);
+    else hipLaunchKernelGGL((k_find_free<false, 16>), dim3(1), dim3(kScan), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(k_reserve, dim3((uint32_t)a.n), dim3(64), 0, stream, a);
     return hipGetLastError();
 }
 
 hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL(k_plan_moves, dim3(1), dim3(kScan), 0, stream, a);
+    if (a.num_pages <= kSmall) hipLaunchKernelGGL((k_plan_moves<4>), dim3(1), dim3(kScan), 0, stream, a);
+    else hipLaunchKernelGGL((k_plan_moves<16>), dim3(1), dim3(kScan), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(k_move, dim3(2048), dim3(256), 0, stream, a, parts_of(a.page_bytes, 1));
     return hipGetLastError();
