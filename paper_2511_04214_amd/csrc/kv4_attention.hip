@@ -65,6 +65,12 @@ __device__ __forceinline__ void split_pages(int b, int e, int split, int splits,
     *end = b + min((split + 1) * each, n);
 }
 
+// The first token that a row at position p sees in a window (0: all).  p may be in front of the first token, and p - window further down than
+// 32 bits reach: nothing is subtracted there.
+__host__ __device__ constexpr int window_begin(int p, int window) { return window && p >= window ? p - window + 1 : 0; }
+static_assert(window_begin(-3, 0x7ffffffe) == 0 && window_begin(-2, 0x7fffffff) == 0 && window_begin(-0x7fffffff, 0x7fffffff) == 0 &&
+              window_begin(0x7ffffffe, 1) == 0x7ffffffe && window_begin(5, 6) == 0 && window_begin(5, 5) == 1 && window_begin(5, 0) == 0, "no difference overflows");
+
 // Range of query rows [q0, q1) of a sequence; empty where the offsets are none.
 __device__ __forceinline__ void query_rows(const AttnArgs& a, int s, int64_t* q0, int* n) {
     int64_t b = s, e = (int64_t)s + 1;
@@ -167,7 +173,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     int nq;
     query_rows(a, s, &q0, &nq);
     if (nq == 0) return;
-    const int rows = nq * a.G, len = a.kv_lens[s], all = min(len, min(a.max_kv, a.table_cols * kKv4Page));
+    const int rows = nq * a.G, len = max(a.kv_lens[s], 0), all = min(len, min(a.max_kv, a.table_cols * kKv4Page));
     // the tokens of this lane's rows, of any row, of all
     const int p0 = len - (a.cu_q ? (int)(a.cu_q[s + 1] - a.cu_q[s]) : 1), p1 = p0 + nq - 1;
     int end[RT], begin[RT], end_any = all, begin_any = 0, end_all = all, begin_all = 0;
@@ -176,7 +182,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     for (int rt = 0; rt < RT; ++rt) {
         const int r = rt * 16 + n, tok = r < rows ? r / a.G : 0, head = kvh * a.G + (r < rows ? r - tok * a.G : 0), p = p0 + tok;
         end[rt] = a.causal ? min(all, p + 1) : all;
-        begin[rt] = a.causal && a.window ? max(0, p - a.window + 1) : 0;
+        begin[rt] = a.causal ? window_begin(p, a.window) : 0;
         const uint8_t* qp = a.q.p + (q0 + tok) * a.q.ts + head * a.q.hs;
         const int flip = a.scale < 0.0f ? (int)0x80008000u : 0;
         const v4i zero = {0, 0, 0, 0};
@@ -189,10 +195,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     if (a.causal) {
         end_any = min(all, p1 + 1);
         end_all = min(all, p0 + 1);
-        if (a.window) {
-            begin_any = max(0, p0 - a.window + 1);
-            begin_all = max(0, p1 - a.window + 1);
-        }
+        begin_any = window_begin(p0, a.window);
+        begin_all = window_begin(p1, a.window);
     }
     end_any = __builtin_amdgcn_readfirstlane(end_any);
     begin_any = __builtin_amdgcn_readfirstlane(begin_any);
@@ -447,7 +451,7 @@ __global__ __launch_bounds__(MODE == kOne ? 256 : 512, MODE == kPair && D == 64 
     int64_t q0;
     if (!tile_of(a, id, TILE, &s, &q0, &nq, &tile)) return;
     const int rows = nq * a.G, r0 = tile * TILE;
-    const int len = a.kv_lens[s], all = min(len, min(a.max_kv, a.table_cols * kKv4Page));
+    const int len = max(a.kv_lens[s], 0), all = min(len, min(a.max_kv, a.table_cols * kKv4Page));
     const int first = len - (a.cu_q ? (int)(a.cu_q[s + 1] - a.cu_q[s]) : 1);          // position of the sequence's first row
     const int rw = r0 + (TALL ? w : w & 3) * 32, r = rw + n, rc = min(r, rows - 1), tok = rc / a.G, head = kvh * a.G + (rc - tok * a.G);
     // tokens that a row of the workgroup sees; that every row of the wavefront sees; that this lane's row sees
@@ -457,11 +461,9 @@ __global__ __launch_bounds__(MODE == kOne ? 256 : 512, MODE == kPair && D == 64 
         end = min(all, first + tok + 1);
         end_all = min(all, first + wa + 1);
         end_wg = min(all, first + gb + 1);
-        if (a.window) {
-            begin = max(0, first + tok - a.window + 1);
-            begin_all = max(0, first + wb - a.window + 1);
-            begin_wg = max(0, first + ga - a.window + 1);
-        }
+        begin = window_begin(first + tok, a.window);
+        begin_all = window_begin(first + wb, a.window);
+        begin_wg = window_begin(first + ga, a.window);
     }
     int page0, page1;
     split_pages(begin_wg / kKv4Page, (max(end_wg, 0) + kKv4Page - 1) / kKv4Page, split, splits, 1, &page0, &page1);
