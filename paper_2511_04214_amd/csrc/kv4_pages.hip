@@ -157,16 +157,18 @@ __device__ __forceinline__ int find_free(const PagesArgs& a, int32_t* pages, int
 template <bool FORK, int PER>
 __global__ __launch_bounds__(kScan) void k_find_free(const PagesArgs a) {
     __shared__ int lds[17];
+    __shared__ int64_t lds2[17];
     const Found f(a.workspace, a.n);
-    int want = 0, total, r[PER];
+    int r[PER];
+    int64_t want = 0, total;                                                     // (1024 rows of up to 2^25 columns, rows named twice among them, pass 32 bits)
     load_refs(a.refs, a.num_pages, (int)threadIdx.x * PER, r);                   // (on their way while the wants are counted)
     for (int i0 = 0; i0 < a.n; i0 += kScan) {
-        const int i = i0 + (int)threadIdx.x, w = i < a.n ? wanted<FORK>(a, i) : 0;
-        const int before = scan_before(w, lds, &total);
-        if (i < a.n) f.first[i] = min(want + before, a.num_pages);               // (more than there are is as good as any more)
-        want = min(want + total, a.num_pages);
+        const int i = i0 + (int)threadIdx.x;
+        const int64_t before = scan_before<int64_t>(i < a.n ? wanted<FORK>(a, i) : 0, lds2, &total);
+        if (i < a.n) f.first[i] = (int)min<int64_t>(want + before, a.num_pages); // (more than there are is as good as any more)
+        want = min<int64_t>(want + total, a.num_pages);
     }
-    const int found = find_free(a, f.pages, want, r, lds);
+    const int found = find_free(a, f.pages, (int)want, r, lds);
     if (threadIdx.x == 0) {
         f.count[0] = found;
         a.result[0] = 0;
