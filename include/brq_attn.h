@@ -90,7 +90,9 @@ brq_status brq_kv4_page_bytes(int64_t Hk, int64_t D, int64_t* bytes);
 /*
  * Writes the keys and values of T tokens to slots[t] (distinct; a slot outside the cache: the token is not
  * written):  keys as brq_qk_norm_rope makes them, kept in fp32, then brq_mxfp4_quantize; values v H_Bv /
- * sqrt(Bv), then the same.  Queries of the same tokens may come along (q, q_out of xdt; NULL together: none).
+ * sqrt(Bv), then the same, except that no scale is above 2^125, the largest under which all codes are finite
+ * (infinities and NaN saturate): what a token's value holds is nothing to rows that do not see it.
+ * Queries of the same tokens may come along (q, q_out of xdt; NULL together: none).
  * Everything else as in brq_qk_norm_rope.  A token whose position is outside the tables is not written.
  */
 brq_status brq_kv4_append(const brq_heads* q, const brq_heads* k, const brq_heads* v, brq_dtype xdt, int64_t T,

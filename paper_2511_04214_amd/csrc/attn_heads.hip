@@ -221,7 +221,10 @@ __global__ __launch_bounds__(256) void k_heads(const HeadsArgs a, int splits, in
                 }
                 if (out.there()) store_chunk<OUT_BF16, !APPEND>(to, v);
             } else {
-                const uint32_t sb = e8m0_from_amax(quad_max(absmax8(v)));
+                uint32_t sb = e8m0_from_amax(quad_max(absmax8(v)));
+                // 6 * 2^(252 - 127) is a number in 32 bits and in bf16; under 253, the scale of an infinity, 6 would become one, and 0 times
+                // it NaN in the rows that do not see the token
+                if constexpr (K == kValue) sb = min(sb, 252u);
                 const uint32_t codes = encode8_e2m1(v, sb);
                 if (write && out.there()) {
                     if constexpr (K == kKey) {
