@@ -100,8 +100,14 @@ struct Turn {
 #pragma unroll
             for (int i = 0; i < 8; ++i) p[i] = __shfl(v[i], src);
         }
+        if (r.rot < L * 8) {                         // channels behind the rotated ones stay as they are: 0 times an infinity is not 0
+            const bool turned = (int)chunk * 8 < r.rot;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(p[i], s[i], v[i] * c[i]);
+            for (int i = 0; i < 8; ++i) v[i] = turned ? __builtin_fmaf(p[i], s[i], v[i] * c[i]) : v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(p[i], s[i], v[i] * c[i]);
+        }
     }
 };
 
