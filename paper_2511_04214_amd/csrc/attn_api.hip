@@ -1,5 +1,8 @@
 // extern "C" boundary of the attention side (include/brq_attn.h): argument validation on the host, then launches on the
 // caller's stream.
+#include <cmath>
+#include <limits>
+
 #include "../../include/brq_attn.h"
 #include "brq_attn.h"
 #include "brq_launch.h"
@@ -251,7 +254,7 @@ brq_status brq_kv4_attention(const brq_heads* q, int64_t T, int64_t D, const uin
                              float scale, int causal, int64_t window, int64_t max_q, int64_t max_kv, const brq_heads* out,
                              float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
     if (!q || !out) return BRQ_ERR_NULL;
-    if (T < 0) return BRQ_ERR_SHAPE;
+    if (T < 0 || !(std::fabs(scale) <= std::numeric_limits<float>::max())) return BRQ_ERR_SHAPE;
     BRQ_CHECK(check_attention_sizes(T, S, q->heads, Hk, D, max_q, max_kv));
     BRQ_CHECK(check_heads(q, 2, T, D, -1, false));
     BRQ_CHECK(check_heads(out, 2, T, D, q->heads, true));
