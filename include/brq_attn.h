@@ -119,7 +119,8 @@ brq_status brq_kv4_read(const uint8_t* pool, int64_t num_pages, int64_t T, int64
  * below 0 count as 0; rows in front of the first token (p < 0) are rows like others.  A row that sees nothing
  * has o = 0, lse = -infinity; a NaN in a query makes its row NaN and no other.  Tokens whose page number is
  * outside the cache are not seen.
- * q and out are BRQ_BF16; lse [T][q.heads] fp32 or NULL; scale is a finite number.  Arithmetic: products exact, summed in the matrix
+ * q and out are BRQ_BF16; lse [T][q.heads] fp32 or NULL; scale is a finite number (of magnitude below 2^-126, 0
+ * included: taken for 2^-126).  Arithmetic: products exact, summed in the matrix
  * cores' fp32, softmax in fp32, its weights rounded to bf16 in front of the product with the values.
  * max_q, max_kv: what the host knows of the longest query and context; rows beyond max_q of a sequence, and rows
  * that are no sequence's, are not written, tokens at max_kv and beyond not seen.  They size the grid and the workspace.

@@ -115,7 +115,9 @@ __device__ __forceinline__ bool tile_of(const AttnArgs& a, int id, int size, int
 // wavefronts a SIMD), one with three in 4.6.
 __device__ __forceinline__ float uniform_f32(float v) { return as_f32(__builtin_amdgcn_readfirstlane(as_u32(v))); }
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// The least scale is that of the smallest normal number, for smaller ones and 0 too: 0 times the -infinity of a token that is not seen
+// would be NaN, and what it makes of any score that 32 bits hold is below 4.
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kLeastScale = 0x1p-126f;
 
 // ---- up to 32 query rows (tokens x heads of a group) against a range of pages: decoding
 
@@ -205,7 +207,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_few(const AttnArgs a, int 
     int page0, page1;
     split_pages(begin_any / kKv4Page, (max(end_any, 0) + kKv4Page - 1) / kKv4Page, split, splits, 4, &page0, &page1);
 
-    const float c = uniform_f32(fmaxf(fabsf(a.scale) * kLog2e, 1e-30f));
+    const float c = uniform_f32(fmaxf(fabsf(a.scale) * kLog2e, kLeastScale));
 
     v4f o[RT][MT];
     float l[RT], ref[RT], top_ref[RT];                    // ref: what is subtracted; top_ref: the same, -inf before any token
@@ -480,7 +482,7 @@ __global__ __launch_bounds__(MODE == kOne ? 256 : 512, MODE == kPair && D == 64 
                 q[k][j] = __builtin_bit_cast(bf16x8, x);
             }
     }
-    const float c = uniform_f32(fmaxf(fabsf(a.scale) * kLog2e, 1e-30f));
+    const float c = uniform_f32(fmaxf(fabsf(a.scale) * kLog2e, kLeastScale));
 
     v16f o[MT];
 #pragma unroll
