@@ -7,8 +7,9 @@
  * nothing allocated, work enqueued on `stream`, argument errors found on the host before anything is
  * launched), and these besides:
  *   - A set of heads (brq_heads) is x[t][h][d] = data[t * token_stride + h * head_stride + d] of one
- *     dtype, d < D contiguous; strides are in elements and any multiples of 16 bytes, so that queries,
- *     keys and values may be views of one packed projection.  Outputs may not overlap inputs.
+ *     dtype, d < D contiguous; strides are in elements and any multiples of 16 bytes from 0 on, so that
+ *     queries, keys and values may be views of one packed projection.  Outputs may not overlap inputs.
+ *     T tokens of a set have T * heads < 2^25 heads together.
  *   - What the host cannot see is checked on the device where memory depends on it: a position outside
  *     the tables, a slot or page number outside the cache, a length or offset outside its table is
  *     never used to address memory; what comes out instead is stated at each call.
@@ -120,10 +121,11 @@ brq_status brq_kv4_read(const uint8_t* pool, int64_t num_pages, int64_t T, int64
  * has o = 0, lse = -infinity; a NaN in a query makes its row NaN and no other.  Tokens whose page number is
  * outside the cache are not seen.
  * q and out are BRQ_BF16; lse [T][q.heads] fp32 or NULL; scale is a finite number (of magnitude below 2^-126, 0
- * included: taken for 2^-126).  Arithmetic: products exact, summed in the matrix
- * cores' fp32, softmax in fp32, its weights rounded to bf16 in front of the product with the values.
+ * included: taken for 2^-126).  Arithmetic: products exact, summed in the matrix cores' fp32, softmax in fp32, its
+ * weights rounded to bf16 in front of the product with the values.
  * max_q, max_kv: what the host knows of the longest query and context; rows beyond max_q of a sequence, and rows
  * that are no sequence's, are not written, tokens at max_kv and beyond not seen.  They size the grid and the workspace.
+ * T * q.heads < 2^25, q.heads and Hk < 2^16, S * Hk < 2^22, max_q and table_cols < 2^25, max_kv < 2^31 - 64.
  * workspace: brq_kv4_attention_workspace bytes (may be 0, then NULL), 16-byte aligned.
  */
 brq_status brq_kv4_attention(const brq_heads* q, int64_t T, int64_t D, const uint8_t* pool, int64_t num_pages,
@@ -152,8 +154,8 @@ brq_status brq_kv4_attention_workspace(int64_t T, int64_t S, int64_t Hq, int64_t
  *          columns; failed[0] (int32) is set to the number of those.
  * compact: the live pages move to the lowest numbers: the k-th free page below their count gets the k-th
  *          live page above it.  table and refs follow; live[0] (int32) is set to the count.
- * workspace: brq_kv4_pages_workspace bytes (compact: n = 0), 16-byte aligned.  table_cols, num_pages, n < 2^31 and
- * S * table_cols < 2^31; page_bytes is a multiple of 16.
+ * workspace: brq_kv4_pages_workspace bytes (compact: n = 0), 16-byte aligned.  S and S * table_cols < 2^31,
+ * num_pages < 2^29, table_cols < 2^25, n < 2^21; page_bytes is a multiple of 16 below 2^31.
  */
 brq_status brq_kv4_pages_workspace(int64_t n, int64_t num_pages, int64_t* bytes);
 brq_status brq_kv4_pages_copy(uint8_t* pool, int64_t page_bytes, int64_t num_pages, const int32_t* src,

@@ -85,8 +85,8 @@ brq_status check_attention_sizes(int64_t T, int64_t S, int64_t Hq, int64_t Hk, i
     if (D != 64 && D != 128) return BRQ_ERR_SHAPE;
     if (T < 0 || S < 0 || S >= kMax || Hk < 1 || Hk >= 65536 || Hq < 1 || Hq % Hk != 0 || Hq >= 65536 || T >= kMax || T * Hq >= kMax / 64) return BRQ_ERR_SHAPE;
     if (max_q < 1 || max_q >= kMax / 64 || max_kv < 0 || max_kv >= kMax - 64) return BRQ_ERR_SHAPE;
-    if (S > 0 && (S * Hq >= kMax || (max_q + 15) / 16 * 16 * (S * Hq) >= kMax)) return BRQ_ERR_SHAPE;
-    if (S * Hk >= kMax / 512) return BRQ_ERR_SHAPE;          // (a workgroup of up to 512 threads to each, in one grid)
+    // a workgroup of up to 512 threads to each, and to every 128 rows besides, in one grid; max_q, a bound alone, adds none
+    if (S * Hk >= kMax / 512) return BRQ_ERR_SHAPE;
     return BRQ_OK;
 }
 
