@@ -905,8 +905,8 @@ static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t strea
     else if (p.mode == kPair) hipLaunchKernelGGL((k_attention_many<D, kPair>), grid, dim3(512), 0, stream, a, p.splits, po, pm);
     else hipLaunchKernelGGL((k_attention_many<D, kOne>), grid, dim3(256), 0, stream, a, 1, nullptr, nullptr);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;
-    const int64_t rows = a.T * Hq;
-    if (p.splits <= 8) hipLaunchKernelGGL((k_attention_join<D, 1>), dim3((uint32_t)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, stream, a, p.splits, po, pm);
+    const int64_t rows = a.T * Hq;                       // (a workgroup to each while a grid has them: 2^32 threads)
+    if (p.splits <= 8 || rows >= int64_t(1) << 24) hipLaunchKernelGGL((k_attention_join<D, 1>), dim3((uint32_t)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, stream, a, p.splits, po, pm);
     else hipLaunchKernelGGL((k_attention_join<D, 1024 / D>), dim3((uint32_t)rows), dim3(256), 0, stream, a, p.splits, po, pm);
     return hipGetLastError();
 }
