@@ -98,6 +98,26 @@ brq_status brq_diag_mxfp4_gemm_on(int32_t route, const uint8_t* aq, const uint8_
                                   brq_layout w_layout, int64_t M, int64_t N, int64_t K, void* y,
                                   brq_dtype ydt, int64_t ldy, void* stream);
 
+/*
+ * The kernels of brq_kv4_attention.  Which of them takes a call is decided by its sizes; the call below names the choice, so that a test
+ * of a kernel can say that it is the one that runs.
+ */
+enum {
+    BRQ_KV4_FEW_16 = 0,          /* up to 16 rows (query rows x heads of a group) of a sequence */
+    BRQ_KV4_FEW_32 = 1,          /* 17 to 32 */
+    BRQ_KV4_ONE = 2,             /* tiles of 128 rows: one group of wavefronts to each, */
+    BRQ_KV4_PAIR = 3,            /* two that share its pages; */
+    BRQ_KV4_TALL = 4             /* tiles of 256 rows */
+};
+
+/*
+ * *route = the kernel that brq_kv4_attention takes for these arguments on a device of `cus` compute units, *parts = into how many
+ * parts it cuts a context.  Host arithmetic only: no device is needed.  A call without rows has none (BRQ_ERR_SHAPE).
+ */
+brq_status brq_diag_kv4_attention_route(int64_t T, int64_t S, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
+                                        int64_t max_kv, int causal, int64_t window, int64_t cus, int32_t* route,
+                                        int32_t* parts);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,7 @@ EXPORTS = ["brq_init", "brq_block_rotate", "brq_operand_bytes", "brq_mxfp4_quant
            "brq_matrix_rotate_quantize_fused", "brq_block_stats", "brq_block_stats_summary", "brq_mxfp4_gemm", "brq_rotate_quantize_gemm_fused", "brq_to_rowmajor", "brq_diag_mfma_ceiling", "brq_diag_mxfp4_gemm_clock", "brq_diag_mxfp4_gemm_no_loads", "brq_diag_mxfp4_gemm_route",
            "brq_diag_mxfp4_gemm_on", "brq_qk_norm_rope", "brq_qk_norm_rope_backward", "brq_qk_norm_rope_backward_workspace", "brq_kv4_page_bytes",
            "brq_kv4_append", "brq_kv4_read", "brq_kv4_attention", "brq_kv4_attention_workspace", "brq_kv4_pages_workspace", "brq_kv4_pages_copy",
-           "brq_kv4_pages_fork", "brq_kv4_pages_free", "brq_kv4_pages_reserve", "brq_kv4_pages_compact", "brq_strerror", "brq_version"]
+           "brq_kv4_pages_fork", "brq_kv4_pages_free", "brq_kv4_pages_reserve", "brq_kv4_pages_compact", "brq_diag_kv4_attention_route", "brq_strerror", "brq_version"]
 
 _lib = None
 _native = None          # the compiled marshalling, its entry points bound to those of _lib; None: not loaded
@@ -538,6 +538,6 @@ def diag_mfma_ceiling(operands, iters, workgroups, sink=None, stream=None):
 
 
 from . import attention as _attention          # noqa: E402  (at the end: it uses what is above)
-from .attention import (KV4_PAGE, kv4_append, kv4_attention, kv4_attention_workspace, kv4_page_bytes, kv4_pages_compact,  # noqa: E402,F401
+from .attention import (KV4_PAGE, KV4_ROUTES, diag_kv4_attention_route, kv4_append, kv4_attention, kv4_attention_workspace, kv4_page_bytes, kv4_pages_compact,  # noqa: E402,F401
                         kv4_pages_copy, kv4_pages_fork, kv4_pages_free, kv4_pages_reserve, kv4_pages_workspace, kv4_read, qk_norm_rope,
                         qk_norm_rope_backward, qk_norm_rope_backward_workspace)

@@ -40,6 +40,7 @@ def declare(L):
             ("kv4_append", [h, h, h, i32, i64, i64, vp, vp, f32, r, i64, i64, vp, vp, i64, h, vp]),
             ("kv4_read", [vp, i64, i64, i64, vp, h, h, i32, vp]),
             ("kv4_attention", [h, i64, i64, vp, i64, i64, vp, i64, vp, vp, i64, f32, i32, i64, i64, i64, h, vp, vp, i64, vp]),
+            ("diag_kv4_attention_route", [i64, i64, i64, i64, i64, i64, i64, i32, i64, i64, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]),
             ("kv4_attention_workspace", [i64, i64, i64, i64, i64, i64, i64, n]),
             ("kv4_pages_workspace", [i64, i64, n]),
             ("kv4_pages_copy", [vp, i64, i64, vp, vp, i64, vp]),
@@ -297,6 +298,18 @@ def kv4_attention(q, pool, table, kv_lens, scale=None, causal=True, window=0, cu
         _ref(ho), _array(lse, "lse", torch.float32, (T, Hq), True), _array(workspace, "workspace", torch.uint8, (None,), True),
         0 if workspace is None else workspace.numel(), _brq._stream(stream)))
     return out if lse is None else (out, lse)
+
+
+# the kernels of kv4_attention (include/brq_diag.h), by their numbers there
+KV4_ROUTES = ("few_16", "few_32", "one", "pair", "tall")
+
+
+def diag_kv4_attention_route(T, S, Hq, Hk, D, max_q, max_kv, causal=True, window=0, cus=256):
+    """(kernel, parts): the kernel that kv4_attention takes for a call of these sizes on a device of `cus` compute units, one of
+    KV4_ROUTES, and into how many parts it cuts a context (brq_diag_kv4_attention_route; needs no GPU)."""
+    r, n = ctypes.c_int32(), ctypes.c_int32()
+    _brq._check(_brq.lib().brq_diag_kv4_attention_route(T, S, Hq, Hk, D, max_q, max_kv, int(bool(causal)), window, cus, ctypes.byref(r), ctypes.byref(n)))
+    return KV4_ROUTES[r.value], n.value
 
 
 def kv4_pages_workspace(n, num_pages):

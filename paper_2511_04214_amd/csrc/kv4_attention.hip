@@ -10,6 +10,8 @@
 // accumulators to the second's operand without leaving the lane and a row's rescaling is one factor a lane.
 #include <algorithm>
 
+#include "../../include/brq_attn.h"
+#include "../../include/brq_diag.h"
 #include "brq_attn.h"
 #include "brq_device.h"
 #include "brq_launch.h"
@@ -858,6 +860,7 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 struct Plan {
     bool few;
     int mode;                    // of the kernel for many rows
+    int route;                   // the kernel, by its number in include/brq_diag.h
     int64_t tiles;               // of a head of the cache (few: one a sequence)
     int splits;
     static Plan of(int64_t T, int64_t S, int Hk, int G, int D, int64_t max_q, int64_t max_kv, bool causal, int window, int cus) {
@@ -876,11 +879,18 @@ struct Plan {
         int64_t n = few || mode == kPair ? cus / wgs : 1;
         if (few && S > 1) n = std::max(n, std::min((4 * cus + wgs - 1) / wgs, (pages + 16) / 32));
         n = pages <= (few ? 16 : 8) ? 1 : std::min(n, few ? (pages + 7) / 8 : (pages + 3) / 4);
-        return {few, mode, tiles, (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
+        const int route = few ? (max_q * G > 16 ? BRQ_KV4_FEW_32 : BRQ_KV4_FEW_16) : mode == kTall ? BRQ_KV4_TALL : mode == kPair ? BRQ_KV4_PAIR : BRQ_KV4_ONE;
+        return {few, mode, route, tiles, (int)std::max<int64_t>(1, std::min<int64_t>(n, 256))};
     }
 };
 
 }  // namespace
+
+int kv4_attention_route(int64_t T, int64_t S, int Hq, int Hk, int D, int64_t max_q, int64_t max_kv, bool causal, int window, int cus, int* parts) {
+    const Plan p = Plan::of(T, S, Hk, Hq / Hk, D, max_q, max_kv, causal, window, cus);
+    *parts = p.splits;
+    return p.route;
+}
 
 int64_t kv4_attention_workspace(int64_t T, int64_t S, int Hq, int Hk, int D, int64_t max_q, int64_t max_kv, int cus) {
     const Plan p = Plan::of(T, S, Hk, Hq / Hk, D, max_q, max_kv, false, 0, cus);
@@ -898,12 +908,15 @@ static hipError_t launch_attention(const AttnArgs& a, int cus, hipStream_t strea
     // 118 us, 122 us as they come; from 48 pages on, since it takes a workgroup 0.5 us to know: 100 of up to 2000 32 us, 31 us as they come)
     const bool sorted = p.few && a.S > 1 && a.S <= 256 && !a.window && pages >= 48 && (int64_t)a.S * a.Hk * p.splits > 2 * cus;
     const int order = sorted ? 1 << (31 - __builtin_clz(pages)) : 0;
-    if (p.mode == kTall) {
-        if constexpr (D == 128) hipLaunchKernelGGL((k_attention_many<D, kTall>), grid, dim3(512), 0, stream, a, 1, nullptr, nullptr);
-    } else if (p.few && a.max_q * a.G > 16) hipLaunchKernelGGL((k_attention_few<D, 2>), grid, dim3(256), 0, stream, a, p.splits, order, po, pm);
-    else if (p.few) hipLaunchKernelGGL((k_attention_few<D, 1>), grid, dim3(256), 0, stream, a, p.splits, order, po, pm);
-    else if (p.mode == kPair) hipLaunchKernelGGL((k_attention_many<D, kPair>), grid, dim3(512), 0, stream, a, p.splits, po, pm);
-    else hipLaunchKernelGGL((k_attention_many<D, kOne>), grid, dim3(256), 0, stream, a, 1, nullptr, nullptr);
+    switch (p.route) {
+        case BRQ_KV4_FEW_16: hipLaunchKernelGGL((k_attention_few<D, 1>), grid, dim3(256), 0, stream, a, p.splits, order, po, pm); break;
+        case BRQ_KV4_FEW_32: hipLaunchKernelGGL((k_attention_few<D, 2>), grid, dim3(256), 0, stream, a, p.splits, order, po, pm); break;
+        case BRQ_KV4_ONE: hipLaunchKernelGGL((k_attention_many<D, kOne>), grid, dim3(256), 0, stream, a, 1, nullptr, nullptr); break;
+        case BRQ_KV4_PAIR: hipLaunchKernelGGL((k_attention_many<D, kPair>), grid, dim3(512), 0, stream, a, p.splits, po, pm); break;
+        case BRQ_KV4_TALL:
+            if constexpr (D == 128) hipLaunchKernelGGL((k_attention_many<D, kTall>), grid, dim3(512), 0, stream, a, 1, nullptr, nullptr);
+            break;
+    }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !po) return e;
     const int64_t rows = a.T * Hq;                       // (a workgroup to each while a grid has them: 2^32 threads)
     if (p.splits <= 8 || rows >= int64_t(1) << 24) hipLaunchKernelGGL((k_attention_join<D, 1>), dim3((uint32_t)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, stream, a, p.splits, po, pm);
@@ -918,3 +931,15 @@ hipError_t launch_kv4_attention(int D, const AttnArgs& a, hipStream_t stream) {
 }
 
 }  // namespace brq
+
+// (here and not with the other entry points: nothing but the rule above is behind it)
+extern "C" brq_status brq_diag_kv4_attention_route(int64_t T, int64_t S, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q, int64_t max_kv, int causal,
+                                                   int64_t window, int64_t cus, int32_t* route, int32_t* parts) {
+    int64_t none = 0;
+    if (const brq_status st = brq_kv4_attention_workspace(0, S, Hq, Hk, D, max_q, max_kv, &none); st != BRQ_OK) return st;
+    if (!route || !parts) return BRQ_ERR_NULL;
+    constexpr int64_t kMax = int64_t(1) << 31;
+    if (T < 1 || S < 1 || T >= kMax || T * Hq >= kMax / 64 || cus < 1 || cus >= kMax || window < 0 || window >= kMax || (window > 0 && !causal)) return BRQ_ERR_SHAPE;
+    *route = brq::kv4_attention_route(T, S, (int)Hq, (int)Hk, (int)D, max_q, max_kv, causal != 0, (int)window, (int)cus, parts);
+    return BRQ_OK;
+}
