@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256) void k_fork(const PagesArgs a, int parts) {
     int32_t *from = a.table + (int64_t)p * a.cols, *to = a.table + (int64_t)c * a.cols;
     const bool failed = want > 0 && f.first[i] >= f.count[0];
     const int page = want > 0 && !failed ? f.pages[f.first[i]] : -1;
-    if (page >= 0) {
+    if (page >= 0 && full < a.cols) {                     // (always, unless another pair is just writing the parent's length)
         const int last = from[full];
         if (in_range(last, a.num_pages)) move_page(a.pool, a.page_bytes, last, page, part, parts);
     }

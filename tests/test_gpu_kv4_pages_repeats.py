@@ -34,3 +34,18 @@ def test_rows_named_twice_among_others():
         for s in range(0, n, 2):
             need = -(-int(tokens[s: s + 2].max()) // 64)
             assert (t[s, :need] >= 0).all() and (t[s, need:] == -1).all() and (t[s + 1] == -1).all()
+
+
+def test_children_that_are_parents():
+    """A pair's child as another's parent in one call: whose state is copied is not said, but pages stay pages."""
+    for cols in (1, 3):
+        S, n = 300, 40
+        table, refs = torch.full((S, cols), -1, dtype=I32, device="cuda"), torch.zeros(2000, dtype=I32, device="cuda")
+        lens = torch.zeros(S, dtype=I32, device="cuda")
+        first = torch.arange(n, dtype=I32, device="cuda")
+        assert int(brq.kv4_pages_reserve(table, refs, first, torch.full((n,), cols * 64, dtype=I32, device="cuda"))) == 0
+        lens[:n:2], lens[1:n:2] = cols * 64, cols * 64 - 7
+        pool = torch.zeros((2000, 4352), dtype=torch.uint8, device="cuda")
+        brq.kv4_pages_fork(pool, table, lens, refs, torch.arange(250, dtype=I32, device="cuda"), torch.arange(n, n + 250, dtype=I32, device="cuda"))
+        t = table.cpu()
+        assert bool(((t >= -1) & (t < 2000)).all()) and bool((lens.cpu() <= cols * 64).all()) and bool((refs.cpu() >= 0).all())
