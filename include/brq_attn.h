@@ -122,7 +122,8 @@ brq_status brq_kv4_read(const uint8_t* pool, int64_t num_pages, int64_t T, int64
  * outside the cache are not seen.
  * q and out are BRQ_BF16; lse [T][q.heads] fp32 or NULL; scale is a finite number (of magnitude below 2^-126, 0
  * included: taken for 2^-126).  Arithmetic: products exact, summed in the matrix cores' fp32, softmax in fp32, its
- * weights rounded to bf16 in front of the product with the values.
+ * weights rounded to bf16 in front of the product with the values (of up to 32 rows, query rows x heads of a group,
+ * to a sequence at most: divided by the sum of the rounded weights; of more: by the weights' own).
  * max_q, max_kv: what the host knows of the longest query and context; rows beyond max_q of a sequence, and rows
  * that are no sequence's, are not written, tokens at max_kv and beyond not seen.  They size the grid and the workspace.
  * T * q.heads < 2^25, q.heads and Hk < 2^16, S * Hk < 2^22, max_q and table_cols < 2^25, max_kv < 2^31 - 64.
