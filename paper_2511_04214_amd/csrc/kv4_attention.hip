@@ -161,7 +161,7 @@ __device__ __forceinline__ int by_length(const AttnArgs& a, int r, int top) {
 }
 
 // Workgroup: sequence, cache head, split.  Wavefront w goes through pages first + w, first + w + 4, ...
-// Bound by the cache's bytes: one row of 131 072 tokens, 143 MB, 26 us (5.4 TB/s); 100 of up to 8192, 609 MB, 115 us.  16 rows of the
+// Bound by the cache's bytes: one row of 131 072 tokens, 143 MB, 27.9 us (5.1 TB/s, and 4.7 us to join 32 parts); 100 of up to 8192, 609 MB, 117 us.  16 rows of the
 // matrix instruction, RT times, take all heads of a group, so that a page is read once for them; each wavefront unpacks its own pages in
 // registers, the next one's loads under way.  (17 to 32 rows here and not in tiles of 128: 8 sequences of 4 rows x 8 heads over up to
 // 4000 tokens 13.9 us, 21.8 us in tiles.)
@@ -441,14 +441,15 @@ struct Share {
 // each, measured) but not another wavefront's.  So the two never mix: a page is a matrix phase (the last page's weights times its
 // values, this page's scores) and a vector phase (scores to weights, unpacking), and of the two groups one is in the one while the
 // other is in the other, a barrier between phases.  With the phases of a wavefront interleaved instruction by instruction instead,
-// and two independent workgroups on a CU, a prompt of 8192 tokens took 535 us, so 482 us (1.14 PFLOP/s; the board's power bounds it).
+// and two independent workgroups on a CU, a prompt of 8192 tokens took 535 us, so 482 us on the same board (480 to 510 us
+// from board to board, 1.08 to 1.15 PFLOP/s: of a SIMD's cycles matrix instructions take 53%, the issue of vector instructions 52%).
 // kPair: 128 rows; the two groups take every other page of them, each with buffers of its own, and add their sums up at the end.
 // For calls that tall tiles do not fill the card with: a page after another costs a lone group 1.4 us, whatever the rest of the card
-// does, and partial sums through memory cost more than they save there (1024 tokens, 32 heads of 128: 28 us; one group 38 us, tall
+// does, and partial sums through memory cost more than they save there (1024 tokens, 32 heads of 128: 27 us; one group 38 us, tall
 // tiles 41 us).
 // Weights are rounded to bf16 here too, and the output is divided by their own sum: 1.12 times as far from 64 bits as the plain form, 1.28 at
 // most (37 draws).  The sum of the rounded ones, by an instruction that adds two of them, takes a prompt of 8192 tokens from 496 to 523 us.
-// kOne: 128 rows, one group, for contexts of a few pages, where a second one is only more to start (64 tokens: 8.3 us, 11.3 us paired).
+// kOne: 128 rows, one group, for contexts of a few pages, where a second one is only more to start (64 tokens: 8.1 us, 11.3 us paired).
 enum { kOne, kPair, kTall };
 template <int D, int MODE>
 __global__ __launch_bounds__(MODE == kOne ? 256 : 512, MODE == kPair && D == 64 ? 4 : 2) void k_attention_many(const AttnArgs a, int splits, float* part_o, float* part_ml) {
@@ -858,20 +859,20 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs a, int sp
 
 // How a call is cut up.  Up to 32 rows of a sequence to a cache head: the kernel whose wavefronts share them and take different
 // pages.  More: one group for contexts of up to 6 pages (350 tokens, 32 heads: 15.2 us, 15.8 us paired; 512: 18.3 either way).  Heads
-// of 64: pairs, whose four wavefronts a SIMD suit work that the vector units bound (8192 tokens, 16 heads: 172 us, tall tiles 189 us).
+// of 64: pairs, whose four wavefronts a SIMD suit work that vector instructions bound (66% of a SIMD's cycles, matrix instructions 34%, 8192
+// tokens of 16 heads: 174 us, tall tiles 189 us).
 // Heads of 128: pairs or tall tiles, whichever is through first by what was measured: a workgroup 8 us to start and end and 1.65 us a
 // page with tall tiles, 9 and 1.15 paired, one a CU; the whole takes its longest, or as many rounds of the mean as there are (32 heads,
 // pairs and tall tiles: 1500 tokens 40 and 46 us, 2048 58 and 61, 3000 110 and 90; 6 chunks of up to 500 over up to 4000 in a window of
 // 1024 54 and 38).
-// The pages are split where the tiles alone leave CUs idle, except so few that joining takes longer than they do.  Few rows: more than
-// 16, to no less than 8 (1000 tokens: 8.1 us, 8.9 us in halves; 1300 9.7 and 9.2).  Many: more than 8, to no less than 4 (64 tokens over
-// 1500, 8 heads on 2 of 128: 17.5 us, 21.0 us to no less than 8; 500 over 500, 32 heads: 18 us, 28 us in halves), and to one workgroup a
-// CU at most, since every split writes and reads its rows' sums in 32 bits (256 tokens over 8192, 32 heads: 57 us, to two a CU 66 us, whole
-// 132 us).  Few:
-// to one a CU at most (one row of 131 072 tokens in a cache: 29 us, to two a CU 31 us; 24 of up to 2000, 8 heads of the cache: 13.9 us whole,
-// 15.8 in halves), of several sequences to four if that leaves 32 pages to a
-// split, because the sequences' lengths differ and shorter parts even out (72 of up to 8192 tokens: 93 us, 106 us to one a CU; 64 of up
-// to 2000, which it leaves whole: 22 us, 27 us to four a CU).
+// The pages are split where the tiles alone leave CUs idle, except so few that joining takes longer than they do.  Few rows: more than 16
+// pages, in at most one part for every 8 begun (1000 tokens: 8.1 us, 8.9 us in halves; 1300, in 3 parts, 9.2 us, whole 9.7).  Many: more than
+// 8, in at most one part for every 4 begun (64 tokens over 1500, 8 heads on 2 of 128: 17.4 us, one for every 8 21.0 us; 500 over 500, 32 heads:
+// 18 us whole, 28 us in halves), and to one workgroup a CU at most, since every part writes and reads its rows' sums in 32 bits (256 tokens over
+// 8192, 32 heads: 54 us, to two a CU 66 us, whole 132 us).  Few: to one a CU at most (one row of 131 072 tokens in a cache: 29 us, to two a CU
+// 31 us; 24 of up to 2000, 8 heads of the cache: 13.9 us whole, 15.8 in halves), of several sequences to four, but no more than one for every 32
+// pages (the last one for 16 and more), because the sequences' lengths differ and shorter parts even out (72 of up to 8192 tokens: 93 us, 106 us to one
+// a CU; 64 of up to 2000, which it leaves whole: 22 us, 27 us to four a CU).
 struct Plan {
     bool few;
     int mode;                    // of the kernel for many rows
