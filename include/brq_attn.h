@@ -64,6 +64,7 @@ brq_status brq_qk_norm_rope(const brq_heads* q, const brq_heads* k, brq_dtype xd
  *     dx = (gn w - x * mean_d(gn w x) / (mean x^2 + eps)) / sqrt(mean x^2 + eps)        (w NULL: dx = gn)
  * dq, dk of xdt; dwq, dwk [D] fp32 are set, not added to (NULL: not wanted; must be NULL where the weight is).
  * The sums over tokens and heads are made in an order that depends on the sizes alone.
+ * A token whose position is outside the tables has NaN for its dx, and dw has it in its sums.
  * workspace: brq_qk_norm_rope_backward_workspace bytes, 16-byte aligned; may be NULL where dwq and dwk are.
  */
 brq_status brq_qk_norm_rope_backward(const brq_heads* q, const brq_heads* k, brq_dtype xdt, int64_t T, int64_t D,

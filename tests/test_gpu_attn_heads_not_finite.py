@@ -30,3 +30,20 @@ def test_channels_behind_the_rotated_ones(D, rot, interleaved, bad):
             assert torch.equal(got[..., rot:], y[..., rot:]) or (math.isnan(bad) and torch.equal(got[..., rot:].nan_to_num(7.5), y[..., rot:].nan_to_num(7.5)))
             # two products and their sum in 32 bits, of values below 5
             assert ((got[..., :rot].double() - clean[..., :rot]).abs() <= 4 * 2.0 ** -24 * 10).all()
+
+
+def test_gradients_of_positions_outside_the_tables():
+    """NaN in the gradients of their own rows, and in the sums that these are part of."""
+    g = torch.Generator().manual_seed(62)
+    T, H, D = 9, 3, 64
+    x, gr = torch.randn((T, H, D), generator=g).cuda(), torch.randn((T, H, D), generator=g).cuda()
+    angle, w = torch.rand((10, D // 2), generator=g) * 6.3, torch.ones(D, device="cuda")
+    pos = torch.arange(T)
+    a = dict(wq=w, cos=angle.cos().cuda(), sin=angle.sin().cuda())
+    want = brq.qk_norm_rope_backward(x, None, gr, None, positions=pos.cuda(), **a)[0]
+    pos[3], pos[7] = 10, -1
+    dx, _, dw, _ = brq.qk_norm_rope_backward(x, None, gr, None, positions=pos.cuda(), **a)
+    out = torch.tensor([3, 7])
+    keep = torch.ones(T, dtype=torch.bool)
+    keep[out] = False
+    assert torch.isnan(dx[out]).all() and torch.equal(dx[keep], want[keep]) and torch.isnan(dw).all()
