@@ -67,6 +67,7 @@ typedef enum {
     BRQ_ERR_LAUNCH = 6,      /* hipLaunchKernel failed (hipGetLastError) */
     BRQ_ERR_LAYOUT = 7,      /* layout is not one of brq_layout */
     BRQ_ERR_DEVICE = 8,      /* no current HIP device, or its one-time set-up failed */
+    BRQ_ERR_ACTIVATION = 9,  /* activation is not one of brq_activation (brq_residual.h) */
     BRQ_STATUS_INT_RANGE_ = 0x7fffffff   /* (gives the type the range of int: see below) */
 } brq_status;
 

@@ -99,6 +99,16 @@ brq_status brq_diag_mxfp4_gemm_on(int32_t route, const uint8_t* aq, const uint8_
                                   brq_dtype ydt, int64_t ldy, void* stream);
 
 /*
+ * brq_mxfp4_gemm_epilogue (brq_residual.h) on the kernel `route`, also where nothing follows the product; BRQ_ERR_SHAPE where that
+ * kernel does not take the shape, or takes no epilogue.
+ */
+brq_status brq_diag_mxfp4_gemm_epilogue_on(int32_t route, const uint8_t* aq, const uint8_t* as, brq_layout a_layout,
+                                           const uint8_t* wq, const uint8_t* ws, brq_layout w_layout, int64_t M,
+                                           int64_t N, int64_t K, const float* bias, int32_t act,
+                                           const void* residual, brq_dtype rdt, int64_t ldr, void* y,
+                                           brq_dtype ydt, int64_t ldy, void* stream);
+
+/*
  * The kernels of brq_kv4_attention.  Which of them takes a call is decided by its sizes; the call below names the choice, so that a test
  * of a kernel can say that it is the one that runs.
  */

@@ -6,7 +6,7 @@ include/brq.h, and returns the output tensors.  No arithmetic of the method happ
 here.  There is no CPU fallback: without the built library, or without a GPU tensor, the
 calls raise.
 
-The five calls that layers are made of, the two of the analysis, and those of the attention side (attention.py) are marshalled in csrc/binding.cpp where their arguments are plain; what it leaves
+The five calls that layers are made of, the two of the analysis, and those of the attention side (attention.py) and the residual side (residual.py) are marshalled in csrc/binding.cpp where their arguments are plain; what it leaves
 (it returns None) goes the way written here, which takes and refuses everything.  So do all calls where that part cannot be
 loaded: it is linked to one torch's C++ interface, libbrq.so to none.
 """
@@ -26,7 +26,9 @@ EXPORTS = ["brq_init", "brq_block_rotate", "brq_operand_bytes", "brq_mxfp4_quant
            "brq_matrix_rotate_quantize_fused", "brq_block_stats", "brq_block_stats_summary", "brq_mxfp4_gemm", "brq_rotate_quantize_gemm_fused", "brq_to_rowmajor", "brq_diag_mfma_ceiling", "brq_diag_mxfp4_gemm_clock", "brq_diag_mxfp4_gemm_no_loads", "brq_diag_mxfp4_gemm_route",
            "brq_diag_mxfp4_gemm_on", "brq_qk_norm_rope", "brq_qk_norm_rope_backward", "brq_qk_norm_rope_backward_workspace", "brq_kv4_page_bytes",
            "brq_kv4_append", "brq_kv4_read", "brq_kv4_attention", "brq_kv4_attention_workspace", "brq_kv4_pages_workspace", "brq_kv4_pages_copy",
-           "brq_kv4_pages_fork", "brq_kv4_pages_free", "brq_kv4_pages_reserve", "brq_kv4_pages_compact", "brq_diag_kv4_attention_route", "brq_strerror", "brq_version"]
+           "brq_kv4_pages_fork", "brq_kv4_pages_free", "brq_kv4_pages_reserve", "brq_kv4_pages_compact", "brq_diag_kv4_attention_route",
+           "brq_add_rms_norm", "brq_add_rms_norm_backward", "brq_add_rms_norm_backward_workspace", "brq_add_rms_norm_rotate_quantize_fused", "brq_mxfp4_gemm_epilogue", "brq_diag_mxfp4_gemm_epilogue_on",
+           "brq_strerror", "brq_version"]
 
 _lib = None
 _native = None          # the compiled marshalling, its entry points bound to those of _lib; None: not loaded
@@ -84,6 +86,7 @@ def lib():
         L.brq_diag_mfma_ceiling.argtypes = [vp, i64, i64, vp, vp]
         L.brq_diag_mfma_ceiling.restype = i32
         _attention.declare(L)
+        _residual.declare(L)
         L.brq_init.restype = i32
         L.brq_strerror.argtypes = [i32]
         L.brq_strerror.restype = ctypes.c_char_p
@@ -99,7 +102,7 @@ def _load_native(L):
         from . import _binding
         if getattr(_binding, "TORCH", None) != str(torch.__version__):
             raise ImportError("built against another torch than %s" % torch.__version__)
-        bind, bind_stats, bind_attention = _binding.bind, _binding.bind_stats, _binding.bind_attention
+        bind, bind_stats, bind_attention, bind_residual = _binding.bind, _binding.bind_stats, _binding.bind_attention, _binding.bind_residual
     except (ImportError, AttributeError) as e:              # (AttributeError: built before these calls came)
         warnings.warn("the compiled part of the binding is not used, calls take some us longer: %s" % e, RuntimeWarning, stacklevel=3)
         return None
@@ -108,6 +111,7 @@ def _load_native(L):
         L.brq_rotate_quantize_gemm_fused)))
     bind_stats(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.brq_block_stats, L.brq_block_stats_summary)))
     bind_attention(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in _attention.NATIVE))
+    bind_residual(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in _residual.NATIVE))
     return _binding
 
 
@@ -412,23 +416,8 @@ def _result(out, M, N, dtype, device):
     return out, ldy
 
 
-def mxfp4_gemm(aq, as_, wq, ws, out_dtype=torch.float32, out=None, stream=None, a_layout="rowmajor",
-               w_layout="rowmajor", M=None, N=None, K=None, clock=None, no_loads=False):
-    """Y[M, N] = deq(aq, as) @ deq(wq, ws)^T on the block-scaled MFMA (brq_mxfp4_gemm).
-
-    Row-major operands are 2-D tensors that carry their shape; a tiled operand is a flat byte
-    buffer, so its rows (M or N) and K must be given.  `clock` (an int64 GPU tensor of 6 elements;
-    large shapes only, brq_diag_mxfp4_gemm_clock) receives the shader-clock cycles and the 100 MHz
-    ticks that the kernel's first workgroup ran for, and their split over K loops and epilogues.
-    `no_loads` (with `clock`; brq_diag_mxfp4_gemm_no_loads) runs the measurement variant without refill
-    loads instead: `out` is written with values without meaning.
-    """
-    if _native is not None and stream is None and clock is None and not no_loads:
-        y = _native.gemm(aq, as_, wq, ws, out_dtype, out, a_layout, w_layout, M, N, K)
-        if y is not None:
-            if type(y) is int:
-                _check(y)
-            return y
+def _operands(aq, as_, wq, ws, a_layout, w_layout, M, N, K):
+    """(layout codes, M, N, K) of a product's operands, checked."""
     for t, n in ((aq, "aq"), (as_, "as"), (wq, "wq"), (ws, "ws")):
         if not (t.is_cuda and t.is_contiguous() and t.dtype == torch.uint8):
             raise ValueError("%s must be a contiguous uint8 GPU tensor" % n)
@@ -447,6 +436,27 @@ def mxfp4_gemm(aq, as_, wq, ws, out_dtype=torch.float32, out=None, stream=None, 
         cb, sb = _operand_size(rows, K, lay)
         if c.numel() < cb or s_.numel() < sb or (lay == "rowmajor" and tuple(s_.shape) != (rows, K // 32)):
             raise ValueError("operand %s: buffers do not match its shape and layout" % n)
+    return la, lw, M, N, K
+
+
+def mxfp4_gemm(aq, as_, wq, ws, out_dtype=torch.float32, out=None, stream=None, a_layout="rowmajor",
+               w_layout="rowmajor", M=None, N=None, K=None, clock=None, no_loads=False):
+    """Y[M, N] = deq(aq, as) @ deq(wq, ws)^T on the block-scaled MFMA (brq_mxfp4_gemm).
+
+    Row-major operands are 2-D tensors that carry their shape; a tiled operand is a flat byte
+    buffer, so its rows (M or N) and K must be given.  `clock` (an int64 GPU tensor of 6 elements;
+    large shapes only, brq_diag_mxfp4_gemm_clock) receives the shader-clock cycles and the 100 MHz
+    ticks that the kernel's first workgroup ran for, and their split over K loops and epilogues.
+    `no_loads` (with `clock`; brq_diag_mxfp4_gemm_no_loads) runs the measurement variant without refill
+    loads instead: `out` is written with values without meaning.
+    """
+    if _native is not None and stream is None and clock is None and not no_loads:
+        y = _native.gemm(aq, as_, wq, ws, out_dtype, out, a_layout, w_layout, M, N, K)
+        if y is not None:
+            if type(y) is int:
+                _check(y)
+            return y
+    la, lw, M, N, K = _operands(aq, as_, wq, ws, a_layout, w_layout, M, N, K)
     y, ldy = _result(out, M, N, out_dtype, aq.device)
     if clock is not None:
         if not (clock.is_cuda and clock.is_contiguous() and clock.dtype == torch.int64 and clock.numel() == 6):
@@ -541,3 +551,6 @@ from . import attention as _attention          # noqa: E402  (at the end: it use
 from .attention import (KV4_PAGE, KV4_ROUTES, diag_kv4_attention_route, kv4_append, kv4_attention, kv4_attention_workspace, kv4_page_bytes, kv4_pages_compact,  # noqa: E402,F401
                         kv4_pages_copy, kv4_pages_fork, kv4_pages_free, kv4_pages_reserve, kv4_pages_workspace, kv4_read, qk_norm_rope,
                         qk_norm_rope_backward, qk_norm_rope_backward_workspace)
+from . import residual as _residual            # noqa: E402
+from .residual import (ACTIVATIONS, add_rms_norm, add_rms_norm_backward, add_rms_norm_backward_workspace,  # noqa: E402,F401
+                       add_rms_norm_rotate_quantize_fused, diag_mxfp4_gemm_epilogue_on, mxfp4_gemm_epilogue)

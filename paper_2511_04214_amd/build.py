@@ -1,4 +1,5 @@
 """Compile the HIP library for gfx950 (hipcc cross-compiles; no GPU needed) and the binding's native part."""
+import concurrent.futures
 import os
 import subprocess
 import sysconfig
@@ -8,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbrq.so")
 BINDING = os.path.join(HERE, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["brq_api.hip", "rotate_quant.hip", "matrix_rotate_quant.hip", "block_summary.hip", "mxfp4_gemm.hip", "mxfp4_gemm_tiled.hip", "mxfp4_gemm_mid.hip",
-           "attn_api.hip", "attn_heads.hip", "kv4_attention.hip", "kv4_pages.hip"]
+           "mxfp4_gemm_mid_with.hip", "residual_api.hip", "add_rms_norm.hip", "attn_api.hip", "attn_heads.hip", "kv4_attention.hip", "kv4_pages.hip"]
 # -ffp-contract=off: the rotation's add/sub/mul sequence is part of the result's definition.
 # packed fp32 instructions are kept out of the generated code.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
@@ -16,8 +17,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=o
 
 
 def build_library(verbose=False):
-    objs = []
-    for src in SOURCES:
+    def compiled(src):
         obj = os.path.join(CSRC, src.replace(".hip", ".o"))
         cmd = ["hipcc"] + FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
@@ -28,7 +28,10 @@ def build_library(verbose=False):
             raise RuntimeError("hipcc failed on %s:\n%s" % (src, out))
         if verbose and out.strip():
             print(out)
-        objs.append(obj)
+        return obj
+
+    with concurrent.futures.ThreadPoolExecutor(4) as pool:        # (the two longest take minutes each)
+        objs = list(pool.map(compiled, sorted(SOURCES, key=lambda s: not s.startswith("mxfp4_gemm_mid"))))
     subprocess.check_call(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs)
     return LIB
 

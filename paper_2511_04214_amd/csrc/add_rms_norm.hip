@@ -1,0 +1,380 @@
+// The residual's addition and the RMS norm of the sum, alone and in front of the online step, and the gradients.
+//
+// A row is held in registers from its load to its last store: W wavefronts of 64 lanes, each lane C chunks of 8 elements, chunk
+// number (c * W + wavefront) * 64 + chunk_of_lane(lane).  So everything crosses HBM once, and a wavefront's pass c is 512 consecutive
+// elements, in the order that the rotations and the quantizer want (brq_device.h).  Lanes behind the row's end load its last chunk
+// again, in bounds, and hold zeros.  The sum of squares is taken in fp32: in a lane 8 C products in the order of the elements, then
+// pairs of lanes by chunk number, then the wavefronts in turn.  W and C depend on the sizes alone, so the norm alone and the fused
+// call have the same bits.
+#include "brq_device.h"
+#include "brq_launch.h"
+#include "brq_residual.h"
+
+namespace brq {
+namespace {
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    const int i = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, CTRL, 0xF, 0xF, true));
+}
+
+// Sum over a wavefront, every lane receiving it: chunks xor 1, 2, 4, 8 (the mirror images, in chunk_of_lane's order), 16, 32.
+__device__ __forceinline__ float wave_sum(float v) {
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    v += dpp<0x141>(v);
+    v += dpp<0x140>(v);
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
+    return v;
+}
+
+// fl(1/sqrt(2^l2)) as in the row-wise kernels: a power of two, or sqrt(2)/2 times one.
+__device__ constexpr uint32_t unit_bits(int l2) {
+    return (l2 & 1) ? (0x3F3504F3u - ((uint32_t)((l2 - 1) / 2) << 23)) : (0x3F800000u - ((uint32_t)(l2 / 2) << 23));
+}
+// H_B / sqrt(B) on each B elements of a wavefront's 512, B = 2^l2b (uniform).
+__device__ __forceinline__ void rotate(float (&v)[8], int l2b, uint32_t chunk) {
+    float s = 1.0f;
+    switch (l2b) {
+#define BRQ_CASE(L) case L: wht_inwave<L>(v, chunk); s = wht_sign<L>(chunk) * as_f32(unit_bits(L)); break;
+        BRQ_CASE(3) BRQ_CASE(4) BRQ_CASE(5) BRQ_CASE(6) BRQ_CASE(7) BRQ_CASE(8) BRQ_CASE(9)
+#undef BRQ_CASE
+        default: return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= s;
+}
+
+// C chunks of a row as they come from memory: 16 bytes each of bf16, 32 of fp32.
+template <int C>
+struct Raw {
+    v4i lo[C], hi[C];
+    __device__ __forceinline__ void load(const uint8_t* row, bool bf16, const uint32_t (&kc)[C]) {
+        if (bf16) {         // uniform
+#pragma unroll
+            for (int c = 0; c < C; ++c) lo[c] = *reinterpret_cast<const v4i*>(row + (size_t)kc[c] * 16);
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                lo[c] = *reinterpret_cast<const v4i*>(row + (size_t)kc[c] * 32);
+                hi[c] = *reinterpret_cast<const v4i*>(row + (size_t)kc[c] * 32 + 16);
+            }
+        }
+    }
+    __device__ __forceinline__ void widen(bool bf16, float (&v)[C][8]) const {
+        if (bf16) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[c][2 * i] = bf16_lo((uint32_t)lo[c][i]);
+                    v[c][2 * i + 1] = bf16_hi((uint32_t)lo[c][i]);
+                }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[c][i] = as_f32((uint32_t)lo[c][i]);
+                    v[c][4 + i] = as_f32((uint32_t)hi[c][i]);
+                }
+        }
+    }
+};
+
+__device__ __forceinline__ void store_values(uint8_t* row, bool bf16, uint32_t kc, const float (&v)[8]) {
+    if (bf16) {             // uniform
+        *reinterpret_cast<v4i*>(row + (size_t)kc * 16) =
+            v4i{(int)pack_bf16x2(v[0], v[1]), (int)pack_bf16x2(v[2], v[3]), (int)pack_bf16x2(v[4], v[5]), (int)pack_bf16x2(v[6], v[7])};
+    } else {
+        *reinterpret_cast<v4f*>(row + (size_t)kc * 32) = v4f{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<v4f*>(row + (size_t)kc * 32 + 16) = v4f{v[4], v[5], v[6], v[7]};
+    }
+}
+
+__device__ __forceinline__ void through_bf16(float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const uint32_t p = pack_bf16x2(v[i], v[i + 1]);
+        v[i] = bf16_lo(p);
+        v[i + 1] = bf16_hi(p);
+    }
+}
+
+template <int C>
+__device__ __forceinline__ void load_weight(const float* w, const uint32_t (&kc)[C], float (&v)[C][8]) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const v4f a = *reinterpret_cast<const v4f*>(w + (size_t)kc[c] * 8), b = *reinterpret_cast<const v4f*>(w + (size_t)kc[c] * 8 + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[c][i] = a[i]; v[c][4 + i] = b[i]; }
+    }
+}
+
+// Rows of a workgroup: 4 / W of W < 4 wavefronts, else one.
+template <int W>
+constexpr int rows_of = W < 4 ? 4 / W : 1;
+template <int W>
+constexpr int threads_of = W < 4 ? 256 : 64 * W;
+
+// N sums over a row's wavefronts, every lane receiving them.  `part`: [wavefronts of the workgroup][N]; every thread of the workgroup calls.
+template <int W, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*part)[N], int wave) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 63u) == 0) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) part[wave][n] = v[n];
+        }
+        __syncthreads();
+        const int first = wave / W * W;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            float s = part[first][n];
+#pragma unroll
+            for (int i = 1; i < W; ++i) s += part[first + i][n];
+            v[n] = s;
+        }
+    }
+}
+
+template <int W, int C, bool QUANT>
+__global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm(const NormArgs a, const KPad pad) {
+    __shared__ float part[threads_of<W> / 64][1];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), sub = wave % W;
+    const uint32_t lane = threadIdx.x & 63u, chunk = chunk_of_lane(lane), n = (uint32_t)(a.K / 8);
+    const int64_t mine = (int64_t)blockIdx.x * rows_of<W> + wave / W, row = mine < a.M ? mine : a.M - 1;
+    uint32_t kc[C];
+    bool live[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        kc[c] = (uint32_t)(c * W + sub) * 64u + chunk;
+        live[c] = kc[c] < n && mine < a.M;
+        kc[c] = min(kc[c], n - 1);
+    }
+    Raw<C> rx, rr;
+    rx.load(a.x.p + row * a.x.pitch, a.x.bf16, kc);
+    if (a.res.p) rr.load(a.res.p + row * a.res.pitch, a.res.bf16, kc);
+    float w[C][8], v[C][8];
+    if (a.w) load_weight(a.w, kc, w);
+    rx.widen(a.x.bf16, v);
+    if (a.res.p) {          // uniform
+        float r[C][8];
+        rr.widen(a.res.bf16, r);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] += r[c][i];
+            if (a.res.bf16) through_bf16(v[c]);
+        }
+    }
+    if (a.h.p) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (live[c]) store_values(a.h.p + row * a.h.pitch, a.h.bf16, kc[c], v[c]);
+    }
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = __builtin_fmaf(v[c][i], v[c][i], s);
+        sum[0] += live[c] ? s : 0.0f;
+    }
+    row_sums<W, 1>(sum, part, wave);
+    const float r = 1.0f / sqrtf(sum[0] / (float)a.K + a.eps);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[c][i] *= r;
+            if (a.w) v[c][i] *= w[c][i];
+        }
+        if constexpr (!QUANT) {
+            if (live[c]) store_values(a.y.p + row * a.y.pitch, a.y.bf16, kc[c], v[c]);
+        } else {
+            // (whole quads, and whole blocks, are behind the row's end together: what they hold reaches no one else)
+            if (a.y.bf16) through_bf16(v[c]);
+            if (a.signs) apply_signs(v[c], a.signs + (size_t)kc[c] * 8);
+            rotate(v[c], a.l2b, chunk);
+            const uint32_t sb = e8m0_from_amax(quad_max(absmax8(v[c]))), codes = encode8_e2m1(v[c], sb);
+            if (live[c]) {
+                const uint64_t at = a.tiled ? tiled_code_offset((uint32_t)row, kc[c], pad.stages) : ((uint64_t)row * n + kc[c]) * 4u;
+                const uint64_t sat = a.tiled ? tiled_scale_offset((uint32_t)row, kc[c], pad.sstages) : ((uint64_t)row * n + kc[c]) >> 2;
+                *reinterpret_cast<uint32_t*>(a.codes + at) = codes;
+                if ((lane & 3u) == 0) a.scales[sat] = (uint8_t)sb;
+            }
+        }
+    }
+    if constexpr (QUANT) pad.zero(blockIdx.x * threads_of<W> + threadIdx.x, gridDim.x * threads_of<W>);
+}
+
+// Wavefronts to a row and chunks to a lane.
+struct Split { int w, c; };
+Split split_of(int64_t M, int64_t K) {
+    const int64_t waves = (K + 511) / 512;              // of one chunk a lane
+    Split s{1, 1};
+    while (s.w * s.c < waves) (s.w < 16 && (s.c >= 2 || M <= 256)) ? s.w *= 2 : s.c *= 2;
+    return s;
+}
+
+}  // namespace
+
+hipError_t launch_add_rms_norm(const NormArgs& a, bool quantize, hipStream_t stream) {
+    const Split sp = split_of(a.M, a.K);
+    const KPad pad = KPad::of(quantize && a.tiled, a.codes, a.scales, a.M, a.K);
+    switch (sp.w * 16 + sp.c) {
+#define BRQ_NORM(W, C)                                                                                                                             \
+    case W * 16 + C: {                                                                                                                             \
+        const dim3 grid((uint32_t)((a.M + rows_of<W> - 1) / rows_of<W>)), block(threads_of<W>);                                                    \
+        if (quantize) hipLaunchKernelGGL((k_add_rms_norm<W, C, true>), grid, block, 0, stream, a, pad);                                            \
+        else hipLaunchKernelGGL((k_add_rms_norm<W, C, false>), grid, block, 0, stream, a, pad);                                                    \
+        break;                                                                                                                                     \
+    }
+        BRQ_NORM(1, 1) BRQ_NORM(2, 1) BRQ_NORM(4, 1) BRQ_NORM(8, 1) BRQ_NORM(16, 1)
+        BRQ_NORM(1, 2) BRQ_NORM(2, 2) BRQ_NORM(4, 2) BRQ_NORM(8, 2) BRQ_NORM(16, 2)
+        BRQ_NORM(16, 4) BRQ_NORM(16, 8)
+#undef BRQ_NORM
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+namespace {
+
+// Backward.  With u = h r: dh = r (g - u mean(g u)) + gh, dw = sum over rows of gy u.  A row's wavefronts keep dw of their chunks in
+// registers over the rows that their workgroup goes through, and each workgroup writes one row of partial sums.
+template <int W, int C>
+__global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm_backward(const NormBackwardArgs a) {
+    __shared__ float part[2][threads_of<W> / 64][2];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), sub = wave % W;
+    const uint32_t chunk = chunk_of_lane(threadIdx.x & 63u), n = (uint32_t)(a.K / 8);
+    uint32_t kc[C];
+    bool in[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        kc[c] = (uint32_t)(c * W + sub) * 64u + chunk;
+        in[c] = kc[c] < n;
+        kc[c] = min(kc[c], n - 1);
+    }
+    float w[C][8], dw[C][8] = {};
+    if (a.w) load_weight(a.w, kc, w);
+    const float inv = 1.0f / (float)a.K;
+    int turn = 0;
+    // (uniform over the workgroup: every thread meets every barrier of row_sums)
+    for (int64_t first = (int64_t)blockIdx.x * rows_of<W>; first < a.M; first += (int64_t)gridDim.x * rows_of<W>) {
+        const int64_t mine = first + wave / W, row = mine < a.M ? mine : a.M - 1;
+        Raw<C> rh, rg;
+        rh.load(a.h.p + row * a.h.pitch, a.h.bf16, kc);
+        rg.load(a.gy.p + row * a.gy.pitch, a.gy.bf16, kc);
+        float h[C][8], g[C][8], sums[2] = {0.0f, 0.0f};
+        rh.widen(a.h.bf16, h);
+        rg.widen(a.gy.bf16, g);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float s = 0.0f, d = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s = __builtin_fmaf(h[c][i], h[c][i], s);
+                d = __builtin_fmaf(a.w ? g[c][i] * w[c][i] : g[c][i], h[c][i], d);
+            }
+            sums[0] += in[c] ? s : 0.0f;
+            sums[1] += in[c] ? d : 0.0f;
+        }
+        Raw<C> rd;
+        if (a.gh.p) rd.load(a.gh.p + row * a.gh.pitch, a.gh.bf16, kc);
+        // (the sums' places alternate: the next row's are written while others still read these)
+        row_sums<W, 2>(sums, part[turn], wave);
+        turn ^= 1;
+        const float r = 1.0f / sqrtf(sums[0] * inv + a.eps), mean = sums[1] * r * inv;
+        float d[C][8];
+        if (a.gh.p) rd.widen(a.gh.bf16, d);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const bool live = in[c] && mine < a.M;
+            float o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float u = h[c][i] * r;
+                dw[c][i] += live ? g[c][i] * u : 0.0f;
+                o[i] = r * ((a.w ? g[c][i] * w[c][i] : g[c][i]) - u * mean);
+                if (a.gh.p) o[i] += d[c][i];
+            }
+            if (live) store_values(a.dh.p + row * a.dh.pitch, a.dh.bf16, kc[c], o);
+        }
+    }
+    if (!a.partial) return;
+    if constexpr (rows_of<W> == 1) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (in[c]) store_values(reinterpret_cast<uint8_t*>(a.partial + (int64_t)blockIdx.x * a.K), false, kc[c], dw[c]);
+    } else {
+        __shared__ float sum[rows_of<W>][W * C * 512];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (in[c]) store_values(reinterpret_cast<uint8_t*>(sum[wave / W]), false, kc[c], dw[c]);
+        __syncthreads();
+        for (int k = (int)threadIdx.x; k < (int)a.K; k += threads_of<W>) {
+            float s = sum[0][k];
+#pragma unroll
+            for (int i = 1; i < rows_of<W>; ++i) s += sum[i][k];
+            a.partial[(int64_t)blockIdx.x * a.K + k] = s;
+        }
+    }
+}
+
+// dw: the sums of the partial sums' columns, 16 columns a workgroup, 64 threads each.
+__global__ __launch_bounds__(1024) void k_add_rms_norm_dw(const float* partial, int parts, int64_t K, float* dw) {
+    __shared__ float sum[64][17];
+    const int64_t k = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15u);
+    const int p0 = (int)(threadIdx.x >> 4);
+    float v = 0.0f;
+#pragma unroll 4
+    for (int p = p0; p < parts; p += 64) v += partial[(int64_t)p * K + k];
+    sum[p0][threadIdx.x & 15u] = v;
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) s += sum[i][threadIdx.x];
+        dw[k] = s;
+    }
+}
+
+// Of the backward pass: one chunk a lane as long as there are wavefronts, which leaves the fewest rows of partial sums.
+Split split_backward(int64_t K) {
+    const int64_t waves = (K + 511) / 512;
+    Split s{1, 1};
+    while (s.w * s.c < waves) s.w < 16 ? s.w *= 2 : s.c *= 2;
+    return s;
+}
+
+}  // namespace
+
+int64_t norm_backward_parts(int64_t M, int64_t K) {
+    const Split sp = split_backward(K);
+    const int64_t rows = sp.w < 4 ? 4 / sp.w : 1, n = (M + rows - 1) / rows, most = sp.w == 16 ? 256 : sp.w == 8 ? 512 : 1024;
+    return n < most ? n : most;
+}
+
+hipError_t launch_add_rms_norm_backward(const NormBackwardArgs& a, hipStream_t stream) {
+    const int parts = (int)norm_backward_parts(a.M, a.K);
+    if (a.M > 0) {
+        const Split sp = split_backward(a.K);
+        switch (sp.w * 16 + sp.c) {
+#define BRQ_BACK(W, C) case W * 16 + C: hipLaunchKernelGGL((k_add_rms_norm_backward<W, C>), dim3(parts), dim3(threads_of<W>), 0, stream, a); break;
+            BRQ_BACK(1, 1) BRQ_BACK(2, 1) BRQ_BACK(4, 1) BRQ_BACK(8, 1) BRQ_BACK(16, 1) BRQ_BACK(16, 2) BRQ_BACK(16, 4) BRQ_BACK(16, 8)
+#undef BRQ_BACK
+            default: return hipErrorInvalidValue;
+        }
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    if (!a.dw) return hipSuccess;
+    hipLaunchKernelGGL(k_add_rms_norm_dw, dim3((uint32_t)(a.K / 16)), dim3(1024), 0, stream, a.partial, parts, a.K, a.dw);
+    return hipGetLastError();
+}
+
+}  // namespace brq

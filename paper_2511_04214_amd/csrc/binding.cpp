@@ -23,6 +23,7 @@
 
 #include "../../include/brq.h"
 #include "../../include/brq_attn.h"
+#include "../../include/brq_residual.h"
 
 namespace {
 
@@ -818,11 +819,195 @@ PyObject* bind_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// ---- the residual side (brq_residual.h)
+
+decltype(&brq_add_rms_norm) f_add_norm;
+decltype(&brq_add_rms_norm_backward) f_add_norm_back;
+decltype(&brq_add_rms_norm_backward_workspace) f_add_norm_back_space;
+decltype(&brq_add_rms_norm_rotate_quantize_fused) f_add_norm_quantize;
+decltype(&brq_mxfp4_gemm_epilogue) f_gemm_epilogue;
+bool g_residual;                     // bind_residual() was called
+
+// A matrix of a call, or one to be made: rows of any pitch.
+struct Matrix {
+    at::Tensor t;                    // undefined: None
+    int64_t ld = 0;
+    brq_dtype dt = BRQ_F32;
+    void fill() { ld = t.size(0) > 1 ? t.stride(0) : t.size(1); }
+    void* p() const { return t.defined() ? t.data_ptr() : nullptr; }
+};
+bool matrix(Call& c, PyObject* o, Matrix* x, bool optional = false) {
+    if (optional && o == Py_None) return true;
+    const at::Tensor* t = c.take(o);
+    if (!t || t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1) || !dtype_of(t->scalar_type(), &x->dt)) return false;
+    x->t = *t;
+    x->fill();
+    return true;
+}
+bool same_sizes(const Matrix& a, const Matrix& b) { return !b.t.defined() || a.t.sizes() == b.t.sizes(); }
+// `o`, of `like`'s sizes and type `s`, or a new one.
+bool matrix_out(Call& c, PyObject* o, const Matrix& like, at::ScalarType s, Matrix* x) {
+    if (o != Py_None) return matrix(c, o, x) && same_sizes(like, *x) && x->t.scalar_type() == s;
+    if (!make(c, like.t.sizes(), s, &x->t)) return false;
+    x->fill();
+    return dtype_of(s, &x->dt);
+}
+// The sum of x and the residual: none without a residual, and where nobody asks for it.
+bool sum_out(Call& c, PyObject* h_out, PyObject* want, const Matrix& x, const Matrix& res, Matrix* h) {
+    if (!PyBool_Check(want)) return false;
+    if (!res.t.defined()) return h_out == Py_None;
+    return (h_out == Py_None && want == Py_False) || matrix_out(c, h_out, x, res.t.scalar_type(), h);
+}
+
+// add_rms_norm(x, residual, weight, eps, out_dtype, out, h_out, want_h)
+PyObject* add_rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    Matrix x, res, y, h;
+    at::Tensor w;
+    double eps;
+    at::ScalarType s;
+    brq_dtype dt;
+    if (n != 8 || !g_residual || !quiet() || !matrix(c, a[0], &x) || !matrix(c, a[1], &res, true) || !same_sizes(x, res) ||
+        !array_of(c, a[2], at::kFloat, {x.t.size(1)}, &w, true) || !number(a[3], &eps)) Py_RETURN_NONE;
+    if (a[5] != Py_None) {
+        const at::Tensor* t = c.take(a[5]);
+        if (!t) Py_RETURN_NONE;
+        s = t->scalar_type();
+    } else if (a[4] == Py_None) {
+        s = x.t.scalar_type();
+    } else if (!dtype_arg(a[4], &s, &dt)) {
+        Py_RETURN_NONE;
+    }
+    if (!matrix_out(c, a[5], x, s, &y) || !sum_out(c, a[6], a[7], x, res, &h)) Py_RETURN_NONE;
+    void* st = current_stream();
+    const brq_status r = released([&] {
+        return f_add_norm(x.p(), x.dt, x.ld, res.p(), res.dt, res.ld, x.t.size(0), x.t.size(1), address<float>(w), (float)eps, h.p(), h.ld, y.p(), y.dt, y.ld, st);
+    });
+    if (r != BRQ_OK) return status(r);
+    PyObject* items[2] = {wrapped(a[5], y.t), wrapped(a[6], h.t)};
+    return tuple_of(items);
+    END_HANDLE_TH_ERRORS
+}
+
+// add_rms_norm_backward(h, gy, gh, weight, eps, dh, workspace)
+PyObject* add_rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    Matrix h, gy, gh, dh;
+    at::Tensor w, dw, space;
+    double eps;
+    if (n != 7 || !g_residual || !quiet() || !matrix(c, a[0], &h) || !matrix(c, a[1], &gy) || !matrix(c, a[2], &gh, true) || !same_sizes(h, gy) || !same_sizes(h, gh) ||
+        (gh.t.defined() && gh.dt != h.dt) || !array_of(c, a[3], at::kFloat, {h.t.size(1)}, &w, true) || !number(a[4], &eps) ||
+        !array_of(c, a[6], at::kByte, {-1}, &space, true) || !matrix_out(c, a[5], h, h.t.scalar_type(), &dh)) Py_RETURN_NONE;
+    const int64_t M = h.t.size(0), K = h.t.size(1);
+    if (w.defined()) {
+        int64_t need = 0;
+        if (const brq_status r = f_add_norm_back_space(M, K, &need); r != BRQ_OK) return status(r);
+        if ((need && !make(c, {need}, at::kByte, &space)) || !make(c, {K}, at::kFloat, &dw)) Py_RETURN_NONE;
+    }
+    void* st = current_stream();
+    const brq_status r = released([&] {
+        return f_add_norm_back(h.p(), h.dt, h.ld, gy.p(), gy.dt, gy.ld, gh.p(), gh.ld, M, K, address<float>(w), (float)eps, dh.p(), dh.ld, address<float>(dw),
+                               address<void>(space), space.defined() ? space.numel() : 0, st);
+    });
+    if (r != BRQ_OK) return status(r);
+    PyObject* items[2] = {wrapped(a[5], dh.t), wrapped(Py_None, dw)};
+    return tuple_of(items);
+    END_HANDLE_TH_ERRORS
+}
+
+// add_rms_norm_rotate_quantize(x, B, residual, weight, eps, y_dtype, h_out, want_h, codes, scales, layout, signs)
+PyObject* add_rms_norm_rotate_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    Matrix x, res, h;
+    at::Tensor w;
+    double eps;
+    int64_t B;
+    at::ScalarType s;
+    brq_dtype dt;
+    brq_layout l;
+    const int8_t* signs;
+    uint8_t *codes, *scales;
+    if (n != 12 || !g_residual || !quiet() || !matrix(c, a[0], &x) || !integer(a[1], &B) || !matrix(c, a[2], &res, true) || !same_sizes(x, res) ||
+        !array_of(c, a[3], at::kFloat, {x.t.size(1)}, &w, true) || !number(a[4], &eps) || !dtype_arg(a[5], &s, &dt) || a[8] == Py_None || a[9] == Py_None ||
+        !c.take(a[8]) || !c.take(a[9]) || (a[11] != Py_None && !c.take(a[11])) || !layout(a[10], &l) || !signs_arg(a[11], x.t.size(1), &signs) ||
+        !buffers(a[8], a[9], x.t.size(0), x.t.size(1), l, &codes, &scales) || !sum_out(c, a[6], a[7], x, res, &h)) Py_RETURN_NONE;
+    if (signs) signs = reinterpret_cast<const int8_t*>(data(a[11]));
+    codes = const_cast<uint8_t*>(data(a[8]));
+    scales = const_cast<uint8_t*>(data(a[9]));
+    void* st = current_stream();
+    const brq_status r = released([&] {
+        return f_add_norm_quantize(x.p(), x.dt, x.ld, res.p(), res.dt, res.ld, x.t.size(0), x.t.size(1), address<float>(w), (float)eps, h.p(), h.ld, dt, B, signs, codes,
+                                   scales, l, st);
+    });
+    if (r != BRQ_OK) return status(r);
+    Py_INCREF(a[8]);
+    Py_INCREF(a[9]);
+    PyObject* items[3] = {a[8], a[9], wrapped(a[6], h.t)};
+    return tuple_of(items);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *s_relu, *s_silu, *s_gelu;
+bool activation(PyObject* o, brq_activation* v) {
+    *v = BRQ_ACT_NONE;
+    if (o == Py_None) return true;
+    if (!PyUnicode_CheckExact(o)) return false;
+    auto is = [&](PyObject* s) { return o == s || PyUnicode_Compare(o, s) == 0; };
+    *v = is(s_relu) ? BRQ_ACT_RELU : is(s_silu) ? BRQ_ACT_SILU : is(s_gelu) ? BRQ_ACT_GELU : BRQ_ACT_NONE;
+    return *v != BRQ_ACT_NONE;
+}
+
+// gemm_epilogue(aq, as, wq, ws, bias, activation, residual, out_dtype, out, a_layout, w_layout, M, N, K)
+PyObject* gemm_epilogue(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Call c;
+    brq_layout la, lw;
+    int64_t M, N, K;
+    at::Tensor bias, y;
+    Matrix res;
+    brq_activation act;
+    brq_dtype dt;
+    int64_t ldy;
+    if (n != 14 || !g_residual || !quiet() || !c.take(a[0]) || !c.take(a[1]) || !c.take(a[2]) || !c.take(a[3]) || (a[8] != Py_None && !c.take(a[8])) || !layout(a[9], &la) ||
+        !layout(a[10], &lw) || !size_arg(a[11], &M) || !size_arg(a[12], &N) || !size_arg(a[13], &K) || !operand(a[0], a[1], la, &M, &K) ||
+        !operand(a[2], a[3], lw, &N, &K) || M < 0 || N < 0 || K < 0 || !operand_fits(a[0], a[1], la, M, K) || !operand_fits(a[2], a[3], lw, N, K) ||
+        !array_of(c, a[4], at::kFloat, {N}, &bias, true) || !activation(a[5], &act) || !matrix(c, a[6], &res, true) ||
+        (res.t.defined() && (res.t.size(0) != M || res.t.size(1) != N)) || !result(a[8], a[7], THPVariable_Unpack(a[0]), M, N, &y, &dt, &ldy)) Py_RETURN_NONE;
+    const uint8_t *ac = data(a[0]), *as = data(a[1]), *wc = data(a[2]), *ws = data(a[3]);
+    void *p = y.data_ptr(), *s = current_stream();
+    return result_or(released([&] { return f_gemm_epilogue(ac, as, la, wc, ws, lw, M, N, K, address<float>(bias), act, res.p(), res.dt, res.ld, p, dt, ldy, s); }), a[8], y);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* bind_residual(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void* p[5];
+    if (n != 5) {
+        PyErr_SetString(PyExc_TypeError, "bind_residual takes the addresses of five entry points");
+        return nullptr;
+    }
+    for (int i = 0; i < 5; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (!p[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an entry point's address is NULL");
+            return nullptr;
+        }
+    }
+    int i = 0;
+    auto set = [&](auto& f) { f = reinterpret_cast<std::decay_t<decltype(f)>>(p[i++]); };
+    set(f_add_norm), set(f_add_norm_back), set(f_add_norm_back_space), set(f_add_norm_quantize), set(f_gemm_epilogue);
+    g_residual = true;
+    Py_RETURN_NONE;
+}
+
 #define BRQ_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {BRQ_METHOD(bind), BRQ_METHOD(rotate_quantize), BRQ_METHOD(swiglu_rotate_quantize), BRQ_METHOD(matrix_rotate_quantize),
                          BRQ_METHOD(gemm), BRQ_METHOD(rotate_quantize_gemm), BRQ_METHOD(bind_stats), BRQ_METHOD(block_stats), BRQ_METHOD(block_stats_summary),
                          BRQ_METHOD(bind_attention), BRQ_METHOD(qk_norm_rope), BRQ_METHOD(qk_norm_rope_backward), BRQ_METHOD(kv4_append), BRQ_METHOD(kv4_read), BRQ_METHOD(kv4_attention),
-                         BRQ_METHOD(kv4_pages_copy), BRQ_METHOD(kv4_pages_fork), BRQ_METHOD(kv4_pages_free), BRQ_METHOD(kv4_pages_reserve), BRQ_METHOD(kv4_pages_compact), {nullptr, nullptr, 0, nullptr}};
+                         BRQ_METHOD(kv4_pages_copy), BRQ_METHOD(kv4_pages_fork), BRQ_METHOD(kv4_pages_free), BRQ_METHOD(kv4_pages_reserve), BRQ_METHOD(kv4_pages_compact),
+                         BRQ_METHOD(bind_residual), BRQ_METHOD(add_rms_norm), BRQ_METHOD(add_rms_norm_backward), BRQ_METHOD(add_rms_norm_rotate_quantize), BRQ_METHOD(gemm_epilogue), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -830,7 +1015,10 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, n
 PyMODINIT_FUNC PyInit__binding() {
     s_rowmajor = PyUnicode_InternFromString("rowmajor");
     s_tiled = PyUnicode_InternFromString("tiled");
-    if (!s_rowmajor || !s_tiled) return nullptr;
+    s_relu = PyUnicode_InternFromString("relu");
+    s_silu = PyUnicode_InternFromString("silu");
+    s_gelu = PyUnicode_InternFromString("gelu");
+    if (!s_rowmajor || !s_tiled || !s_relu || !s_silu || !s_gelu) return nullptr;
     PyObject* m = PyModule_Create(&module);
     // The torch whose headers this was built with: tensors are read through them, so no other will do.
     if (m && PyModule_AddStringConstant(m, "TORCH", BRQ_TORCH) != 0) Py_CLEAR(m);

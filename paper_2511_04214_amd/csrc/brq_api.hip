@@ -73,6 +73,20 @@ brq_status launched(hipError_t e) { return e == hipSuccess ? BRQ_OK : BRQ_ERR_LA
 
 }  // namespace
 
+brq_status brq::check_gemm(const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq,
+                            const uint8_t* ws, brq_layout w_layout, int64_t M, int64_t N, int64_t K, const void* y,
+                            brq_dtype ydt, int64_t ldy) {
+    int es = dtype_size(ydt);
+    if (es == 0) return BRQ_ERR_DTYPE;
+    if (!layout_ok(a_layout) || !layout_ok(w_layout)) return BRQ_ERR_LAYOUT;
+    if (M < 0 || N < 0 || K <= 0 || K % 32 != 0 || ldy < N) return BRQ_ERR_SHAPE;
+    if (M >= (int64_t(1) << 31) || N >= (int64_t(1) << 31) || K >= (int64_t(1) << 31)) return BRQ_ERR_SHAPE;
+    if (M > 0 && N > 0 && (!aq || !as || !wq || !ws || !y)) return BRQ_ERR_NULL;
+    if (!aligned16(aq) || !aligned16(as) || !aligned16(wq) || !aligned16(ws) || !aligned16(y))
+        return BRQ_ERR_ALIGN;
+    return BRQ_OK;
+}
+
 extern "C" {
 
 brq_status brq_init(void) {
@@ -243,24 +257,10 @@ brq_status brq_matrix_rotate_quantize_fused(const void* x, brq_dtype xdt, int64_
                                               layout == BRQ_LAYOUT_TILED, static_cast<hipStream_t>(stream)));
 }
 
-static brq_status check_gemm(const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq,
-                             const uint8_t* ws, brq_layout w_layout, int64_t M, int64_t N, int64_t K, const void* y,
-                             brq_dtype ydt, int64_t ldy) {
-    int es = dtype_size(ydt);
-    if (es == 0) return BRQ_ERR_DTYPE;
-    if (!layout_ok(a_layout) || !layout_ok(w_layout)) return BRQ_ERR_LAYOUT;
-    if (M < 0 || N < 0 || K <= 0 || K % 32 != 0 || ldy < N) return BRQ_ERR_SHAPE;
-    if (M >= (int64_t(1) << 31) || N >= (int64_t(1) << 31) || K >= (int64_t(1) << 31)) return BRQ_ERR_SHAPE;
-    if (M > 0 && N > 0 && (!aq || !as || !wq || !ws || !y)) return BRQ_ERR_NULL;
-    if (!aligned16(aq) || !aligned16(as) || !aligned16(wq) || !aligned16(ws) || !aligned16(y))
-        return BRQ_ERR_ALIGN;
-    return BRQ_OK;
-}
-
 brq_status brq_diag_mxfp4_gemm_clock(const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq,
                                      const uint8_t* ws, brq_layout w_layout, int64_t M, int64_t N, int64_t K, void* y,
                                      brq_dtype ydt, int64_t ldy, uint64_t* clock, void* stream) {
-    brq_status st = check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy);
+    brq_status st = brq::check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy);
     if (st != BRQ_OK) return st;
     if (!clock) return BRQ_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(clock) & 7u) return BRQ_ERR_ALIGN;
@@ -278,7 +278,7 @@ brq_status brq_diag_mxfp4_gemm_clock(const uint8_t* aq, const uint8_t* as, brq_l
 brq_status brq_diag_mxfp4_gemm_no_loads(const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq,
                                         const uint8_t* ws, brq_layout w_layout, int64_t M, int64_t N, int64_t K, void* y,
                                         brq_dtype ydt, int64_t ldy, uint64_t* clock, void* stream) {
-    brq_status st = check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy);
+    brq_status st = brq::check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy);
     if (st != BRQ_OK) return st;
     if (!clock) return BRQ_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(clock) & 7u) return BRQ_ERR_ALIGN;
@@ -294,7 +294,7 @@ brq_status brq_diag_mxfp4_gemm_no_loads(const uint8_t* aq, const uint8_t* as, br
 brq_status brq_mxfp4_gemm(const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq,
                           const uint8_t* ws, brq_layout w_layout, int64_t M, int64_t N, int64_t K, void* y,
                           brq_dtype ydt, int64_t ldy, void* stream) {
-    brq_status st = check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy);
+    brq_status st = brq::check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy);
     if (st != BRQ_OK) return st;
     if (M == 0 || N == 0) return BRQ_OK;
     const brq::Operand a{aq, as, a_layout == BRQ_LAYOUT_TILED}, w{wq, ws, w_layout == BRQ_LAYOUT_TILED};
@@ -304,7 +304,7 @@ brq_status brq_mxfp4_gemm(const uint8_t* aq, const uint8_t* as, brq_layout a_lay
 brq_status brq_diag_mxfp4_gemm_route(brq_layout a_layout, brq_layout w_layout, int64_t M, int64_t N, int64_t K, brq_dtype ydt,
                                      int64_t ldy, int64_t cus, int32_t* route) {
     alignas(16) static const uint8_t operand[16] = {};      // (nothing is launched: any aligned address will do)
-    brq_status st = check_gemm(operand, operand, a_layout, operand, operand, w_layout, M, N, K, operand, ydt, ldy);
+    brq_status st = brq::check_gemm(operand, operand, a_layout, operand, operand, w_layout, M, N, K, operand, ydt, ldy);
     if (st != BRQ_OK) return st;
     if (!route) return BRQ_ERR_NULL;
     if (M == 0 || N == 0 || cus < 1 || cus >= (int64_t(1) << 31)) return BRQ_ERR_SHAPE;
@@ -315,7 +315,7 @@ brq_status brq_diag_mxfp4_gemm_route(brq_layout a_layout, brq_layout w_layout, i
 brq_status brq_diag_mxfp4_gemm_on(int32_t route, const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq,
                                   const uint8_t* ws, brq_layout w_layout, int64_t M, int64_t N, int64_t K, void* y,
                                   brq_dtype ydt, int64_t ldy, void* stream) {
-    brq_status st = check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy);
+    brq_status st = brq::check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy);
     if (st != BRQ_OK) return st;
     const brq::Operand a{aq, as, a_layout == BRQ_LAYOUT_TILED}, w{wq, ws, w_layout == BRQ_LAYOUT_TILED};
     const brq::GemmShape g{M, N, K, a.tiled, w.tiled, ydt == BRQ_BF16, ldy, reinterpret_cast<uintptr_t>(y)};
@@ -375,6 +375,7 @@ const char* brq_strerror(brq_status s) {
         case BRQ_ERR_LAUNCH: return "kernel launch failed";
         case BRQ_ERR_LAYOUT: return "unknown operand layout";
         case BRQ_ERR_DEVICE: return "no usable HIP device, or its one-time set-up failed";
+        case BRQ_ERR_ACTIVATION: return "unknown activation";
         case BRQ_STATUS_INT_RANGE_: break;
     }
     return "unknown status";

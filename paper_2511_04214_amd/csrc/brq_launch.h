@@ -3,7 +3,13 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/brq.h"
+
 namespace brq {
+
+// The arguments that every product has (brq_api.hip).
+brq_status check_gemm(const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq, const uint8_t* ws, brq_layout w_layout,
+                      int64_t M, int64_t N, int64_t K, const void* y, brq_dtype ydt, int64_t ldy);
 
 // Per-device facts and one-time set-up.  The launchers size their grids by the number of compute units
 // and four kernel families ask for more than the default 64 KB of LDS, which HIP wants declared per
@@ -13,6 +19,7 @@ namespace brq {
 hipError_t device_cus(int* cus);
 hipError_t setup_gemm_tiled();     // mxfp4_gemm_tiled.hip
 hipError_t setup_gemm_mid();       // mxfp4_gemm_mid.hip
+hipError_t setup_gemm_mid_with();  // mxfp4_gemm_mid_with.hip, called by the former
 hipError_t setup_matrix_rotate();  // matrix_rotate_quant.hip
 hipError_t setup_gemm_decode_fused();   // mxfp4_gemm.hip
 
@@ -69,6 +76,7 @@ struct GemmShape {
     bool a_tiled, w_tiled, out_bf16;
     int64_t ldy;
     uintptr_t y;
+    bool epilogue = false;      // something follows the product: the persistent kernels do not take it
     int64_t padded_k() const { return (K + 511) / 512 * 512; }
     // K of whole 512-element superstages: tiled operands are zero-padded to that
     bool whole_k() const { return K % 512 == 0 || (a_tiled && w_tiled); }
@@ -79,9 +87,18 @@ enum GemmRoute { ROUTE_GENERAL, ROUTE_SKINNY, ROUTE_STREAM, ROUTE_256x256, ROUTE
 bool gemm_route_supported(int route, const GemmShape& g);
 // The route of a product on a device of `cus` compute units: host arithmetic.
 int gemm_route(const GemmShape& g, int cus);
-hipError_t launch_mxfp4_gemm(const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s);
+// What follows a product: y = act(p + bias) + residual.
+enum Activation { ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU };     // the numbers of brq_residual.h
+struct Epilogue {
+    const float* bias;          // [N] or null
+    const uint8_t* res;         // [M] rows res_pitch bytes apart, or null
+    int64_t res_pitch;
+    int res_bf16, act, out_bf16;
+};
+// epi: null, or what follows (g.epilogue says whether).
+hipError_t launch_mxfp4_gemm(const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi = nullptr);
 // The same on a route that takes the shape (gemm_route_supported), device_cus() having been called.
-hipError_t launch_gemm_route(int route, const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s);
+hipError_t launch_gemm_route(int route, const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi = nullptr);
 
 // The decode-size product with the online step (B = 32 rotation + quantizer) of its activations in its own
 // prologue: x [M <= 16][ldx] bf16 or fp32, K % 512 == 0, K <= DECODE_FUSED_MAX_K (the quantized activations of
@@ -104,14 +121,20 @@ hipError_t launch_gemm_tiled(const Operand& a, const Operand& w, int64_t M, int6
 bool mid_gemm_supported(int tile, const GemmShape& g);
 bool mid_gemm_pairs(int tile, bool both_tiled, int64_t K);       // whether it loads its stages in pairs
 hipError_t launch_gemm_mid(int tile, const Operand& a, const Operand& w, int64_t M, int64_t N, int64_t K, void* y,
-                           bool out_bf16, int64_t ldy, hipStream_t s);
+                           bool out_bf16, int64_t ldy, hipStream_t s, const Epilogue* epi = nullptr);
 
 // The same for any K of at least 256 elements and any mix of layouts, 64 or 128 rows x 128 columns a workgroup.  It takes its
 // operands in pairs of stages, 8 groups: where pair t's eight scale bytes begin, from the row's first (of a row-major row's last pair the
 // row's last eight).
 constexpr int64_t pair_scales(bool tiled, int t, int groups) { return tiled ? (int64_t)(t >> 1) * 1024 + (t & 1) * 8 : 8 * t < groups - 8 ? 8 * t : groups - 8; }
 hipError_t launch_gemm_any_k(const Operand& a, const Operand& w, int64_t M, int64_t N, int64_t K, void* y, bool out_bf16, int64_t ldy,
-                             hipStream_t s);
+                             hipStream_t s, const Epilogue* epi = nullptr);
+
+// The two with what follows the product (mxfp4_gemm_mid_with.hip).
+hipError_t launch_gemm_any_k_with(const Operand& a, const Operand& w, int64_t M, int64_t N, int64_t K, void* y, bool out_bf16, int64_t ldy,
+                                  hipStream_t s, const Epilogue& epi);
+hipError_t launch_gemm_mid_with(int tile, const Operand& a, const Operand& w, int64_t M, int64_t N, int64_t K, void* y,
+                                bool out_bf16, int64_t ldy, hipStream_t s, const Epilogue& epi);
 
 // Tiled -> row-major copy of a quantized operand.
 hipError_t launch_to_rowmajor(const uint8_t* codes_t, const uint8_t* scales_t, int64_t rows, int64_t K,

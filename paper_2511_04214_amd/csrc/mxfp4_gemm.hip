@@ -8,8 +8,7 @@
 // (row 8*(i/4) + 4*(l>>5) + i%4, column l & 31).  The 16x16x128 form: row (l & 15), group
 // (l >> 4); accumulator i is (row 4*(l>>4) + i, column l & 15).
 #include <type_traits>
-#include "mfma_fp4.h"
-#include "brq_launch.h"
+#include "gemm_epilogue.h"
 
 namespace brq {
 
@@ -44,13 +43,36 @@ __device__ __forceinline__ void store_out(void* y, bool out_bf16, int64_t idx, f
     else reinterpret_cast<float*>(y)[idx] = v;
 }
 
+// N elements of column col, rows row_of(i), with what follows the product: all their residuals are asked for before the first is used.
+// Every lane calls, and all values are made here in front of the branch: the compiler moves what only some lanes need behind the branch that they
+// take, products and their scales too, and a scale that its lane has not made is another row's factor.
+template <int N, class F>
+__device__ __forceinline__ void store_column(const Epilogue& e, float (&v)[N], void* y, bool out_bf16, int64_t ldy, int M, int cols, int col, F row_of) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+    if (col >= cols) return;
+    float r[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = e.res && row_of(i) < M ? residual_at(e, row_of(i), col) : 0.0f;
+    if (e.bias) {
+        const float b = e.bias[col];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += b;
+    }
+    activate(v, e.act);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (row_of(i) < M) store_out(y, out_bf16, (int64_t)row_of(i) * ldy + col, e.res ? v[i] + r[i] : v[i]);
+}
+
 // ---- general shapes: one 32x32 output tile per wavefront, operands straight from global ----
 // The K groups are taken in the order of the LDS-staged kernels (step j of a 128-element stage: groups j and 2 + j),
 // so that a product does not depend on which of them it runs on.
+template <bool EPI>
 __global__ void __launch_bounds__(256) k_gemm_direct(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as,
                                                      int a_tiled, const uint8_t* __restrict__ wq,
                                                      const uint8_t* __restrict__ ws, int w_tiled, int M, int N, int K,
-                                                     void* __restrict__ y, int out_bf16, int64_t ldy) {
+                                                     void* y, int out_bf16, int64_t ldy, EpilogueArg<EPI> epi) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int m0 = blockIdx.y * 64 + (wave >> 1) * 32, n0 = blockIdx.x * 64 + (wave & 1) * 32;
     if (m0 >= M || n0 >= N) return;   // whole wavefront leaves together
@@ -73,6 +95,13 @@ __global__ void __launch_bounds__(256) k_gemm_direct(const uint8_t* __restrict__
         acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 4, 0, sca, 0, scb);
     }
     const int col = n0 + r;
+    if constexpr (EPI) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = acc[i];
+        store_column(epi.e, v, y, out_bf16, ldy, M, N, col, [&](int i) { return m0 + 8 * (i / 4) + 4 * h + (i % 4); });
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         int row = m0 + 8 * (i / 4) + 4 * h + (i % 4);
@@ -83,10 +112,11 @@ __global__ void __launch_bounds__(256) k_gemm_direct(const uint8_t* __restrict__
 // ---- M <= 16 (decode): weight streaming, 16 output columns per workgroup -------------------
 // Each of the 4 wavefronts takes every 4th 128-wide K step for the same 16 weight rows; the
 // partial 16x16 tiles are summed through LDS in a fixed order.
+template <bool EPI>
 __global__ void __launch_bounds__(256) k_gemm_skinny(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as,
                                                      int a_tiled, const uint8_t* __restrict__ wq,
                                                      const uint8_t* __restrict__ ws, int w_tiled, int M, int N, int K,
-                                                     void* __restrict__ y, int out_bf16, int64_t ldy) {
+                                                     void* y, int out_bf16, int64_t ldy, EpilogueArg<EPI> epi) {
     __shared__ float part[4][64][4];
     load_args(aq, as, a_tiled, wq, ws, w_tiled, M, N, K, y, out_bf16, ldy);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -118,6 +148,13 @@ __global__ void __launch_bounds__(256) k_gemm_skinny(const uint8_t* __restrict__
     __syncthreads();
     if (wave == 0) {
         const int col = n0 + r;
+        if constexpr (EPI) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = ((part[0][lane][i] + part[1][lane][i]) + part[2][lane][i]) + part[3][lane][i];
+            store_column(epi.e, v, y, out_bf16, ldy, M, N, col, [&](int i) { return 4 * kq + i; });
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float s = ((part[0][lane][i] + part[1][lane][i]) + part[2][lane][i]) + part[3][lane][i];
@@ -217,11 +254,11 @@ constexpr int smallm_lds_bytes(int sets, bool rows) { return sets * smallm_buf_b
 // TAIL = (K / 512) % SETS: the superstages left after the main loop, which takes them SETS at a time in
 // one basic block (no load behind a branch: the compiler's count of the outstanding weight loads is
 // then exact; with early exits inside the loop it falls back to waiting for all of them).
-template <bool ROWS, int SETS, int TAIL>
+template <bool ROWS, int SETS, int TAIL, bool EPI>
 __global__ void __launch_bounds__(256) k_gemm_smallm(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as,
                                                      int a_tiled, const uint8_t* __restrict__ wq,
                                                      const uint8_t* __restrict__ ws, int M, int N, int K,
-                                                     void* __restrict__ y, int out_bf16, int64_t ldy, int nw) {
+                                                     void* y, int out_bf16, int64_t ldy, int nw, EpilogueArg<EPI> epi) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int STG = 1024;                           // one stage of A codes: 16 rows x 64 bytes
     constexpr int BUF = smallm_buf_bytes;               // codes [4 stages][16 rows][64], then scales, 1 KB per wavefront
@@ -345,6 +382,13 @@ __global__ void __launch_bounds__(256) k_gemm_smallm(const uint8_t* __restrict__
     static_for([&](auto Kc) __attribute__((always_inline)) { turn(Kc, IC<D - 1 - decltype(Kc)::value>{}, No{}, ss + decltype(Kc)::value); }, IC<TAIL>{});
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the repeated loads land before the LDS is released
     const int col = n0 + r;
+    if constexpr (EPI) {
+        float v[8];                                     // rows 0 .. 15: the others do not exist
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = acc[i];
+        store_column(epi.e, v, y, out_bf16, ldy, M, N, col, [&](int i) { return 8 * (i / 4) + 4 * h + (i % 4); });
+        return;
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -540,13 +584,16 @@ hipError_t launch_mfma_ceiling(const uint8_t* operands, int iters, int workgroup
     return hipGetLastError();
 }
 
-using SmallmKern = void (*)(const uint8_t*, const uint8_t*, int, const uint8_t*, const uint8_t*, int, int, int, void*, int, int64_t, int);
+template <bool EPI>
+using SmallmKern = void (*)(const uint8_t*, const uint8_t*, int, const uint8_t*, const uint8_t*, int, int, int, void*, int, int64_t, int, EpilogueArg<EPI>);
 constexpr int FEW = 3, MANY = 5;      // register sets
-#define BRQ_FEW(ROWS) {k_gemm_smallm<ROWS, FEW, 0>, k_gemm_smallm<ROWS, FEW, 1>, k_gemm_smallm<ROWS, FEW, 2>}
-#define BRQ_MANY(ROWS) {k_gemm_smallm<ROWS, MANY, 0>, k_gemm_smallm<ROWS, MANY, 1>, k_gemm_smallm<ROWS, MANY, 2>, k_gemm_smallm<ROWS, MANY, 3>, \
-                        k_gemm_smallm<ROWS, MANY, 4>}
-static const SmallmKern smallm_few[2][FEW] = {BRQ_FEW(false), BRQ_FEW(true)};          // [weights row-major][K / 512 % sets]
-static const SmallmKern smallm_many[2][MANY] = {BRQ_MANY(false), BRQ_MANY(true)};
+#define BRQ_FEW(ROWS) {k_gemm_smallm<ROWS, FEW, 0, EPI>, k_gemm_smallm<ROWS, FEW, 1, EPI>, k_gemm_smallm<ROWS, FEW, 2, EPI>}
+#define BRQ_MANY(ROWS) {k_gemm_smallm<ROWS, MANY, 0, EPI>, k_gemm_smallm<ROWS, MANY, 1, EPI>, k_gemm_smallm<ROWS, MANY, 2, EPI>, \
+                        k_gemm_smallm<ROWS, MANY, 3, EPI>, k_gemm_smallm<ROWS, MANY, 4, EPI>}
+template <bool EPI>
+static const SmallmKern<EPI> smallm_few[2][FEW] = {BRQ_FEW(false), BRQ_FEW(true)};          // [weights row-major][K / 512 % sets]
+template <bool EPI>
+static const SmallmKern<EPI> smallm_many[2][MANY] = {BRQ_MANY(false), BRQ_MANY(true)};
 #undef BRQ_FEW
 #undef BRQ_MANY
 using DecodeKern = void (*)(const void*, int64_t, const int8_t*, const uint8_t*, const uint8_t*, int, int, int, int, void*, int, int64_t, int);
@@ -652,7 +699,7 @@ bool gemm_route_supported(int route, const GemmShape& g) {
         case ROUTE_SKINNY: return g.M <= 16;
         case ROUTE_STREAM: return g.M <= 16 && g.whole_k() && g.padded_k() < (int64_t(1) << 26);
         case ROUTE_256x256:
-        case ROUTE_128x256: return tiled_gemm_supported(g.M, g.N, g.K, g.out_bf16, g.ldy, g.a_tiled && g.w_tiled);
+        case ROUTE_128x256: return !g.epilogue && tiled_gemm_supported(g.M, g.N, g.K, g.out_bf16, g.ldy, g.a_tiled && g.w_tiled);
         case ROUTE_ANY_K: return g.K >= 256;
         default: return route >= ROUTE_ONE_TILE && route < ROUTE_ANY_K && mid_gemm_supported(route - ROUTE_ONE_TILE, g);
     }
@@ -704,38 +751,48 @@ int gemm_route(const GemmShape& g, int cus) {
     return t >= 0 ? t : g.M <= 16 ? ROUTE_SKINNY : any_k(g) ? ROUTE_ANY_K : ROUTE_GENERAL;
 }
 
-hipError_t launch_gemm_route(int route, const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s) {
+// The kernels of this file; EPI: with what follows the product.
+template <bool EPI>
+static hipError_t launch_here(int route, const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, EpilogueArg<EPI> epi) {
     const int64_t M = g.M, N = g.N, K = g.K;
     switch (route) {
         case ROUTE_GENERAL:
-            hipLaunchKernelGGL(k_gemm_direct, dim3((uint32_t)((N + 63) / 64), (uint32_t)((M + 63) / 64)), dim3(256), 0, s, a.codes, a.scales,
-                               (int)a.tiled, w.codes, w.scales, (int)w.tiled, (int)M, (int)N, (int)K, y, (int)g.out_bf16, g.ldy);
+            hipLaunchKernelGGL(k_gemm_direct<EPI>, dim3((uint32_t)((N + 63) / 64), (uint32_t)((M + 63) / 64)), dim3(256), 0, s, a.codes, a.scales,
+                               (int)a.tiled, w.codes, w.scales, (int)w.tiled, (int)M, (int)N, (int)K, y, (int)g.out_bf16, g.ldy, epi);
             return hipGetLastError();
-        case ROUTE_ANY_K: return launch_gemm_any_k(a, w, M, N, K, y, g.out_bf16, g.ldy, s);
         case ROUTE_SKINNY:
-            hipLaunchKernelGGL(k_gemm_skinny, dim3((uint32_t)((N + 15) / 16)), dim3(256), 0, s, a.codes, a.scales, (int)a.tiled, w.codes,
-                               w.scales, (int)w.tiled, (int)M, (int)N, (int)K, y, (int)g.out_bf16, g.ldy);
+            hipLaunchKernelGGL(k_gemm_skinny<EPI>, dim3((uint32_t)((N + 15) / 16)), dim3(256), 0, s, a.codes, a.scales, (int)a.tiled, w.codes,
+                               w.scales, (int)w.tiled, (int)M, (int)N, (int)K, y, (int)g.out_bf16, g.ldy, epi);
             return hipGetLastError();
-        case ROUTE_STREAM: {
+        default: {      // ROUTE_STREAM
             int cus = 0;
             if (hipError_t e = device_cus(&cus); e != hipSuccess) return e;
             const int64_t nss = g.padded_k() / 512;
             const int nw = streaming_waves(N, cus), sets = nw == 1 && nss >= MANY ? MANY : FEW;
-            const SmallmKern* const kern = sets == MANY ? smallm_many[!w.tiled] : smallm_few[!w.tiled];
+            const SmallmKern<EPI>* const kern = sets == MANY ? smallm_many<EPI>[!w.tiled] : smallm_few<EPI>[!w.tiled];
             hipLaunchKernelGGL(kern[nss % sets], dim3((uint32_t)((N + 32 * nw - 1) / (32 * nw))), dim3(256), smallm_lds_bytes(sets, !w.tiled),
-                               s, a.codes, a.scales, (int)a.tiled, w.codes, w.scales, (int)M, (int)N, (int)K, y, (int)g.out_bf16, g.ldy, nw);
+                               s, a.codes, a.scales, (int)a.tiled, w.codes, w.scales, (int)M, (int)N, (int)K, y, (int)g.out_bf16, g.ldy, nw, epi);
             return hipGetLastError();
         }
-        case ROUTE_256x256:
-        case ROUTE_128x256: return launch_gemm_tiled(a, w, M, N, K, y, g.out_bf16, g.ldy, s, route == ROUTE_128x256);
-        default: return launch_gemm_mid(route - ROUTE_ONE_TILE, a, w, M, N, K, y, g.out_bf16, g.ldy, s);
     }
 }
 
-hipError_t launch_mxfp4_gemm(const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s) {
+hipError_t launch_gemm_route(int route, const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi) {
+    switch (route) {
+        case ROUTE_GENERAL:
+        case ROUTE_SKINNY:
+        case ROUTE_STREAM: return epi ? launch_here<true>(route, a, w, g, y, s, EpilogueArg<true>{*epi}) : launch_here<false>(route, a, w, g, y, s, {});
+        case ROUTE_ANY_K: return launch_gemm_any_k(a, w, g.M, g.N, g.K, y, g.out_bf16, g.ldy, s, epi);
+        case ROUTE_256x256:
+        case ROUTE_128x256: return epi ? hipErrorInvalidValue : launch_gemm_tiled(a, w, g.M, g.N, g.K, y, g.out_bf16, g.ldy, s, route == ROUTE_128x256);
+        default: return launch_gemm_mid(route - ROUTE_ONE_TILE, a, w, g.M, g.N, g.K, y, g.out_bf16, g.ldy, s, epi);
+    }
+}
+
+hipError_t launch_mxfp4_gemm(const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi) {
     int cus = 0;
     if (hipError_t e = device_cus(&cus); e != hipSuccess) return e;      // (also the per-device kernel set-up)
-    return launch_gemm_route(gemm_route(g, cus), a, w, g, y, s);
+    return launch_gemm_route(gemm_route(g, cus), a, w, g, y, s, epi);
 }
 
 }  // namespace brq
