@@ -80,7 +80,8 @@ enum {
     BRQ_GEMM_192x256 = 8,
     BRQ_GEMM_320x128 = 9,
     BRQ_GEMM_256x128 = 10,
-    BRQ_GEMM_ANY_K = 11          /* any shape with K of at least 256, through LDS */
+    BRQ_GEMM_ANY_K = 11,         /* any shape with K of at least 256, through LDS */
+    BRQ_GEMM_EPILOGUE_FEW = 12   /* of brq_mxfp4_gemm_epilogue alone: M <= 16, K of whole 512-element superstages */
 };
 
 /*
@@ -100,13 +101,15 @@ brq_status brq_diag_mxfp4_gemm_on(int32_t route, const uint8_t* aq, const uint8_
 
 /*
  * brq_mxfp4_gemm_epilogue (brq_residual.h) on the kernel `route`, also where nothing follows the product; BRQ_ERR_SHAPE where that
- * kernel does not take the shape, or takes no epilogue.
+ * kernel does not take the shape, or takes no epilogue.  slices > 1 (BRQ_GEMM_64x128 and BRQ_GEMM_128x128, 2 to 16 slices of at least
+ * 1024 of K): split along K, with a workspace of slices * M * ceil4(N) * 4 bytes.
  */
-brq_status brq_diag_mxfp4_gemm_epilogue_on(int32_t route, const uint8_t* aq, const uint8_t* as, brq_layout a_layout,
-                                           const uint8_t* wq, const uint8_t* ws, brq_layout w_layout, int64_t M,
-                                           int64_t N, int64_t K, const float* bias, int32_t act,
-                                           const void* residual, brq_dtype rdt, int64_t ldr, void* y,
-                                           brq_dtype ydt, int64_t ldy, void* stream);
+brq_status brq_diag_mxfp4_gemm_epilogue_on(int32_t route, int32_t slices, const uint8_t* aq, const uint8_t* as,
+                                           brq_layout a_layout, const uint8_t* wq, const uint8_t* ws,
+                                           brq_layout w_layout, int64_t M, int64_t N, int64_t K, const float* bias,
+                                           int32_t act, const void* residual, brq_dtype rdt, int64_t ldr, void* y,
+                                           brq_dtype ydt, int64_t ldy, void* workspace, int64_t workspace_bytes,
+                                           void* stream);
 
 /*
  * The kernels of brq_kv4_attention.  Which of them takes a call is decided by its sizes; the call below names the choice, so that a test

@@ -73,7 +73,9 @@ brq_status brq_add_rms_norm_rotate_quantize_fused(const void* x, brq_dtype xdt, 
  * and pitch).  y's pitch is free (>= N) as in brq_mxfp4_gemm.
  * act of t:  BRQ_ACT_RELU  max(t, 0) (NaN stays NaN);   BRQ_ACT_SILU  t / (1 + exp(-t));
  *            BRQ_ACT_GELU  t/2 erfc(-t / sqrt 2)  (the exact one, not its tanh form)
- * Of the fp32 t they are within (8 + 2 |t|) 2^-24 |silu(t)| + 2^-119 |t| and (16 + 2 t^2) 2^-24 |gelu(t)| + 2^-118.
+ * workspace: brq_mxfp4_gemm_epilogue_workspace bytes (may be 0, then NULL; where nothing follows the product too), 16-byte aligned: a product of
+ * few rows and columns and a long K is split along K, and the slices' fp32 sums are added in their order.
+ * Of the fp32 t the activations are within (8 + 2 |t|) 2^-24 |silu(t)| + 2^-119 |t| and (16 + 2 t^2) 2^-24 |gelu(t)| + 2^-118.
  */
 typedef enum {
     BRQ_ACT_NONE = 0,
@@ -86,7 +88,10 @@ typedef enum {
 brq_status brq_mxfp4_gemm_epilogue(const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq,
                                    const uint8_t* ws, brq_layout w_layout, int64_t M, int64_t N, int64_t K,
                                    const float* bias, brq_activation act, const void* residual, brq_dtype rdt,
-                                   int64_t ldr, void* y, brq_dtype ydt, int64_t ldy, void* stream);
+                                   int64_t ldr, void* y, brq_dtype ydt, int64_t ldy, void* workspace,
+                                   int64_t workspace_bytes, void* stream);
+brq_status brq_mxfp4_gemm_epilogue_workspace(brq_layout a_layout, brq_layout w_layout, int64_t M, int64_t N, int64_t K,
+                                             int64_t* bytes);
 
 #ifdef __cplusplus
 }

@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbrq.so")
 BINDING = os.path.join(HERE, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["brq_api.hip", "rotate_quant.hip", "matrix_rotate_quant.hip", "block_summary.hip", "mxfp4_gemm.hip", "mxfp4_gemm_tiled.hip", "mxfp4_gemm_mid.hip",
-           "mxfp4_gemm_mid_with.hip", "residual_api.hip", "add_rms_norm.hip", "attn_api.hip", "attn_heads.hip", "kv4_attention.hip", "kv4_pages.hip"]
+           "mxfp4_gemm_mid_with.hip", "mxfp4_gemm_split.hip", "mxfp4_gemm_few.hip", "residual_api.hip", "add_rms_norm.hip", "attn_api.hip", "attn_heads.hip", "kv4_attention.hip", "kv4_pages.hip"]
 # -ffp-contract=off: the rotation's add/sub/mul sequence is part of the result's definition.
 # packed fp32 instructions are kept out of the generated code.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

@@ -826,6 +826,7 @@ decltype(&brq_add_rms_norm_backward) f_add_norm_back;
 decltype(&brq_add_rms_norm_backward_workspace) f_add_norm_back_space;
 decltype(&brq_add_rms_norm_rotate_quantize_fused) f_add_norm_quantize;
 decltype(&brq_mxfp4_gemm_epilogue) f_gemm_epilogue;
+decltype(&brq_mxfp4_gemm_epilogue_workspace) f_gemm_epilogue_space;
 bool g_residual;                     // bind_residual() was called
 
 // A matrix of a call, or one to be made: rows of any pitch.
@@ -960,35 +961,41 @@ bool activation(PyObject* o, brq_activation* v) {
     return *v != BRQ_ACT_NONE;
 }
 
-// gemm_epilogue(aq, as, wq, ws, bias, activation, residual, out_dtype, out, a_layout, w_layout, M, N, K)
+// gemm_epilogue(aq, as, wq, ws, bias, activation, residual, out_dtype, out, a_layout, w_layout, M, N, K, workspace)
 PyObject* gemm_epilogue(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     Call c;
     brq_layout la, lw;
     int64_t M, N, K;
-    at::Tensor bias, y;
+    at::Tensor bias, y, space;
     Matrix res;
     brq_activation act;
     brq_dtype dt;
     int64_t ldy;
-    if (n != 14 || !g_residual || !quiet() || !c.take(a[0]) || !c.take(a[1]) || !c.take(a[2]) || !c.take(a[3]) || (a[8] != Py_None && !c.take(a[8])) || !layout(a[9], &la) ||
+    if (n != 15 || !g_residual || !quiet() || !c.take(a[0]) || !c.take(a[1]) || !c.take(a[2]) || !c.take(a[3]) || (a[8] != Py_None && !c.take(a[8])) || !layout(a[9], &la) ||
         !layout(a[10], &lw) || !size_arg(a[11], &M) || !size_arg(a[12], &N) || !size_arg(a[13], &K) || !operand(a[0], a[1], la, &M, &K) ||
         !operand(a[2], a[3], lw, &N, &K) || M < 0 || N < 0 || K < 0 || !operand_fits(a[0], a[1], la, M, K) || !operand_fits(a[2], a[3], lw, N, K) ||
         !array_of(c, a[4], at::kFloat, {N}, &bias, true) || !activation(a[5], &act) || !matrix(c, a[6], &res, true) ||
-        (res.t.defined() && (res.t.size(0) != M || res.t.size(1) != N)) || !result(a[8], a[7], THPVariable_Unpack(a[0]), M, N, &y, &dt, &ldy)) Py_RETURN_NONE;
+        (res.t.defined() && (res.t.size(0) != M || res.t.size(1) != N)) || !array_of(c, a[14], at::kByte, {-1}, &space, true) ||
+        !result(a[8], a[7], THPVariable_Unpack(a[0]), M, N, &y, &dt, &ldy)) Py_RETURN_NONE;
+    if (!space.defined() && (bias.defined() || act != BRQ_ACT_NONE || res.t.defined())) {
+        int64_t need = 0;
+        if (const brq_status r = f_gemm_epilogue_space(la, lw, M, N, K, &need); r != BRQ_OK) return status(r);
+        if (need && !make(c, {need}, at::kByte, &space)) Py_RETURN_NONE;
+    }
     const uint8_t *ac = data(a[0]), *as = data(a[1]), *wc = data(a[2]), *ws = data(a[3]);
     void *p = y.data_ptr(), *s = current_stream();
-    return result_or(released([&] { return f_gemm_epilogue(ac, as, la, wc, ws, lw, M, N, K, address<float>(bias), act, res.p(), res.dt, res.ld, p, dt, ldy, s); }), a[8], y);
+    return result_or(released([&] { return f_gemm_epilogue(ac, as, la, wc, ws, lw, M, N, K, address<float>(bias), act, res.p(), res.dt, res.ld, p, dt, ldy, address<void>(space), space.defined() ? space.numel() : 0, s); }), a[8], y);
     END_HANDLE_TH_ERRORS
 }
 
 PyObject* bind_residual(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    void* p[5];
-    if (n != 5) {
-        PyErr_SetString(PyExc_TypeError, "bind_residual takes the addresses of five entry points");
+    void* p[6];
+    if (n != 6) {
+        PyErr_SetString(PyExc_TypeError, "bind_residual takes the addresses of six entry points");
         return nullptr;
     }
-    for (int i = 0; i < 5; ++i) {
+    for (int i = 0; i < 6; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an entry point's address is NULL");
@@ -997,7 +1004,7 @@ PyObject* bind_residual(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     int i = 0;
     auto set = [&](auto& f) { f = reinterpret_cast<std::decay_t<decltype(f)>>(p[i++]); };
-    set(f_add_norm), set(f_add_norm_back), set(f_add_norm_back_space), set(f_add_norm_quantize), set(f_gemm_epilogue);
+    set(f_add_norm), set(f_add_norm_back), set(f_add_norm_back_space), set(f_add_norm_quantize), set(f_gemm_epilogue), set(f_gemm_epilogue_space);
     g_residual = true;
     Py_RETURN_NONE;
 }

@@ -83,7 +83,7 @@ struct GemmShape {
 };
 constexpr int MID_TILES = 6;
 enum GemmRoute { ROUTE_GENERAL, ROUTE_SKINNY, ROUTE_STREAM, ROUTE_256x256, ROUTE_128x256, ROUTE_ONE_TILE /* + a tile's number */,
-                 ROUTE_ANY_K = ROUTE_ONE_TILE + MID_TILES };
+                 ROUTE_ANY_K = ROUTE_ONE_TILE + MID_TILES, ROUTE_FEW /* with an epilogue alone */ };
 bool gemm_route_supported(int route, const GemmShape& g);
 // The route of a product on a device of `cus` compute units: host arithmetic.
 int gemm_route(const GemmShape& g, int cus);
@@ -95,8 +95,9 @@ struct Epilogue {
     int64_t res_pitch;
     int res_bf16, act, out_bf16;
 };
-// epi: null, or what follows (g.epilogue says whether).
-hipError_t launch_mxfp4_gemm(const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi = nullptr);
+// epi: null, or what follows (g.epilogue says whether); with it a workspace of split_gemm_workspace(g, gemm_split(g, cus)) bytes.
+hipError_t launch_mxfp4_gemm(const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi = nullptr,
+                             void* workspace = nullptr);
 // The same on a route that takes the shape (gemm_route_supported), device_cus() having been called.
 hipError_t launch_gemm_route(int route, const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi = nullptr);
 
@@ -135,6 +136,19 @@ hipError_t launch_gemm_any_k_with(const Operand& a, const Operand& w, int64_t M,
                                   hipStream_t s, const Epilogue& epi);
 hipError_t launch_gemm_mid_with(int tile, const Operand& a, const Operand& w, int64_t M, int64_t N, int64_t K, void* y,
                                 bool out_bf16, int64_t ldy, hipStream_t s, const Epilogue& epi);
+
+// Up to 16 rows, K of whole superstages (mxfp4_gemm_few.hip).
+hipError_t launch_gemm_few(const Operand& a, const Operand& w, const GemmShape& g, void* y, const Epilogue& epi, hipStream_t s);
+
+// The one-tile kernels split along K, with what follows the product where the slices are joined (mxfp4_gemm_split.hip).
+constexpr int MAX_SLICES = 16;
+struct GemmSplit { int rows, slices; };      // rows of a tile (64 or 128; of 128 columns); 1 slice: not split
+GemmSplit gemm_split(const GemmShape& g, int cus);                              // host arithmetic
+int64_t split_gemm_workspace(const GemmShape& g, const GemmSplit& s);           // bytes
+bool gemm_split_supported(const GemmShape& g, const GemmSplit& s);
+hipError_t launch_gemm_split(const GemmSplit& sp, const Operand& a, const Operand& w, const GemmShape& g, void* y, void* workspace,
+                             const Epilogue& epi, hipStream_t s);
+hipError_t setup_gemm_split();
 
 // Tiled -> row-major copy of a quantized operand.
 hipError_t launch_to_rowmajor(const uint8_t* codes_t, const uint8_t* scales_t, int64_t rows, int64_t K,

@@ -17,6 +17,32 @@ __device__ __forceinline__ void static_for(F&& f, IC<N> n, IC<S> = {}) {
     }
 }
 
+// Addressing of one row of a quantized operand, valid for both layouts: the 16 code bytes of
+// group g sit at codes + (g >> 2) * cstep + (g & 3) * 16 and its scale at scales + (g >> 4) * sstep
+// + (g & 15), with (cstep, sstep) = (64, 16) for row-major rows and (4096, 1024) for the tiled
+// layout (64-row slabs; 64 code bytes per row and stage, 16 scale bytes per row and superstage).
+struct RowView {
+    const uint8_t* codes;
+    const uint8_t* scales;
+    uint32_t cstep, sstep;
+    __device__ __forceinline__ RowView(const uint8_t* c, const uint8_t* s, bool tiled, int64_t row, int K) {
+        if (tiled) {
+            const int64_t Kp = ((int64_t)K + 511) / 512 * 512;
+            codes = c + (row >> 6) * (Kp / 128) * 4096 + (row & 63) * 64;
+            scales = s + (row >> 6) * (Kp / 512) * 1024 + (row & 63) * 16;
+            cstep = 4096; sstep = 1024;
+        } else {
+            codes = c + row * (K / 2);
+            scales = s + row * (K / 32);
+            cstep = 64; sstep = 16;
+        }
+    }
+    __device__ __forceinline__ v4i group(int g) const {
+        return *reinterpret_cast<const v4i*>(codes + (int64_t)(g >> 2) * cstep + (g & 3) * 16);
+    }
+    __device__ __forceinline__ int scale(int g) const { return scales[(int64_t)(g >> 4) * sstep + (g & 15)]; }
+};
+
 // Wait until at most N of this wavefront's vector-memory operations are outstanding and all
 // its LDS reads have returned, then meet the other wavefronts.
 template <int N>

@@ -12,32 +12,6 @@
 
 namespace brq {
 
-// Addressing of one row of a quantized operand, valid for both layouts: the 16 code bytes of
-// group g sit at codes + (g >> 2) * cstep + (g & 3) * 16 and its scale at scales + (g >> 4) * sstep
-// + (g & 15), with (cstep, sstep) = (64, 16) for row-major rows and (4096, 1024) for the tiled
-// layout (64-row slabs; 64 code bytes per row and stage, 16 scale bytes per row and superstage).
-struct RowView {
-    const uint8_t* codes;
-    const uint8_t* scales;
-    uint32_t cstep, sstep;
-    __device__ __forceinline__ RowView(const uint8_t* c, const uint8_t* s, bool tiled, int64_t row, int K) {
-        if (tiled) {
-            const int64_t Kp = ((int64_t)K + 511) / 512 * 512;
-            codes = c + (row >> 6) * (Kp / 128) * 4096 + (row & 63) * 64;
-            scales = s + (row >> 6) * (Kp / 512) * 1024 + (row & 63) * 16;
-            cstep = 4096; sstep = 1024;
-        } else {
-            codes = c + row * (K / 2);
-            scales = s + row * (K / 32);
-            cstep = 64; sstep = 16;
-        }
-    }
-    __device__ __forceinline__ v4i group(int g) const {
-        return *reinterpret_cast<const v4i*>(codes + (int64_t)(g >> 2) * cstep + (g & 3) * 16);
-    }
-    __device__ __forceinline__ int scale(int g) const { return scales[(int64_t)(g >> 4) * sstep + (g & 15)]; }
-};
-
 __device__ __forceinline__ void store_out(void* y, bool out_bf16, int64_t idx, float v) {
     if (out_bf16) reinterpret_cast<uint16_t*>(y)[idx] = (uint16_t)f32_to_bf16_bits(v);
     else reinterpret_cast<float*>(y)[idx] = v;
@@ -51,18 +25,27 @@ __device__ __forceinline__ void store_column(const Epilogue& e, float (&v)[N], v
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
     if (col >= cols) return;
-    float r[N];
+    uint32_t r[N] = {};                                 // as they lie in memory; rows past the last: the last one's
+    if (e.res && e.res_bf16) {                          // uniform
 #pragma unroll
-    for (int i = 0; i < N; ++i) r[i] = e.res && row_of(i) < M ? residual_at(e, row_of(i), col) : 0.0f;
+        for (int i = 0; i < N; ++i) r[i] = reinterpret_cast<const uint16_t*>(e.res + (int64_t)min(row_of(i), M - 1) * e.res_pitch)[col];
+    } else if (e.res) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i] = reinterpret_cast<const uint32_t*>(e.res + (int64_t)min(row_of(i), M - 1) * e.res_pitch)[col];
+    }
     if (e.bias) {
         const float b = e.bias[col];
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += b;
     }
     activate(v, e.act);
+    if (e.res) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += as_f32(e.res_bf16 ? r[i] << 16 : r[i]);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if (row_of(i) < M) store_out(y, out_bf16, (int64_t)row_of(i) * ldy + col, e.res ? v[i] + r[i] : v[i]);
+        if (row_of(i) < M) store_out(y, out_bf16, (int64_t)row_of(i) * ldy + col, v[i]);
 }
 
 // ---- general shapes: one 32x32 output tile per wavefront, operands straight from global ----
@@ -671,7 +654,7 @@ static const Tile TILES[] = {
 };
 
 // The cheapest of these that take the shape, or -1.  (The one-tile kernels' sixth tile is not among them: see tall_tile.)
-static int pick_tile(const GemmShape& g, int cus) {
+static int pick_tile(const GemmShape& g, int cus, float* us = nullptr) {
     const bool tiled = g.a_tiled && g.w_tiled;
     const float stages = (float)((g.K + 511) / 512 * 4), output = 0.6e-6f * (float)g.M * (float)g.N * (g.out_bf16 ? 1.0f : 2.0f);
     const float bytes = 0.53125f * ((float)g.M + (float)g.N) * (float)g.K / 5.0e6f;
@@ -690,7 +673,51 @@ static int pick_tile(const GemmShape& g, int cus) {
         const float cost = c.fixed + sqrtf(sqrtf(pow4(alone) + pow4(full) + pow4(bytes))) + (lines ? c.store : c.store_off) * output;
         if (best < 0 || cost < least) { best = t.route; least = cost; }
     }
+    if (us) *us = least;
     return best;
+}
+
+// Whether to split a product with something behind it along K: for few tiles and a long K.  By the same estimate, with a slice's stages for K's and
+// its tiles times the slices; `alone` is 1.36 of the table's (a stage's operands come from HBM, and nobody else's are on their way), a second
+// workgroup on a CU costs 0.88 of a first (whole tiles of these two are held against that), and where some CUs have one more than others the bytes take longer by that imbalance to the power 0.6.  The join,
+// a launch that reads what the slices wrote: 2.8 us and 2.25 us per million fp32 sums of all slices.  Fitted to 84 shapes (M 17 .. 600, N 1024 ..
+// 11008, K 2048 .. 28672, both layouts; 552 pairs of tile and slices): chosen by it the slices are 0.4 % over the best (7 % at worst), split or not 0.8 % (13 %).
+// us, whole K -> split: tiled 48 x 4096 x 11008 23.1 -> 13.9, 100 x 8192 x 28672 53.0 -> 37.3, row-major 300 x 1288 x 8192 17.3 -> 13.9, 17 x 8192 x
+// 28672 66.8 -> 31.3.  By sizes and layouts alone, so that the workspace is too.
+GemmSplit gemm_split(const GemmShape& shape, int cus) {
+    GemmShape g = shape;
+    g.out_bf16 = true;
+    g.ldy = g.N;
+    g.y = 0;
+    g.epilogue = true;
+    GemmSplit best{64, 1};
+    float least = 0.0f;
+    if (g.M <= 16) return best;
+    const int whole = pick_tile(g, cus, &least);
+    if (whole < 0) return best;
+    const bool tiled = g.a_tiled && g.w_tiled;
+    const int64_t kq = g.padded_k() / 512;
+    const float bytes = 0.53125f * ((float)g.M + (float)g.N) * (float)g.K / 5.0e6f, mn = (float)g.M * (float)g.N;
+    auto pow4 = [](float x) { return x * x * x * x; };
+    auto estimate = [&](const Tile& t, int n) {
+        const TileCost& c = tiled ? t.tiled : !mid_gemm_pairs(t.route - ROUTE_ONE_TILE, tiled, g.K) ? t.singles : t.rowmajor;
+        const int64_t tm = (g.M + 64 * t.mb - 1) / (64 * t.mb), tiles = tm * ((g.N + 127) / 128), wgs = tiles * n, load = (wgs + cus - 1) / cus;
+        const float alone = (float)((kq + n - 1) / n * 4) * c.alone * 1.36f * (load == 1 ? 1.0f : 0.88f * (float)load);
+        const float full = (float)(kq * 4) * c.full * 0.457f * (float)tiles / (float)cus * (0.5f + 0.5f * (float)g.M / (float)(64 * t.mb * tm));
+        const float uneven = load > 1 ? powf((float)(load * cus) / (float)wgs, 0.6f) : 1.0f;
+        return c.fixed + sqrtf(sqrtf(pow4(alone) + pow4(full) + pow4(bytes * uneven))) + (n > 1 ? 2.8f + 2.25e-6f * (float)n * mn : 0.0f);
+    };
+    for (int i = 2; i <= 3; ++i)
+        if (TILES[i].route == whole) least = estimate(TILES[i], 1);
+    for (int i = 2; i <= 3; ++i)
+        for (int n = 2; n <= MAX_SLICES && gemm_split_supported(g, {64 * TILES[i].mb, n}); ++n)
+            if (const float cost = estimate(TILES[i], n); cost < least) { best = {64 * TILES[i].mb, n}; least = cost; }
+    return best;
+}
+
+bool gemm_split_supported(const GemmShape& g, const GemmSplit& s) {
+    return (s.rows == 64 || s.rows == 128) && s.slices >= 2 && s.slices <= MAX_SLICES && g.padded_k() / 512 / s.slices >= 2 &&
+           gemm_route_supported(s.rows == 64 ? ROUTE_ONE_TILE : ROUTE_ONE_TILE + 1, g) && g.M * ((g.N + 3) / 4) < (int64_t(1) << 31);
 }
 
 bool gemm_route_supported(int route, const GemmShape& g) {
@@ -701,6 +728,7 @@ bool gemm_route_supported(int route, const GemmShape& g) {
         case ROUTE_256x256:
         case ROUTE_128x256: return !g.epilogue && tiled_gemm_supported(g.M, g.N, g.K, g.out_bf16, g.ldy, g.a_tiled && g.w_tiled);
         case ROUTE_ANY_K: return g.K >= 256;
+        case ROUTE_FEW: return g.epilogue && gemm_route_supported(ROUTE_STREAM, g);
         default: return route >= ROUTE_ONE_TILE && route < ROUTE_ANY_K && mid_gemm_supported(route - ROUTE_ONE_TILE, g);
     }
 }
@@ -736,6 +764,9 @@ static bool any_k(const GemmShape& g) {
     return g.K >= 4096 || (double)((g.M + 31) / 32) * (double)((g.N + 31) / 32) * (double)g.K >= (double)(1 << 20);
 }
 
+// With something behind the product, up to 16 rows: split along K over a workgroup's wavefronts (mxfp4_gemm_few.hip) or streamed.
+static bool gemm_few_faster(const GemmShape& g, int cus) { return gemm_route_supported(ROUTE_FEW, g) && g.N <= 32 * (int64_t)cus; }
+
 int gemm_route(const GemmShape& g, int cus) {
     // Up to 16 rows: the weights are streamed (k_gemm_smallm).  The staged 64 x 128 kernel and the K-split one (ROUTE_SKINNY, which
     // sums in another order) against it, us, weights in no cache, 1 / 16 rows, streaming : 64 x 128 : K-split:
@@ -745,6 +776,7 @@ int gemm_route(const GemmShape& g, int cus) {
     //   weights row-major  64 x 512 2.4 / 2.7 : 3.5 / 3.5,  28672 x 512 4.6 / 5.0 : 5.2 / 5.2 : 4.3 / 5.3,  28672 x 1024 6.4 / 6.8 :
     //                      6.6 / 6.7 : 6.8 / 8.1,  28672 x 2048 9.1 / 9.6 : 9.7 / 9.9 : 11.4 / 13.1,  28672 x 8192 30.5 / 31.1 : 31.2 /
     //                      31.3 : 38.0 / 42.8,  2048 x 8192 8.7 / 9.1 : 18.6 / 19.2 : 12.6 / 13.0,  14336 x 4096 9.3 / 9.8 : 12.4 / 12.9
+    if (gemm_few_faster(g, cus)) return ROUTE_FEW;
     if (gemm_route_supported(ROUTE_STREAM, g)) return ROUTE_STREAM;
     const int t = g.M > 16 || g.K % 512 == 0 ? pick_tile(g, cus) : -1;
     if (tall_tile(t, g, cus)) return TALL_TILE;
@@ -782,6 +814,7 @@ hipError_t launch_gemm_route(int route, const Operand& a, const Operand& w, cons
         case ROUTE_GENERAL:
         case ROUTE_SKINNY:
         case ROUTE_STREAM: return epi ? launch_here<true>(route, a, w, g, y, s, EpilogueArg<true>{*epi}) : launch_here<false>(route, a, w, g, y, s, {});
+        case ROUTE_FEW: return epi ? launch_gemm_few(a, w, g, y, *epi, s) : hipErrorInvalidValue;
         case ROUTE_ANY_K: return launch_gemm_any_k(a, w, g.M, g.N, g.K, y, g.out_bf16, g.ldy, s, epi);
         case ROUTE_256x256:
         case ROUTE_128x256: return epi ? hipErrorInvalidValue : launch_gemm_tiled(a, w, g.M, g.N, g.K, y, g.out_bf16, g.ldy, s, route == ROUTE_128x256);
@@ -789,9 +822,11 @@ hipError_t launch_gemm_route(int route, const Operand& a, const Operand& w, cons
     }
 }
 
-hipError_t launch_mxfp4_gemm(const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi) {
+hipError_t launch_mxfp4_gemm(const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi, void* workspace) {
     int cus = 0;
     if (hipError_t e = device_cus(&cus); e != hipSuccess) return e;      // (also the per-device kernel set-up)
+    if (epi)
+        if (const GemmSplit sp = gemm_split(g, cus); sp.slices > 1) return launch_gemm_split(sp, a, w, g, y, workspace, *epi, s);
     return launch_gemm_route(gemm_route(g, cus), a, w, g, y, s, epi);
 }
 

@@ -257,12 +257,19 @@ __device__ __forceinline__ void store_tile_with(const Epilogue& e, v16f (&acc)[N
     }, IC<NB>{});
 }
 
+// Split along K (SPLIT): the workgroup multiplies one of `n` slices of at least two superstages each and stores fp32 sums to a matrix of the slice's own,
+// y + slice * M * ldy: for few tiles, which would leave most of the chip idle for all of K.  The slices are joined in another launch (mxfp4_gemm_split.hip).
+template <bool SPLIT>
+struct SplitArg {};
+template <>
+struct SplitArg<true> { int n; };
+
 // DW == DA unless PAIR.
-template <bool OUT_BF16, int NA, int MB, int DW, int DA, bool PAIR, bool EPI>
+template <bool OUT_BF16, int NA, int MB, int DW, int DA, bool PAIR, bool EPI, bool SPLIT = false>
 __global__ void __launch_bounds__(256, (lds_bytes(NA, MB, DW, DA) <= 81920 ? 2 : 1))
 k_gemm_mid(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as, const uint8_t* __restrict__ wq,
            const uint8_t* __restrict__ ws, int M, int N, int K, void* y, int64_t ldy, int a_tiled,
-           int w_tiled, int lines, EpilogueArg<EPI> epi) {
+           int w_tiled, int lines, EpilogueArg<EPI> epi, SplitArg<SPLIT> split) {
     constexpr int S = NA + MB, NM = NA * MB, NS = 2 * NM;      // MFMAs per step and per stage
     constexpr int TM = 64 * MB, TN = 64 * NA, G = PAIR ? 2 : 1;       // G: stages per slot of the rings
     constexpr int WSLOT = 4096 * NA * G, ASLOT = 4096 * MB * G, ABASE = 4096 * NA * DW;
@@ -281,18 +288,34 @@ k_gemm_mid(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as, const
     tw.tiles_m = (M + TM - 1) / TM;
     tw.tiles_n = (N + TN - 1) / TN;
     {
-        const int T = tw.tiles_m * tw.tiles_n, per_xcd = (T + 7) / 8;
+        int T = tw.tiles_m * tw.tiles_n;
+        if constexpr (SPLIT) T *= split.n;
+        const int per_xcd = (T + 7) / 8;
         tw.first = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
         tw.end = min(((int)(blockIdx.x & 7) + 1) * per_xcd, T);
         tw.stride = 1;
     }
     if (tw.first >= tw.end) return;                            // uniform over the workgroup
+    [[maybe_unused]] int slice = 0, q0 = 0;                    // slices one after the other, tiles inside; the slice's first superstage
+    if constexpr (SPLIT) {
+        const int T = tw.tiles_m * tw.tiles_n;
+        slice = tw.first / T;
+        tw.first -= slice * T;
+    }
     int tm, tn;
     tw.tile(0, tm, tn);
     const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * TN;
-    const int KQ = (K + 511) / 512;
-    const int64_t Kp = (int64_t)KQ * 512;
-    const int ovd = (K == Kp || w_tiled) ? 0 : (int)((Kp - K) / 128);   // stages the last window shares with the one before
+    const int KQ_all = (K + 511) / 512;
+    const int64_t Kp = (int64_t)KQ_all * 512;
+    int KQ = KQ_all, ovd = (K == Kp || w_tiled) ? 0 : (int)((Kp - K) / 128);   // superstages; stages the last window shares with the one before
+    if constexpr (SPLIT) {
+        const int each = KQ_all / split.n, more = KQ_all - each * split.n;
+        q0 = slice * each + min(slice, more);
+        KQ = each + (slice < more ? 1 : 0);
+        if (q0 + KQ < KQ_all) ovd = 0;
+        y = reinterpret_cast<float*>(y) + (int64_t)slice * M * ldy;
+    }
+    const bool to_end = !SPLIT || q0 + KQ == KQ_all;
 
     // ---- loads.  A wavefront brings 16 NA rows of W and 16 MB rows of A per stage, 16 rows x 64 bytes per
     // instruction (lane i: chunk (i & 3) ^ ((i >> 4) & 3) of row i >> 2), or 8 rows x 128 bytes of a pair, and its share of the scale rows, 64
@@ -312,8 +335,8 @@ k_gemm_mid(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as, const
     };
     // (bases moved to the tile's first row, so that the offsets stay below 2^32 for any M and N)
     const int64_t wslab = n0 >> 6, aslab = m0 >> 6;            // TM and TN are multiples of 64
-    const uint8_t* const wbase = uniform_ptr(wq + (w_tiled ? wslab * (Kp / 128) * 4096 : n0 * (K / 2)));
-    const uint8_t* const abase = uniform_ptr(aq + (a_tiled ? aslab * (Kp / 128) * 4096 : m0 * (K / 2)));
+    const uint8_t* const wbase = uniform_ptr(wq + (w_tiled ? wslab * (Kp / 128) * 4096 : n0 * (K / 2)) + (int64_t)q0 * (w_tiled ? 16384 : 256));
+    const uint8_t* const abase = uniform_ptr(aq + (a_tiled ? aslab * (Kp / 128) * 4096 : m0 * (K / 2)) + (int64_t)q0 * (a_tiled ? 16384 : 256));
     const int64_t nrows = N - n0, mrows = M - m0;
     uint32_t vw[G * NA], va[G * MB], vsc[SPW];
 #pragma unroll
@@ -345,13 +368,13 @@ k_gemm_mid(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as, const
         vsc[i] = isw ? scale_off(64 * idx + lane, nrows, tl) : scale_off(64 * (idx - NA) + lane, mrows, tl);
         const uint8_t* b = isw ? ws + (tl ? wslab * (Kp / 512) * 1024 : n0 * (K / 32))
                                : as + (tl ? aslab * (Kp / 512) * 1024 : m0 * (K / 32));
-        sbase[i] = uniform_ptr(b);
         sdst[i] = lds0 + SCALE_BASE + idx * 1024;
         sstep[i] = tl ? 1024 : 16;
-        slast[i] = tl ? (KQ - 1) * 1024 : K / 32 - 16;
+        sbase[i] = uniform_ptr(b + (int64_t)q0 * sstep[i]);
+        slast[i] = tl || !to_end ? (KQ - 1) * sstep[i] : K / 32 - 16 - q0 * 16;
     }
-    const int w_stage = w_tiled ? 4096 : 64, w_last = w_tiled ? (KQ - 1) * 16384 : K / 2 - 256;
-    const int a_stage = a_tiled ? 4096 : 64, a_last = a_tiled ? (KQ - 1) * 16384 : K / 2 - 256;
+    const int w_stage = w_tiled ? 4096 : 64, w_last = w_tiled || !to_end ? (KQ - 1) * 4 * w_stage : K / 2 - 256 - q0 * 256;
+    const int a_stage = a_tiled ? 4096 : 64, a_last = a_tiled || !to_end ? (KQ - 1) * 4 * a_stage : K / 2 - 256 - q0 * 256;
     const uint32_t dst_w = lds0 + wave * (WSLOT / 4), dst_a = lds0 + ABASE + wave * (ASLOT / 4);
     const uint8_t *pw = wbase, *pa = abase;                    // superstages that are being loaded
     uint32_t ld_buf = 0, rd_buf = 0;                           // scale buffers of the superstages being loaded and read
@@ -680,7 +703,9 @@ k_gemm_any_k(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as, con
 constexpr int any_k_lds_bytes(int mb) { return 2 * (128 * (128 + 64 * mb) + 8 * 256); }
 
 template <bool EPI>
-using Kern = void (*)(const uint8_t*, const uint8_t*, const uint8_t*, const uint8_t*, int, int, int, void*, int64_t, int, int, int, EpilogueArg<EPI>);
+using Kern = void (*)(const uint8_t*, const uint8_t*, const uint8_t*, const uint8_t*, int, int, int, void*, int64_t, int, int, int, EpilogueArg<EPI>, SplitArg<false>);
+template <bool EPI>
+using AnyK = void (*)(const uint8_t*, const uint8_t*, const uint8_t*, const uint8_t*, int, int, int, void*, int64_t, int, int, int, EpilogueArg<EPI>);
 template <bool EPI>
 struct Variant { int na, mb, dw, da; Kern<EPI> bf16, f32; };
 // (OUT_BF16 says nothing where there is an epilogue: one kernel for both)
@@ -694,7 +719,7 @@ static const Variant<EPI> pairs[MID_TILES] = {BRQ_MID(2, 1, 6, 6, true), BRQ_MID
                                               BRQ_MID(2, 4, 6, 4, true)};       // (6 stages of A: 0.5 % slower to 1 % faster)
 #undef BRQ_MID
 template <bool EPI>
-static const Kern<EPI> any_k[2][2] = {{k_gemm_any_k<EPI, 1, EPI>, k_gemm_any_k<true, 1, EPI>},
+static const AnyK<EPI> any_k[2][2] = {{k_gemm_any_k<EPI, 1, EPI>, k_gemm_any_k<true, 1, EPI>},
                                       {k_gemm_any_k<EPI, 2, EPI>, k_gemm_any_k<true, 2, EPI>}};    // [MB - 1][bf16 out]
 
 }  // namespace mid
@@ -709,7 +734,7 @@ hipError_t mid_setup() {
                                                    mid::lds_bytes(v.na, v.mb, v.dw, v.da)); e != hipSuccess) return e;
     }
     for (int mb = 1; mb <= 2; ++mb)
-        for (mid::Kern<EPI> k : mid::any_k<EPI>[mb - 1])
+        for (mid::AnyK<EPI> k : mid::any_k<EPI>[mb - 1])
             if (hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, mid::any_k_lds_bytes(mb)); e != hipSuccess) return e;
     return hipSuccess;
 }
@@ -734,7 +759,7 @@ hipError_t mid_launch(int tile, const Operand& a, const Operand& w, int64_t M, i
     const mid::Variant<EPI>& v = (mid_gemm_pairs(tile, a.tiled && w.tiled, K) ? mid::pairs<EPI> : mid::singles<EPI>)[tile];
     const int64_t tm = (M + 64 * v.mb - 1) / (64 * v.mb), tn = (N + 64 * v.na - 1) / (64 * v.na), T = tm * tn;
     hipLaunchKernelGGL((out_bf16 ? v.bf16 : v.f32), dim3((uint32_t)((T + 7) / 8 * 8)), dim3(256), mid::lds_bytes(v.na, v.mb, v.dw, v.da), s,
-                       a.codes, a.scales, w.codes, w.scales, (int)M, (int)N, (int)K, y, ldy, (int)a.tiled, (int)w.tiled, on_half_lines(y, N, ldy, out_bf16), epi);
+                       a.codes, a.scales, w.codes, w.scales, (int)M, (int)N, (int)K, y, ldy, (int)a.tiled, (int)w.tiled, on_half_lines(y, N, ldy, out_bf16), epi, mid::SplitArg<false>{});
     return hipGetLastError();
 }
 

@@ -7,6 +7,7 @@ bool mid_gemm_pairs(int tile, bool both_tiled, int64_t K) { return !both_tiled &
 
 hipError_t setup_gemm_mid() {
     if (hipError_t e = mid_setup<false>(); e != hipSuccess) return e;
+    if (hipError_t e = setup_gemm_split(); e != hipSuccess) return e;
     return setup_gemm_mid_with();
 }
 

@@ -166,32 +166,62 @@ brq_status brq_add_rms_norm_backward(const void* h, brq_dtype hdt, int64_t ldh, 
     return launched(brq::launch_add_rms_norm_backward(a, static_cast<hipStream_t>(stream)));
 }
 
+brq_status brq_mxfp4_gemm_epilogue_workspace(brq_layout a_layout, brq_layout w_layout, int64_t M, int64_t N, int64_t K, int64_t* bytes) {
+    alignas(16) static const uint8_t operand[16] = {};      // (nothing is launched: any aligned address will do)
+    if (!bytes) return BRQ_ERR_NULL;
+    BRQ_CHECK(brq::check_gemm(operand, operand, a_layout, operand, operand, w_layout, M, N, K, operand, BRQ_F32, N));
+    *bytes = 0;
+    if (M == 0 || N == 0) return BRQ_OK;
+    int cus = 0;
+    if (brq::device_cus(&cus) != hipSuccess) return BRQ_ERR_DEVICE;
+    const brq::GemmShape g{M, N, K, a_layout == BRQ_LAYOUT_TILED, w_layout == BRQ_LAYOUT_TILED, true, N, 0, true};
+    *bytes = brq::split_gemm_workspace(g, brq::gemm_split(g, cus));
+    return BRQ_OK;
+}
+
 brq_status brq_mxfp4_gemm_epilogue(const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq, const uint8_t* ws,
                                    brq_layout w_layout, int64_t M, int64_t N, int64_t K, const float* bias, brq_activation act,
-                                   const void* residual, brq_dtype rdt, int64_t ldr, void* y, brq_dtype ydt, int64_t ldy, void* stream) {
+                                   const void* residual, brq_dtype rdt, int64_t ldr, void* y, brq_dtype ydt, int64_t ldy, void* workspace,
+                                   int64_t workspace_bytes, void* stream) {
     BRQ_CHECK(brq::check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy));
     BRQ_CHECK(check_epilogue(M, N, bias, act, residual, rdt, ldr, y, ydt, ldy));
+    if (!aligned(workspace, 16)) return BRQ_ERR_ALIGN;
     if (M == 0 || N == 0) return BRQ_OK;
     const brq::Operand a{aq, as, a_layout == BRQ_LAYOUT_TILED}, w{wq, ws, w_layout == BRQ_LAYOUT_TILED};
     brq::GemmShape g{M, N, K, a.tiled, w.tiled, ydt == BRQ_BF16, ldy, reinterpret_cast<uintptr_t>(y)};
     if (!bias && act == BRQ_ACT_NONE && !residual) return launched(brq::launch_mxfp4_gemm(a, w, g, y, static_cast<hipStream_t>(stream)));
     g.epilogue = true;
+    int cus = 0;
+    if (brq::device_cus(&cus) != hipSuccess) return BRQ_ERR_LAUNCH;
+    const int64_t need = brq::split_gemm_workspace(g, brq::gemm_split(g, cus));
+    if (need > 0 && !workspace) return BRQ_ERR_NULL;
+    if (need > workspace_bytes) return BRQ_ERR_SHAPE;
     const brq::Epilogue e = epilogue(bias, act, residual, rdt, ldr, ydt);
-    return launched(brq::launch_mxfp4_gemm(a, w, g, y, static_cast<hipStream_t>(stream), &e));
+    return launched(brq::launch_mxfp4_gemm(a, w, g, y, static_cast<hipStream_t>(stream), &e, workspace));
 }
 
-brq_status brq_diag_mxfp4_gemm_epilogue_on(int32_t route, const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq, const uint8_t* ws,
+brq_status brq_diag_mxfp4_gemm_epilogue_on(int32_t route, int32_t slices, const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq, const uint8_t* ws,
                                            brq_layout w_layout, int64_t M, int64_t N, int64_t K, const float* bias, int32_t act,
-                                           const void* residual, brq_dtype rdt, int64_t ldr, void* y, brq_dtype ydt, int64_t ldy, void* stream) {
+                                           const void* residual, brq_dtype rdt, int64_t ldr, void* y, brq_dtype ydt, int64_t ldy, void* workspace,
+                                           int64_t workspace_bytes, void* stream) {
     BRQ_CHECK(brq::check_gemm(aq, as, a_layout, wq, ws, w_layout, M, N, K, y, ydt, ldy));
     BRQ_CHECK(check_epilogue(M, N, bias, (brq_activation)act, residual, rdt, ldr, y, ydt, ldy));
+    if (!aligned(workspace, 16)) return BRQ_ERR_ALIGN;
     const brq::Operand a{aq, as, a_layout == BRQ_LAYOUT_TILED}, w{wq, ws, w_layout == BRQ_LAYOUT_TILED};
     brq::GemmShape g{M, N, K, a.tiled, w.tiled, ydt == BRQ_BF16, ldy, reinterpret_cast<uintptr_t>(y)};
     g.epilogue = true;
-    if (M == 0 || N == 0 || !brq::gemm_route_supported(route, g)) return BRQ_ERR_SHAPE;
+    if (M == 0 || N == 0 || slices < 1 || !brq::gemm_route_supported(route, g)) return BRQ_ERR_SHAPE;
+    const brq::GemmSplit sp{route == BRQ_GEMM_64x128 ? 64 : route == BRQ_GEMM_128x128 ? 128 : 0, slices};
+    if (slices > 1) {
+        if (!brq::gemm_split_supported(g, sp)) return BRQ_ERR_SHAPE;
+        const int64_t need = brq::split_gemm_workspace(g, sp);
+        if (!workspace) return BRQ_ERR_NULL;
+        if (need > workspace_bytes) return BRQ_ERR_SHAPE;
+    }
     int cus = 0;
     if (brq::device_cus(&cus) != hipSuccess) return BRQ_ERR_LAUNCH;
     const brq::Epilogue e = epilogue(bias, (brq_activation)act, residual, rdt, ldr, ydt);
+    if (slices > 1) return launched(brq::launch_gemm_split(sp, a, w, g, y, workspace, e, static_cast<hipStream_t>(stream)));
     return launched(brq::launch_gemm_route(route, a, w, g, y, static_cast<hipStream_t>(stream), &e));
 }
 

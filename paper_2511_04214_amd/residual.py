@@ -12,9 +12,11 @@ import paper_2511_04214_amd as _brq
 from .attention import _array, _on, _same_device, _size
 
 ACTIVATIONS = {None: 0, "relu": 1, "silu": 2, "gelu": 3}
+# the kernels of mxfp4_gemm_epilogue (include/brq_diag.h), by their numbers there
+EPILOGUE_ROUTES = _brq.GEMM_ROUTES + ("few",)
 # the entry points that the compiled marshalling calls, in its order
 NATIVE = ("brq_add_rms_norm", "brq_add_rms_norm_backward", "brq_add_rms_norm_backward_workspace", "brq_add_rms_norm_rotate_quantize_fused",
-          "brq_mxfp4_gemm_epilogue")
+          "brq_mxfp4_gemm_epilogue", "brq_mxfp4_gemm_epilogue_workspace")
 
 
 def declare(L):
@@ -25,8 +27,9 @@ def declare(L):
             ("add_rms_norm_backward", [vp, i32, i64, vp, i32, i64, vp, i64, i64, i64, vp, f32, vp, i64, vp, vp, i64, vp]),
             ("add_rms_norm_backward_workspace", [i64, i64, ctypes.POINTER(i64)]),
             ("add_rms_norm_rotate_quantize_fused", [vp, i32, i64, vp, i32, i64, i64, i64, vp, f32, vp, i64, i32, i64, vp, vp, vp, i32, vp]),
-            ("diag_mxfp4_gemm_epilogue_on", [i32, vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, vp, i32, i64, vp]),
-            ("mxfp4_gemm_epilogue", [vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, vp, i32, i64, vp])):
+            ("diag_mxfp4_gemm_epilogue_on", [i32, i32, vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, vp, i32, i64, vp, i64, vp]),
+            ("mxfp4_gemm_epilogue", [vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, vp, i32, i64, vp, i64, vp]),
+            ("mxfp4_gemm_epilogue_workspace", [i32, i32, i64, i64, i64, ctypes.POINTER(i64)])):
         f = getattr(L, "brq_" + name)
         f.argtypes, f.restype = args, i32
 
@@ -150,35 +153,47 @@ def _activation(name):
     return code
 
 
+def mxfp4_gemm_epilogue_workspace(M, N, K, a_layout="rowmajor", w_layout="rowmajor"):
+    """Bytes of the workspace of mxfp4_gemm_epilogue (brq_mxfp4_gemm_epilogue_workspace)."""
+    return _size(_brq.lib().brq_mxfp4_gemm_epilogue_workspace, _brq._layout_code(a_layout), _brq._layout_code(w_layout), M, N, K)
+
+
 def mxfp4_gemm_epilogue(aq, as_, wq, ws, bias=None, activation=None, residual=None, out_dtype=torch.float32, out=None, stream=None,
-                        a_layout="rowmajor", w_layout="rowmajor", M=None, N=None, K=None):
+                        a_layout="rowmajor", w_layout="rowmajor", M=None, N=None, K=None, workspace=None):
     """Y = act(deq(aq, as) @ deq(wq, ws)^T + bias) + residual, rounded once (brq_mxfp4_gemm_epilogue).
 
     Operands as in mxfp4_gemm.  bias: fp32 [N]; activation: None, "relu", "silu" or "gelu" (with erfc); residual: [M, N], float32 or bfloat16,
     which may be `out`."""
-    r = _native("gemm_epilogue", stream, aq, as_, wq, ws, bias, activation, residual, out_dtype, out, a_layout, w_layout, M, N, K)
+    r = _native("gemm_epilogue", stream, aq, as_, wq, ws, bias, activation, residual, out_dtype, out, a_layout, w_layout, M, N, K, workspace)
     if r is not None:
         return r
     la, lw, M, N, K = _brq._operands(aq, as_, wq, ws, a_layout, w_layout, M, N, K)
     act = _activation(activation)
-    _same_device(aq, as_, wq, ws, bias, residual, out)
+    _same_device(aq, as_, wq, ws, bias, residual, out, workspace)
     pb = _array(bias, "bias", torch.float32, (N,), True)
     pr, dr, ldr = _matrix(residual, "residual", (M, N))
+    need = 0 if bias is None and not act and residual is None else mxfp4_gemm_epilogue_workspace(M, N, K, a_layout, w_layout)
     with _on(stream):
         y, ldy = _brq._result(out, M, N, out_dtype, aq.device)
+        if workspace is None and need:
+            workspace = torch.empty((need,), dtype=torch.uint8, device=aq.device)
     _brq._check(_brq.lib().brq_mxfp4_gemm_epilogue(aq.data_ptr(), as_.data_ptr(), la, wq.data_ptr(), ws.data_ptr(), lw, M, N, K, pb, act,
-                                                   pr, dr, ldr, y.data_ptr(), _brq._dtype_code(y), ldy, _brq._stream(stream)))
+                                                   pr, dr, ldr, y.data_ptr(), _brq._dtype_code(y), ldy,
+                                                   _array(workspace, "workspace", torch.uint8, (None,), True),
+                                                   0 if workspace is None else workspace.numel(), _brq._stream(stream)))
     return y
 
 
 def diag_mxfp4_gemm_epilogue_on(route, aq, as_, wq, ws, out, K, bias=None, activation=None, residual=None, a_layout="rowmajor",
-                                w_layout="rowmajor", stream=None):
-    """out[M, N] = mxfp4_gemm_epilogue on the kernel `route`, one of GEMM_ROUTES (brq_diag_mxfp4_gemm_epilogue_on)."""
+                                w_layout="rowmajor", slices=1, stream=None):
+    """out[M, N] = mxfp4_gemm_epilogue on the kernel `route`, one of EPILOGUE_ROUTES, in so many slices of K (brq_diag_mxfp4_gemm_epilogue_on)."""
     M, N, ldy = _brq._rows(out, "out")
     la, lw, _, _, _ = _brq._operands(aq, as_, wq, ws, a_layout, w_layout, M, N, K)
     pb = _array(bias, "bias", torch.float32, (N,), True)
     pr, dr, ldr = _matrix(residual, "residual", (M, N))
+    with _on(stream):
+        space = torch.empty((slices * M * ((N + 3) // 4 * 16) if slices > 1 else 0,), dtype=torch.uint8, device=out.device)
     _brq._check(_brq.lib().brq_diag_mxfp4_gemm_epilogue_on(
-        _brq.GEMM_ROUTES.index(route), aq.data_ptr(), as_.data_ptr(), la, wq.data_ptr(), ws.data_ptr(), lw, M, N, K, pb, _activation(activation),
-        pr, dr, ldr, out.data_ptr(), _brq._dtype_code(out), ldy, _brq._stream(stream)))
+        EPILOGUE_ROUTES.index(route), slices, aq.data_ptr(), as_.data_ptr(), la, wq.data_ptr(), ws.data_ptr(), lw, M, N, K, pb, _activation(activation),
+        pr, dr, ldr, out.data_ptr(), _brq._dtype_code(out), ldy, space.data_ptr(), space.numel(), _brq._stream(stream)))
     return out

@@ -122,12 +122,12 @@ def test_one_tile_kernels(brq, route):
 
 
 @pytest.mark.parametrize("route,shapes", [("stream", [(1, 96, 512), (16, 33, 1536), (5, 700, 2560), (3, 4, 4096)]), ("skinny", [(1, 40, 96), (16, 17, 544), (7, 300, 32)]),
-                                          ("general", [(1, 1, 32), (33, 65, 96), (70, 130, 544)]), ("any_k", [(1, 5, 256), (64, 129, 1056), (65, 128, 288), (200, 300, 4000)])])
+                                          ("general", [(1, 1, 32), (33, 65, 96), (70, 130, 544)]), ("few", [(1, 5, 512), (16, 33, 512 * 9), (5, 100, 512 * 13), (3, 70, 544), (7, 16, 512 * 2 + 96), (2, 1, 4096)]), ("any_k", [(1, 5, 256), (64, 129, 1056), (65, 128, 288), (200, 300, 4000)])])
 def test_other_kernels(brq, route, shapes):
     for M, N, K in shapes:
         c = Case(M, N, K, seed=M + N)
         for la, lw in LAYOUTS:
-            if route == "stream" and K % 512 and (la, lw) != ("tiled", "tiled"):
+            if route in ("stream", "few") and K % 512 and (la, lw) != ("tiled", "tiled"):
                 continue
             for bias, act, res, dt in FORMS:
                 for pad in (0, 8):
@@ -135,9 +135,41 @@ def test_other_kernels(brq, route, shapes):
                     c.check(on_route(brq, route, c, la, lw), bias, act, res, dt, pad, in_place=res == dt and pad == 8)
 
 
+@pytest.mark.parametrize("route", ["64x128", "128x128"])
+def test_split_along_k(brq, route):
+    """Slices of equal and unequal length, to 16; row-major K that ends inside the last slice's last superstage."""
+    for M, N, K, slices in ((1, 3, 1024 * 2, 2), (65, 130, 512 * 7, 3), (130, 72, 6144, 5), (40, 300, 512 * 13, 6), (70, 129, 128 * 27, 3), (20, 4, 128 * 17, 2), (129, 140, 7168, 7)):
+        c = Case(M, N, K, seed=K)
+        for la, lw in LAYOUTS:
+            if K % 512 and (la, lw) not in (("tiled", "tiled"), ("rowmajor", "rowmajor")):
+                continue
+            for bias, act, res, dt in FORMS:
+                for pad in (0, 8):
+                    print("case", route, M, N, K, slices, la, lw, bias, act, res, dt, pad, flush=True)
+
+                    def call(out, b, a, r):
+                        return brq.diag_mxfp4_gemm_epilogue_on(route, *c.a[la], *c.w[lw], out, c.K, bias=b, activation=a, residual=r, a_layout=la, w_layout=lw, slices=slices)
+                    c.check(call, bias, act, res, dt, pad, in_place=res == dt and pad == 8)
+    long_k(brq, route, 33, 68, 1024 * 16, slices=16)
+
+
+def long_k(brq, route, rows, columns, K, **kw):
+    (a, va), (w, vw) = operand(1, rows, K), operand(2, columns, K)           # partial sums are no longer all exact
+    a, w = ([to_dev(t) for t in to_tiled(*o)] for o in (a, w))
+    out = torch.empty((rows, columns), device="cuda")
+    brq.diag_mxfp4_gemm_epilogue_on(route, *a, *w, out, K, a_layout="tiled", w_layout="tiled", **kw)
+    want, scale = torch.from_numpy(va @ vw.T).cuda(), torch.from_numpy(np.abs(va) @ np.abs(vw).T).cuda()
+    assert bool(((out.double() - want).abs() <= 1e-5 * scale).all())
+
+
+def test_long_k_of_few_rows(brq):
+    for K in (512 * 61, 512 * 64, 512 * 79):             # 8 to 10 superstages a wavefront
+        long_k(brq, "few", 16, 40, K)
+
+
 def test_the_call(brq):
     """Through the dispatcher, both ways of the binding; what the call makes, takes and returns."""
-    for M, N, K in ((1, 256, 512), (16, 200, 544), (40, 72, 96), (100, 520, 1024), (300, 136, 2048), (130, 1000, 1056), (700, 260, 512)):
+    for M, N, K in ((1, 256, 512), (16, 200, 544), (40, 72, 96), (100, 520, 1024), (300, 136, 2048), (130, 1000, 1056), (700, 260, 512), (48, 260, 7168)):
         c = Case(M, N, K, seed=K)
         for la, lw in LAYOUTS:
             kw = dict(a_layout=la, w_layout=lw, M=M, N=N, K=K)
@@ -151,6 +183,16 @@ def test_the_call(brq):
                     new = brq.mxfp4_gemm_epilogue(*c.a[la], *c.w[lw], bias=c.bias if bias else None, activation=act, residual=None if res is None else c.res[res], out_dtype=dt,
                                                   stream=stream, **kw)
                     assert new.dtype == dt and torch.equal(new, got)
+        need = brq.mxfp4_gemm_epilogue_workspace(M, N, K, "tiled", "tiled")
+        assert (need > 0) == (K == 7168)
+        if need:                                         # few tiles and a long K: split, in a workspace of the caller's too
+            assert need % (M * N * 4) == 0
+            kw = dict(a_layout="tiled", w_layout="tiled", M=M, N=N, K=K)
+            got = brq.mxfp4_gemm_epilogue(*c.a["tiled"], *c.w["tiled"], bias=c.bias, workspace=torch.empty(need, dtype=torch.uint8, device="cuda"), **kw)
+            assert torch.equal(got, brq.mxfp4_gemm_epilogue(*c.a["tiled"], *c.w["tiled"], bias=c.bias, **kw))
+            for stream in (None, torch.cuda.current_stream()):
+                with pytest.raises(brq.BrqError):
+                    brq.mxfp4_gemm_epilogue(*c.a["tiled"], *c.w["tiled"], bias=c.bias, workspace=torch.empty(need - 16, dtype=torch.uint8, device="cuda"), stream=stream, **kw)
         nothing = brq.mxfp4_gemm_epilogue(*c.a["tiled"], *c.w["tiled"], a_layout="tiled", w_layout="tiled", M=M, N=N, K=K)
         assert torch.equal(nothing, brq.mxfp4_gemm(*c.a["tiled"], *c.w["tiled"], a_layout="tiled", w_layout="tiled", M=M, N=N, K=K))
 

@@ -67,12 +67,12 @@ def test_backward(L):
 
 
 def test_gemm_epilogue(L):
-    def f(aq=P, as_=P, la=0, wq=P, ws=P, lw=0, M=4, N=6, K=64, bias=P, act=2, res=Q, rdt=1, ldr=6, y=R, ydt=1, ldy=6, call=None):
-        return (call or L.brq_mxfp4_gemm_epilogue)(aq, as_, la, wq, ws, lw, M, N, K, bias, act, res, rdt, ldr, y, ydt, ldy, None)
+    def f(aq=P, as_=P, la=0, wq=P, ws=P, lw=0, M=4, N=6, K=64, bias=P, act=2, res=Q, rdt=1, ldr=6, y=R, ydt=1, ldy=6, space=S, n=1 << 30, call=None):
+        return (call or L.brq_mxfp4_gemm_epilogue)(aq, as_, la, wq, ws, lw, M, N, K, bias, act, res, rdt, ldr, y, ydt, ldy, space, n, None)
     assert f(M=0) == f(N=0, ldr=0, ldy=0) == OK and f(M=0, aq=None, y=None, res=None) == OK
 
-    def on(route):
-        return lambda *a: L.brq_diag_mxfp4_gemm_epilogue_on(route, *a)
+    def on(route, slices=1):
+        return lambda *a: L.brq_diag_mxfp4_gemm_epilogue_on(route, slices, *a)
     for call in (None, on(0)):
         assert f(aq=None, call=call) == f(ws=None, call=call) == f(y=None, call=call) == NULL
         assert f(ydt=2, call=call) == f(rdt=2, call=call) == DTYPE and f(la=3, call=call) == LAYOUT
@@ -80,10 +80,19 @@ def test_gemm_epilogue(L):
             assert f(act=act, call=call) == ACTIVATION
         assert f(M=-1, call=call) == f(K=40, call=call) == f(ldy=5, call=call) == f(ldr=5, call=call) == f(ldr=1 << 30, call=call) == SHAPE
         assert f(y=Q, ldy=8, call=call) == f(y=Q, ydt=0, call=call) == SHAPE                  # a sum in the residual's place: the same rows
-        assert f(bias=P + 2, call=call) == f(res=Q + 1, call=call) == f(res=Q + 2, rdt=0, call=call) == f(y=R + 8, call=call) == ALIGN
+        assert f(bias=P + 2, call=call) == f(res=Q + 1, call=call) == f(res=Q + 2, rdt=0, call=call) == f(y=R + 8, call=call) == f(space=S + 8, call=call) == ALIGN
     assert f(M=0, call=on(0)) == SHAPE
     for route in (3, 4, 12, -1, 1, 2, 5, 11):            # persistent kernels; no kernels; kernels that do not take 20 rows of K = 64
         assert f(M=20, call=on(route)) == SHAPE
+    big = dict(M=70, N=130, K=4096, la=1, lw=1, ldr=130, ldy=130)
+    assert f(**big, space=None, call=on(5, 2)) == NULL and f(**big, n=2 * 70 * 132 * 4 - 1, call=on(6, 2)) == SHAPE
+    for route, slices in ((5, 0), (5, -1), (5, 5), (6, 17), (7, 2), (0, 2), (2, 2)):     # no slices; slices below 1024; too many; kernels that are not split
+        assert f(**big, call=on(route, slices)) == SHAPE
+    n = ctypes.c_int64()
+    space = L.brq_mxfp4_gemm_epilogue_workspace
+    assert space(0, 0, 4, 6, 64, None) == NULL and space(2, 0, 4, 6, 64, byref(n)) == LAYOUT
+    assert space(0, 0, -1, 6, 64, byref(n)) == space(0, 0, 4, 1 << 40, 64, byref(n)) == space(0, 0, 4, 6, 65, byref(n)) == SHAPE
+    assert space(0, 0, 0, 6, 64, byref(n)) == OK and n.value == 0
     assert "activation" in brq.lib().brq_strerror(ACTIVATION).decode()
 
 
