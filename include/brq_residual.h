@@ -28,7 +28,7 @@ extern "C" {
  * in fp32.  res NULL: h = x, and `h` must be NULL (rdt and ldr are not looked at).  h NULL: the sum is not
  * wanted.  w: [K] fp32, 16-byte aligned, or NULL (no weight).  eps >= 0 and not NaN; with eps = 0 a row of
  * zeros comes out as NaN.  The sum of a row's squares has to be finite in fp32.
- * x [M][ldx] of xdt, res [M][ldr] and h [M][ldh] of rdt, y [M][ldy] of ydt.  K <= 65536.
+ * x [M][ldx] of xdt, res [M][ldr] and h [M][ldh] of rdt, y [M][ldy] of ydt.  K <= 32768.
  */
 brq_status brq_add_rms_norm(const void* x, brq_dtype xdt, int64_t ldx, const void* res, brq_dtype rdt,
                             int64_t ldr, int64_t M, int64_t K, const float* w, float eps, void* h, int64_t ldh,
@@ -56,7 +56,7 @@ brq_status brq_add_rms_norm_backward_workspace(int64_t M, int64_t K, int64_t* by
  * in one pass; y never visits memory.  Bit-identical to that two-call sequence of THIS library (ydt =
  * BRQ_BF16 rounds y to bf16 before the rotation; BRQ_F32 keeps the fp32 value).
  * B = 1 (no rotation; signs must then be NULL) or 8 ... 512: blocks that a wavefront holds.  Wider ones,
- * and K above 65536: the two calls.
+ * and rows above 32768: the two calls.
  */
 brq_status brq_add_rms_norm_rotate_quantize_fused(const void* x, brq_dtype xdt, int64_t ldx, const void* res,
                                                   brq_dtype rdt, int64_t ldr, int64_t M, int64_t K, const float* w,

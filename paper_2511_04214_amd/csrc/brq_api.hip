@@ -28,6 +28,7 @@ hipError_t device_cus(int* cus) {
         if (hipError_t e = setup_gemm_mid(); e != hipSuccess) return e;
         if (hipError_t e = setup_matrix_rotate(); e != hipSuccess) return e;
         if (hipError_t e = setup_gemm_decode_fused(); e != hipSuccess) return e;
+        if (hipError_t e = setup_add_rms_norm(); e != hipSuccess) return e;
         slot.cus = v;
         slot.ready = true;
     }

@@ -12,9 +12,9 @@ brq_status check_gemm(const uint8_t* aq, const uint8_t* as, brq_layout a_layout,
                       int64_t M, int64_t N, int64_t K, const void* y, brq_dtype ydt, int64_t ldy);
 
 // Per-device facts and one-time set-up.  The launchers size their grids by the number of compute units
-// and four kernel families ask for more than the default 64 KB of LDS, which HIP wants declared per
+// and five kernel families ask for more than the default 64 KB of LDS, which HIP wants declared per
 // function and device before the first launch.  device_cus() returns the CU count of the CURRENT device and
-// on its first call for that device (under a lock, keyed by the device id) runs the four set-up routines;
+// on its first call for that device (under a lock, keyed by the device id) runs the five set-up routines;
 // brq_init() is that call made ahead of time.  Nothing else in the library outlives a call.
 hipError_t device_cus(int* cus);
 hipError_t setup_gemm_tiled();     // mxfp4_gemm_tiled.hip
@@ -22,6 +22,7 @@ hipError_t setup_gemm_mid();       // mxfp4_gemm_mid.hip
 hipError_t setup_gemm_mid_with();  // mxfp4_gemm_mid_with.hip, called by the former
 hipError_t setup_matrix_rotate();  // matrix_rotate_quant.hip
 hipError_t setup_gemm_decode_fused();   // mxfp4_gemm.hip
+hipError_t setup_add_rms_norm();   // add_rms_norm.hip
 
 // mode: 0 rotate, 1 quantize, 2 fused rotate+quantize.  log2b: 0 for quantize, else 3..14.
 // tiled: codes and scales go out in the tiled operand layout instead of row-major.

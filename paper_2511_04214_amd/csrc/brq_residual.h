@@ -24,7 +24,7 @@ struct NormArgs {
     int l2b;                    // log2 of the rotation block, 0: none
     const int8_t* signs;        // [K] or null
 };
-constexpr int64_t NORM_MAX_K = 65536;
+constexpr int64_t NORM_MAX_K = 32768;
 hipError_t launch_add_rms_norm(const NormArgs& a, bool quantize, hipStream_t s);
 
 struct NormBackwardArgs {

@@ -670,7 +670,11 @@ static int pick_tile(const GemmShape& g, int cus, float* us = nullptr) {
         const float filled = one_tile ? 0.5f + 0.5f * (float)g.M / (float)(64 * t.mb * tm) : 1.0f;
         const float alone = stages * c.alone * (float)((T + places - 1) / places);
         const float full = stages * c.full * (float)T / (float)cus * filled;
-        const float cost = c.fixed + sqrtf(sqrtf(pow4(alone) + pow4(full) + pow4(bytes))) + (lines ? c.store : c.store_off) * output;
+        // What follows a product takes a tile's time by itself, 1 us for every 64 x 64 where nothing else runs on the CU meanwhile; two workgroups a CU
+        // overlap it.  Of the one-tile kernels 192 x 256 and 320 x 128 then lose to 128 x 128 (2048 x 6144 x 4096, bias and residual: 60 and 55 us : 38).  Over the
+        // best of the six, 9 shapes with bias, residual, or both and a GELU: 11.8 % without this term, 3.7 % with it.
+        const float after = g.epilogue ? (float)(t.na * t.mb) * (float)((T + places - 1) / places) : 0.0f;
+        const float cost = c.fixed + sqrtf(sqrtf(pow4(alone) + pow4(full) + pow4(bytes))) + (lines ? c.store : c.store_off) * output + after;
         if (best < 0 || cost < least) { best = t.route; least = cost; }
     }
     if (us) *us = least;
@@ -764,8 +768,19 @@ static bool any_k(const GemmShape& g) {
     return g.K >= 4096 || (double)((g.M + 31) / 32) * (double)((g.N + 31) / 32) * (double)g.K >= (double)(1 << 20);
 }
 
-// With something behind the product, up to 16 rows: split along K over a workgroup's wavefronts (mxfp4_gemm_few.hip) or streamed.
-static bool gemm_few_faster(const GemmShape& g, int cus) { return gemm_route_supported(ROUTE_FEW, g) && g.N <= 32 * (int64_t)cus; }
+// With something behind the product, up to 16 rows: split along K over a workgroup's wavefronts (mxfp4_gemm_few.hip) or streamed.  The former starts a
+// workgroup for 16 columns, which has to pay: few columns or a long K, and with row-major operands, whose lines it asks for in halves, few rows or
+// few columns.  Its time over the streaming kernel's, 1 / 16 rows (182 shapes): tiled, N <= 4096, K = 512 1.03 / 1.05, K = 1024 0.91 / 0.94, K = 4096 0.63 /
+// 0.67, 16384 0.58 / 0.64; N 6144 to 12288, K = 1024 1.07 / 1.15, 2048 0.95 / 0.98, 4096 0.76 / 0.84, 8192 0.92 / 0.94, 16384 1.00 / 1.10; N from 16384,
+// K = 2048 1.07 / 1.13, 4096 0.86 / 0.97, 8192 1.03 / 1.10.  Row-major, N <= 4096, K = 1024 1.02 / 1.13, 2048 0.86 / 0.96, from 4096 0.62 / 0.78; N above,
+// K = 2048 1.20 / 1.49, from 4096 1 / 4 / 8 / 16 rows 0.89 / 0.95 / 1.03 / 1.12.
+static bool gemm_few_faster(const GemmShape& g, int cus) {
+    if (!gemm_route_supported(ROUTE_FEW, g)) return false;
+    const bool tiled = g.a_tiled && g.w_tiled;
+    if (g.N <= 16 * (int64_t)cus) return g.K >= (tiled ? 1024 : 2048);
+    if (!tiled) return g.K >= 4096 && g.M <= 4;
+    return g.N <= 48 * (int64_t)cus ? g.K >= 2048 : g.K >= 4096 && g.K < 8192;
+}
 
 int gemm_route(const GemmShape& g, int cus) {
     // Up to 16 rows: the weights are streamed (k_gemm_smallm).  The staged 64 x 128 kernel and the K-split one (ROUTE_SKINNY, which

@@ -49,7 +49,7 @@ def check_norm(y, h, w, eps, dtype):
 
 
 # one wavefront, parts of one, one element group; two to sixteen wavefronts, one to eight chunks a lane, ragged ends of each
-KS = [32, 64, 480, 512, 544, 1024, 1056, 2016, 2048, 2080, 4096, 4128, 8192, 8224, 16384, 16416, 32768, 32800, 65536]
+KS = [32, 64, 480, 512, 544, 1024, 1056, 2016, 2048, 2080, 4096, 4128, 8192, 8224, 16384, 16416, 32736, 32768]
 MS = [1, 2, 3, 5, 257]
 
 

@@ -22,7 +22,7 @@ def norm_refusals(f):
     assert f(M=0) == OK and f(M=0, x=None, res=None, h=None) == OK
     assert f(x=None) == f(h=P + 0x100, res=None) == NULL
     assert f(xdt=2) == f(rdt=-1) == DTYPE
-    assert f(M=-1) == f(M=1 << 31) == f(K=0) == f(K=-32) == f(K=48) == f(K=65536 + 32) == f(M=1 << 29, K=64) == SHAPE
+    assert f(M=-1) == f(M=1 << 31) == f(K=0) == f(K=-32) == f(K=48) == f(K=32768 + 32) == f(M=1 << 29, K=64) == SHAPE
     assert f(ldx=32) == f(ldr=32) == f(ldh=32) == f(ldx=1 << 30) == f(ldr=1 << 62) == f(ldh=(1 << 63) - 1) == SHAPE
     assert f(eps=-1e-6) == f(eps=float("nan")) == f(eps=-float("inf")) == SHAPE
     assert f(x=P + 8) == f(res=Q + 2) == f(h=R + 4) == f(w=P + 4) == f(ldx=68) == f(ldr=66) == f(ldh=70) == ALIGN
@@ -56,7 +56,7 @@ def test_backward(L):
         return L.brq_add_rms_norm_backward(h, hdt, ldh, gy, gdt, ldgy, gh, ldgh, M, K, w, eps, dh, lddh, dw, ws, n, None)
     assert f(h=None) == f(gy=None) == f(dh=None) == f(ws=None) == f(w=None) == NULL           # (w: a gradient of a weight that is not there)
     assert f(hdt=3) == f(gdt=9) == DTYPE
-    assert f(M=-1) == f(K=40) == f(K=1 << 17) == f(ldh=32) == f(ldgy=32) == f(ldgh=32) == f(lddh=32) == f(eps=float("nan")) == f(n=16) == f(n=-1) == SHAPE
+    assert f(M=-1) == f(K=40) == f(K=1 << 16) == f(ldh=32) == f(ldgy=32) == f(ldgh=32) == f(lddh=32) == f(eps=float("nan")) == f(n=16) == f(n=-1) == SHAPE
     assert f(dh=R, lddh=72) == f(dh=P, lddh=72) == f(dh=Q, gdt=0) == f(dh=Q, lddh=72) == SHAPE
     assert f(h=P + 2) == f(gy=Q + 4) == f(gh=R + 8) == f(dh=S + 2) == f(w=P + 4) == f(dw=P + 2) == f(ws=P + 8) == f(ldgh=68) == ALIGN
     assert f(M=0, w=None, dw=None, ws=None, n=0, h=None, gy=None, gh=None, dh=None) == OK
