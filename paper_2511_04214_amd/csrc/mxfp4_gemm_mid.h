@@ -137,18 +137,60 @@ __device__ __forceinline__ void store_tile(v16f (&acc)[NA][MB], uint8_t* lds, vo
     }, IC<NM>{});
 }
 
+// The residuals of a wavefront's part of a tile as they lie in memory, where all 8 columns of a lane's are there: of bf16 lo.xy and lo.zw, of fp32 lo and hi.
+// A lane has 8 columns of rows (lane >> 3) + 8 j of every 32 x 64 block: for bf16 out 8 neighbours, for fp32 out 4 of each half.
+template <int NA, int MB>
+struct TileResiduals {
+    typedef unsigned int u4 __attribute__((ext_vector_type(4)));
+    static constexpr int NB = NA / 2 * MB;
+    u4 lo[NB][4], hi[NB][4];
+    __device__ __forceinline__ void load(const Epilogue& e, int64_t m0, int64_t n0, int M, int N) {
+        typedef unsigned int u2 __attribute__((ext_vector_type(2)));
+        typedef unsigned int u4_any __attribute__((ext_vector_type(4), aligned(2)));
+        typedef unsigned int u2_any __attribute__((ext_vector_type(2), aligned(2)));
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const bool bf16 = e.out_bf16 != 0;
+        const int O1 = bf16 ? 4 : 32, o0 = (bf16 ? 8 : 4) * (lane & 7);
+        const int64_t row0 = m0 + (wave & 1) * 32 * MB + (lane >> 3), col0 = n0 + (wave >> 1) * 32 * NA;
+#pragma unroll
+        for (int x = 0; x < NB; ++x) {
+            const int row = (x % MB) * 32, col = (x / MB) * 64 + o0;
+            const uint8_t* const at = e.res + (row0 + row) * e.res_pitch + (col0 + col) * (e.res_bf16 ? 2 : 4);
+            const int64_t mr = e.res && N - col0 - col >= O1 + 4 ? M - row0 - row : 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // (values of their own until all branches have met: a branch that ends by storing to these arrays, next to another that does,
+                // makes the compiler keep them in memory)
+                u4 l = {0, 0, 0, 0}, h = {0, 0, 0, 0};
+                if (8 * j < mr) {
+                    const uint8_t* const p = at + (int64_t)(8 * j) * e.res_pitch;
+                    if (!e.res_bf16) {
+                        l = *reinterpret_cast<const u4_any*>(p);
+                        h = *reinterpret_cast<const u4_any*>(p + 4 * O1);
+                    } else if (bf16) {
+                        l = *reinterpret_cast<const u4_any*>(p);
+                    } else {
+                        const u2 a = *reinterpret_cast<const u2_any*>(p), b = *reinterpret_cast<const u2_any*>(p + 2 * O1);
+                        l = u4{a.x, a.y, b.x, b.y};
+                    }
+                }
+                lo[x][j] = l;
+                hi[x][j] = h;
+            }
+        }
+    }
+};
+
 // The same with what follows the product.  That has to come before the rounding, so it is fp32 that is turned round: 32 rows x 64 columns at a
-// time, 8 KB of a wavefront's own (`lds`: 32 KB that nobody reads any more), 16-byte chunk c of row i at i * 256 + ((c ^ (i & 15)) << 4).  A lane
-// then has 8 columns of rows (lane >> 3) + 8 j: for bf16 out 8 neighbours (one store of 16 bytes), for fp32 out 4 of each half (two stores, each
-// of 128 contiguous bytes per 8 lanes).  The residuals of the whole tile are asked for before the first is used: one latency, not one a block.
+// time, 8 KB of a wavefront's own (`lds`: 32 KB that nobody reads any more), 16-byte chunk c of row i at i * 256 + ((c ^ (i & 15)) << 4).  For bf16
+// out a lane then stores 16 bytes a row, for fp32 out twice 16, each time 128 contiguous bytes per 8 lanes.  The residuals of the whole tile are
+// asked for before the first is used, and on the small tiles before the last superstage.
 // (The output's type is looked at here: as a template's argument it doubles what there is to compile.)
 template <int NA, int MB>
-__device__ __forceinline__ void store_tile_with(const Epilogue& e, v16f (&acc)[NA][MB], uint8_t* lds, void* y, int64_t ldy, int64_t m0, int64_t n0, int M, int N, int lines) {
+__device__ __forceinline__ void store_tile_with(const Epilogue& e, v16f (&acc)[NA][MB], const TileResiduals<NA, MB>& res, uint8_t* lds, void* y, int64_t ldy, int64_t m0, int64_t n0, int M, int N, int lines) {
     constexpr int NB = NA / 2 * MB;
     typedef unsigned int u4 __attribute__((ext_vector_type(4)));
-    typedef unsigned int u2 __attribute__((ext_vector_type(2)));
     typedef unsigned int u4_any __attribute__((ext_vector_type(4), aligned(2)));
-    typedef unsigned int u2_any __attribute__((ext_vector_type(2), aligned(2)));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5, wn = wave >> 1, wm = wave & 1;
     const bool bf16 = e.out_bf16 != 0;
     const int es = bf16 ? 2 : 4, O1 = bf16 ? 4 : 32;           // the lane's columns in a block: 4 from o0, 4 from o0 + O1
@@ -156,31 +198,6 @@ __device__ __forceinline__ void store_tile_with(const Epilogue& e, v16f (&acc)[N
     const int i0 = lane >> 3, c = lane & 7, o0 = bf16 ? 8 * c : 4 * c, c0 = bf16 ? 2 * c : c, c1 = bf16 ? 2 * c + 1 : c + 8;
     const int64_t row0 = m0 + wm * 32 * MB + i0, col0 = n0 + wn * 32 * NA;
     const int64_t mrem = M - row0, ncols = N - col0;
-    auto block_row = [](int x) { return (x % MB) * 32; };
-    auto block_col = [](int x) { return (x / MB) * 64; };
-    // residuals as they lie in memory: of bf16 lo.xy and lo.zw, of fp32 lo and hi
-    u4 lo[NB][4], hi[NB][4];
-    if (e.res) {                                               // uniform
-#pragma unroll
-        for (int x = 0; x < NB; ++x) {
-            const uint8_t* const at = e.res + (row0 + block_row(x)) * e.res_pitch + (col0 + block_col(x) + o0) * (e.res_bf16 ? 2 : 4);
-            const int64_t mr = ncols - block_col(x) - o0 >= O1 + 4 ? mrem - block_row(x) : 0;      // rows from the lane's first on; all 8 columns there
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (8 * j >= mr) continue;
-                const uint8_t* const p = at + (int64_t)(8 * j) * e.res_pitch;
-                if (!e.res_bf16) {
-                    lo[x][j] = *reinterpret_cast<const u4_any*>(p);
-                    hi[x][j] = *reinterpret_cast<const u4_any*>(p + 4 * O1);
-                } else if (bf16) {
-                    lo[x][j] = *reinterpret_cast<const u4_any*>(p);
-                } else {
-                    const u2 a = *reinterpret_cast<const u2_any*>(p), b = *reinterpret_cast<const u2_any*>(p + 2 * O1);
-                    lo[x][j] = u4{a.x, a.y, b.x, b.y};
-                }
-            }
-        }
-    }
     float bias[NA / 2][8] = {};
     if (e.bias) {
 #pragma unroll
@@ -221,10 +238,10 @@ __device__ __forceinline__ void store_tile_with(const Epilogue& e, v16f (&acc)[N
                 if (e.res) {
                     if (e.res_bf16) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] += (k & 1) ? bf16_hi(lo[X][j][k >> 1]) : bf16_lo(lo[X][j][k >> 1]);
+                        for (int k = 0; k < 8; ++k) v[k] += (k & 1) ? bf16_hi(res.lo[X][j][k >> 1]) : bf16_lo(res.lo[X][j][k >> 1]);
                     } else {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] += as_f32(k < 4 ? lo[X][j][k & 3] : hi[X][j][k & 3]);
+                        for (int k = 0; k < 8; ++k) v[k] += as_f32(k < 4 ? res.lo[X][j][k & 3] : res.hi[X][j][k & 3]);
                     }
                 }
                 if (8 * j >= mr) continue;
@@ -573,10 +590,18 @@ k_gemm_mid(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as, const
     static_for([&](auto Ic) { set_scale(IC<0>{}, IC<0>{}, Ic, -1); }, IC<S>{});   // (a single superstage shares nothing)
     rd_buf = NSB == 1 ? 0u : (uint32_t)SCALE_BUF;
     for (int kq = 0; kq < KQ - 1; ++kq) superstage(IC<0>{}, kq);
-    superstage(IC<1>{}, KQ - 1);
-
-    if constexpr (EPI) store_tile_with<NA, MB>(epi.e, acc, lds, y, ldy, m0, n0, M, N, lines);
-    else store_tile<OUT_BF16, NA, MB>(acc, lds, y, ldy, m0, n0, M, N, lines);
+    if constexpr (EPI) {
+        // (younger than every load into LDS: the last superstage's counted waits only get stricter)
+        constexpr bool EARLY = NA * MB <= 4;
+        TileResiduals<NA, MB> res;
+        if constexpr (EARLY) res.load(epi.e, m0, n0, M, N);
+        superstage(IC<1>{}, KQ - 1);
+        if constexpr (!EARLY) res.load(epi.e, m0, n0, M, N);
+        store_tile_with<NA, MB>(epi.e, acc, res, lds, y, ldy, m0, n0, M, N, lines);
+    } else {
+        superstage(IC<1>{}, KQ - 1);
+        store_tile<OUT_BF16, NA, MB>(acc, lds, y, ldy, m0, n0, M, N, lines);
+    }
 }
 
 // ---- any K of at least 256 elements, any mix of layouts: what the kernels above do not take (row-major K that is not a multiple
@@ -697,8 +722,11 @@ k_gemm_any_k(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as, con
     int t = 0;
     for (; t + SETS <= pairs; t += SETS) static_for([&](auto Kc) __attribute__((always_inline)) { turn(Kc, t + decltype(Kc)::value); }, IC<SETS>{});
     if (t < pairs) turn(IC<0>{}, t);
-    if constexpr (EPI) store_tile_with<NA, MB>(epi.e, acc, lds, y, ldy, m0, n0, M, N, lines);
-    else store_tile<OUT_BF16, NA, MB>(acc, lds, y, ldy, m0, n0, M, N, lines);
+    if constexpr (EPI) {
+        TileResiduals<NA, MB> res;
+        res.load(epi.e, m0, n0, M, N);
+        store_tile_with<NA, MB>(epi.e, acc, res, lds, y, ldy, m0, n0, M, N, lines);
+    } else store_tile<OUT_BF16, NA, MB>(acc, lds, y, ldy, m0, n0, M, N, lines);
 }
 constexpr int any_k_lds_bytes(int mb) { return 2 * (128 * (128 + 64 * mb) + 8 * 256); }
 
