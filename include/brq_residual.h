@@ -10,6 +10,7 @@
  * row pitches), and these besides:
  *   - Outputs may not overlap inputs, except that a sum may replace a summand: an output of the same
  *     address, dtype and row pitch as the residual it adds (and, of the norm, as x).
+ *   - A workspace is one call's until that call's work is done: calls on one stream may share it, calls on two may not.
  *   - Infinities and NaN are not refused: they stay in their row (norms) or element (bias, residual).
  */
 #ifndef BRQ_RESIDUAL_H
@@ -68,14 +69,16 @@ brq_status brq_add_rms_norm_rotate_quantize_fused(const void* x, brq_dtype xdt, 
  * The W4A4 product with what follows it:
  *     y[m][n] = act(p[m][n] + bias[n]) + residual[m][n],     p the product of brq_mxfp4_gemm in fp32
  * evaluated in fp32 on the accumulators and rounded once to ydt.
- * bias: [N] fp32, 4-byte aligned, or NULL.  residual: [M][ldr] of rdt or NULL (rdt and ldr are then not looked at);
- * its address and pitch are multiples of its element's size, and it may be y itself (same address, dtype
- * and pitch).  y's pitch is free (>= N) as in brq_mxfp4_gemm.
+ * bias: [N] fp32, 4-byte aligned, or NULL.  residual: [M][ldr] of rdt or NULL (rdt and ldr are then not looked
+ * at); its address is a multiple of its element's size, its pitch free, and it may be y itself (same address,
+ * dtype and pitch).  y's pitch is free (>= N) as in brq_mxfp4_gemm.
  * act of t:  BRQ_ACT_RELU  max(t, 0) (NaN stays NaN);   BRQ_ACT_SILU  t / (1 + exp(-t));
  *            BRQ_ACT_GELU  t/2 erfc(-t / sqrt 2)  (the exact one, not its tanh form)
- * workspace: brq_mxfp4_gemm_epilogue_workspace bytes (may be 0, then NULL; where nothing follows the product too), 16-byte aligned: a product of
- * few rows and columns and a long K is split along K, and the slices' fp32 sums are added in their order.
- * Of the fp32 t the activations are within (8 + 2 |t|) 2^-24 |silu(t)| + 2^-119 |t| and (16 + 2 t^2) 2^-24 |gelu(t)| + 2^-118.
+ * workspace: brq_mxfp4_gemm_epilogue_workspace bytes (may be 0, then NULL; where nothing follows the product too),
+ * 16-byte aligned: a product of few tiles and a long K is split along K, and the slices' fp32 sums are added in
+ * their order.
+ * Of the fp32 t the activations are within (8 + 2 |t|) 2^-24 |silu(t)| + 2^-119 |t| and (16 + 2 t^2) 2^-24 |gelu(t)|
+ * + 2^-118.
  */
 typedef enum {
     BRQ_ACT_NONE = 0,
