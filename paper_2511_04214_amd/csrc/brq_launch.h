@@ -118,6 +118,8 @@ bool tiled_gemm_supported(int64_t M, int64_t N, int64_t K, bool out_bf16, int64_
 hipError_t launch_gemm_tiled(const Operand& a, const Operand& w, int64_t M, int64_t N, int64_t K, void* y,
                              bool out_bf16, int64_t ldy, hipStream_t s, bool half, unsigned long long* clk = nullptr,
                              bool no_loads = false);
+// With what follows it, one tile per workgroup.
+hipError_t launch_gemm_tiled_with(const Operand& a, const Operand& w, const GemmShape& g, void* y, const Epilogue& e, hipStream_t s, bool half);
 
 // One output tile per workgroup, the tile one of a family (mxfp4_gemm_mid.hip): any M, N and pitch.
 bool mid_gemm_supported(int tile, const GemmShape& g);

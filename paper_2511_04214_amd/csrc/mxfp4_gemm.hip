@@ -730,7 +730,7 @@ bool gemm_route_supported(int route, const GemmShape& g) {
         case ROUTE_SKINNY: return g.M <= 16;
         case ROUTE_STREAM: return g.M <= 16 && g.whole_k() && g.padded_k() < (int64_t(1) << 26);
         case ROUTE_256x256:
-        case ROUTE_128x256: return !g.epilogue && tiled_gemm_supported(g.M, g.N, g.K, g.out_bf16, g.ldy, g.a_tiled && g.w_tiled);
+        case ROUTE_128x256: return tiled_gemm_supported(g.M, g.N, g.K, g.out_bf16, g.ldy, g.a_tiled && g.w_tiled);
         case ROUTE_ANY_K: return g.K >= 256;
         case ROUTE_FEW: return g.epilogue && gemm_route_supported(ROUTE_STREAM, g);
         default: return route >= ROUTE_ONE_TILE && route < ROUTE_ANY_K && mid_gemm_supported(route - ROUTE_ONE_TILE, g);
@@ -832,7 +832,7 @@ hipError_t launch_gemm_route(int route, const Operand& a, const Operand& w, cons
         case ROUTE_FEW: return epi ? launch_gemm_few(a, w, g, y, *epi, s) : hipErrorInvalidValue;
         case ROUTE_ANY_K: return launch_gemm_any_k(a, w, g.M, g.N, g.K, y, g.out_bf16, g.ldy, s, epi);
         case ROUTE_256x256:
-        case ROUTE_128x256: return epi ? hipErrorInvalidValue : launch_gemm_tiled(a, w, g.M, g.N, g.K, y, g.out_bf16, g.ldy, s, route == ROUTE_128x256);
+        case ROUTE_128x256: return epi ? launch_gemm_tiled_with(a, w, g, y, *epi, s, route == ROUTE_128x256) : launch_gemm_tiled(a, w, g.M, g.N, g.K, y, g.out_bf16, g.ldy, s, route == ROUTE_128x256);
         default: return launch_gemm_mid(route - ROUTE_ONE_TILE, a, w, g.M, g.N, g.K, y, g.out_bf16, g.ldy, s, epi);
     }
 }

@@ -39,6 +39,7 @@
 //
 // LDS map (bytes): [0, 128K) 4 stages x (W rows 16K | A rows 16K); [128K, 144K) 2 scale
 // buffers x (W 4K | A 4K); [144K, 160K) 4 epilogue blocks.
+#include "gemm_epilogue.h"
 #include "mfma_fp4.h"
 #include "brq_launch.h"
 
@@ -53,7 +54,7 @@ constexpr int LDS_BYTES = EPI_BASE + 4 * 4096;          // 163840, all of the CU
 
 // f(IC<-1>), f(IC<0>), ..., f(IC<N>)
 template <class F, int N, int S = -1>
-__device__ __forceinline__ void static_for_drain(F& f, IC<N> n, IC<S> = {}) {
+__device__ __forceinline__ void static_for_drain(F&& f, IC<N> n, IC<S> = {}) {
     f(IC<S>{});
     if constexpr (S < N) static_for_drain(f, n, IC<S + 1>{});
 }
@@ -71,6 +72,101 @@ __device__ __forceinline__ void static_for_drain(F& f, IC<N> n, IC<S> = {}) {
 #define BRQ_N0(X) do { if constexpr (!(LAST && U == 3)) { X; } } while (0)
 #define BRQ_LD_SCALES(I) do { if constexpr (!LAST) ld_scales(Uc, IC<(I)>{}); } while (0)
 
+// A wavefront's part of a tile with what follows the product, in two passes of 64 rows (MB = 2: one).  That comes before the rounding, so it is fp32 that is
+// turned round, through the ring, which nothing is loaded to any more: 64 rows x 128 columns, 32 KB of a wavefront's own (`lds`), 16-byte
+// chunk c of row i at i * 512 + ((c ^ (i & 7)) << 4), written and read without bank conflicts.  Read back half a wavefront has a row and a
+// lane 4 columns, the same in every row, so its biases stay in registers.  Bias and activation are done in LDS, in a rolled loop: unrolled over the
+// accumulators a GELU would be 45 KB of code that a tile runs once.
+// RES: 0 no residual, 1 bf16, 2 fp32.  A pass's residuals are all asked for at once, the next one's as these are used: 8 rows at a time took 36 us a tile.
+template <int MB, int RES, bool LINES>
+__device__ __forceinline__ void store_with(const Epilogue& e, const v16f (&acc)[4][MB], uint8_t* lds, void* y, int64_t ldy, int m0, int n0, int M, int N) {
+    typedef unsigned int u2 __attribute__((ext_vector_type(2)));
+    typedef unsigned int u4 __attribute__((ext_vector_type(4)));
+    typedef unsigned int u2_any __attribute__((ext_vector_type(2), aligned(2)));
+    typedef unsigned int u4_any __attribute__((ext_vector_type(4), aligned(2)));
+    using Residual = std::conditional_t<RES == 1, u2, u4>;
+    using ResidualAt = std::conditional_t<RES == 1, u2_any, u4_any>;
+    constexpr int ROWS = RES ? 4 : 8, PASSES = MB / 2, PAIRS = RES ? 32 : 1;       // pairs of rows at a time in the rolled loop; of a pass
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    const int col = min(n0 + 4 * r, N - 4);           // (N is a multiple of 4; columns past it are nobody's)
+    const bool mine = n0 + 4 * r < N;
+    const uint8_t* const rcol = e.res + (int64_t)col * (RES == 1 ? 2 : 4);
+    Residual res[PAIRS];
+    auto residual = [&](int pass, int i) __attribute__((always_inline)) {
+        if constexpr (RES != 0) res[i] = *reinterpret_cast<const ResidualAt*>(rcol + (int64_t)min(m0 + 64 * pass + 2 * i + h, M - 1) * e.res_pitch);
+    };
+    if constexpr (RES != 0) {
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) residual(0, i);
+    }
+    float bias[4] = {};
+    if (e.bias) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bias[k] = e.bias[col + k];
+    }
+    const int64_t pitch = ldy * (e.out_bf16 ? 2 : 4);
+    uint8_t* const ytile = reinterpret_cast<uint8_t*>(y) + m0 * pitch + (int64_t)n0 * (e.out_bf16 ? 2 : 4);
+    const uint32_t ylane = (uint32_t)h * (uint32_t)pitch + 4u * r * (e.out_bf16 ? 2 : 4);      // (a pitch is below 2^28)
+    auto at = [&](int i) __attribute__((always_inline)) { return reinterpret_cast<float4*>(lds + (2 * i + h) * 512 + ((r ^ ((2 * i + h) & 7)) << 4)); };
+    auto put = [&](auto v, uint8_t* p) __attribute__((always_inline)) {      // (the hint as in out_store)
+        if constexpr (LINES) __builtin_nontemporal_store(v, reinterpret_cast<decltype(v)*>(p));
+        else *reinterpret_cast<decltype(v)*>(p) = v;
+    };
+    auto store = [&](int i, const float* v) __attribute__((always_inline)) {       // rows 2 i, 2 i + 1
+        if (mine && (m0 + 2 * i + 1 < M || (m0 + 2 * i < M && h == 0))) {
+            uint8_t* const p = ytile + 2 * i * pitch + ylane;
+            if (e.out_bf16) put(u2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}, p);
+            else put(u4{as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3])}, p);
+        }
+    };
+    lds_wait_and_barrier();                           // the last stage's reads are done in every wavefront: the ring is free
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+        static_for_drain([&](auto Xc) __attribute__((always_inline)) {
+            constexpr int X = decltype(Xc)::value, A = X >> 1, B = X & 1;
+            if constexpr (X >= 0) {
+                float t[16];
+                read_acc8(pass ? acc[A][(MB - 2) + B] : acc[A][B], IC<0>{}, t);
+                read_acc8(pass ? acc[A][(MB - 2) + B] : acc[A][B], IC<8>{}, t);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<float4*>(lds + (32 * B + r) * 512 + (((8 * A + 2 * q + h) ^ (r & 7)) << 4)) = make_float4(t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]);
+            }
+        }, IC<7>{});
+        const int rows = min(M - m0 - 64 * pass, 64);
+        if (RES == 0 || e.act != ACT_NONE) {
+            for (int i0 = 0; 2 * i0 < rows; i0 += ROWS) {
+                float v[4 * ROWS];
+#pragma unroll
+                for (int j = 0; j < ROWS; ++j) {
+                    const float4 t = *at(i0 + j);
+                    v[4 * j + 0] = t.x + bias[0]; v[4 * j + 1] = t.y + bias[1]; v[4 * j + 2] = t.z + bias[2]; v[4 * j + 3] = t.w + bias[3];
+                }
+                activate(v, e.act);
+#pragma unroll
+                for (int j = 0; j < ROWS; ++j) {
+                    if constexpr (RES != 0) *at(i0 + j) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                    else store(32 * pass + i0 + j, v + 4 * j);
+                }
+            }
+        }
+        if constexpr (RES != 0) {
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                const float4 t = *at(i);
+                float v[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (e.act == ACT_NONE) v[k] += bias[k];
+                    v[k] += RES == 1 ? as_f32(k & 1 ? res[i][k >> 1] & 0xffff0000u : res[i][k >> 1] << 16) : as_f32(res[i][k]);
+                }
+                if (pass + 1 < PASSES) residual(pass + 1, i);
+                store(32 * pass + i, v);
+            }
+        }
+    }
+}
+
 // Where the measurement instantiation reports its clock; the product instantiation's is empty.
 template <bool TIMED>
 struct ClockOut {};
@@ -85,11 +181,12 @@ struct ClockOut<true> { unsigned long long* p; };
 // MFMA, LDS read, barrier and output store runs as in the product, and the result is NOT the product - what
 // the kernel would cost if its operands moved themselves.  The product (DIAG == 0) has no such code.
 // LINES: the output's rows begin on 128-byte lines (asked in the kernel it cost 8192 x 14336 x 4096 3 %).
-template <bool OUT_BF16, int MB, int DIAG, bool LINES>
+// EPI: with what follows the product (epi, which then says the output's type too), one tile per workgroup; see store_with below.
+template <bool OUT_BF16, int MB, int DIAG, bool LINES, bool EPI = false>
 __global__ void __launch_bounds__(256, 1) k_gemm_tiled(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as,
                                                        const uint8_t* __restrict__ wq, const uint8_t* __restrict__ ws,
                                                        int M, int N, int K, void* __restrict__ y, int64_t ldy, int a_tiled, int w_tiled,
-                                                       ClockOut<DIAG != 0> clk) {
+                                                       ClockOut<DIAG != 0> clk, EpilogueArg<EPI> epi) {
     constexpr bool TIMED = DIAG != 0;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -592,6 +689,18 @@ __global__ void __launch_bounds__(256, 1) k_gemm_tiled(const uint8_t* __restrict
     // hidden in inline assembly: the compiler does not know to keep the 18 wait states between a 16-pass
     // MFMA and a read of its result.
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    if constexpr (EPI) {
+        int tm, tn;
+        tw.tile(0, tm, tn);
+        if (KQ == 1) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // loads into the ring for a successor that does not exist
+        auto store = [&](auto Res) __attribute__((always_inline)) {
+            store_with<MB, decltype(Res)::value, LINES>(epi.e, acc, lds + wave * 32768, y, ldy, tm * TMv + wm * 32 * MB, tn * TN + wn * 128, M, N);
+        };
+        if (!epi.e.res) store(IC<0>{});
+        else if (epi.e.res_bf16) store(IC<1>{});
+        else store(IC<2>{});
+        return;
+    }
     out_begin(ntiles - 1);
     static_for_drain(drain_slot, IC<NACC>{});
     if constexpr (TIMED) { const unsigned long long t = __builtin_readcyclecounter(); t_epi += t - t_mark; t_mark = t; }
@@ -633,15 +742,17 @@ static void launch_one(dim3 g, hipStream_t s, const Operand& a, const Operand& w
     tiled::ClockOut<DIAG != 0> c;
     if constexpr (DIAG != 0) c.p = clk;
     hipLaunchKernelGGL((tiled::k_gemm_tiled<OUT_BF16, MB, DIAG, LINES>), g, dim3(256), tiled::LDS_BYTES, s, a.codes, a.scales, w.codes,
-                       w.scales, M, N, K, y, ldy, (int)a.tiled, (int)w.tiled, c);
+                       w.scales, M, N, K, y, ldy, (int)a.tiled, (int)w.tiled, c, EpilogueArg<false>{});
 }
 
 // The kernels use all 160 KB of the CU's LDS: declared once per device.
 hipError_t setup_gemm_tiled() {
 #define BRQ_TILED(BF, MB) (const void*)tiled::k_gemm_tiled<BF, MB, 0, true>, (const void*)tiled::k_gemm_tiled<BF, MB, 0, false>, \
                           (const void*)tiled::k_gemm_tiled<BF, MB, 1, true>
-    const void* kernels[13] = {BRQ_TILED(true, 4), BRQ_TILED(false, 4), BRQ_TILED(true, 2), BRQ_TILED(false, 2),
-                               (const void*)tiled::k_gemm_tiled<true, 4, 2, true>};
+    const void* kernels[17] = {BRQ_TILED(true, 4), BRQ_TILED(false, 4), BRQ_TILED(true, 2), BRQ_TILED(false, 2),
+                               (const void*)tiled::k_gemm_tiled<true, 4, 2, true>, (const void*)tiled::k_gemm_tiled<true, 4, 0, true, true>,
+                               (const void*)tiled::k_gemm_tiled<true, 4, 0, false, true>, (const void*)tiled::k_gemm_tiled<true, 2, 0, true, true>,
+                               (const void*)tiled::k_gemm_tiled<true, 2, 0, false, true>};
 #undef BRQ_TILED
     for (const void* k : kernels)
         if (hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, tiled::LDS_BYTES); e != hipSuccess) return e;
@@ -671,6 +782,20 @@ hipError_t launch_gemm_tiled(const Operand& a, const Operand& w, int64_t M, int6
         else out_bf16 ? BRQ_LAUNCH(true, 4) : BRQ_LAUNCH(false, 4);
 #undef BRQ_LAUNCH
     }
+    return hipGetLastError();
+}
+
+hipError_t launch_gemm_tiled_with(const Operand& a, const Operand& w, const GemmShape& g, void* y, const Epilogue& e, hipStream_t s, bool half) {
+    int cus = 0;
+    if (hipError_t err = device_cus(&cus); err != hipSuccess) return err;      // (the per-device kernel set-up)
+    const int64_t K = g.padded_k(), T = (half ? (g.M + 127) / 128 : (g.M + 255) / 256) * ((g.N + tiled::TN - 1) / tiled::TN);
+    auto launch = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3((uint32_t)((T + 7) & ~int64_t(7))), dim3(256), tiled::LDS_BYTES, s, a.codes, a.scales, w.codes, w.scales, (int)g.M, (int)g.N, (int)K, y, g.ldy,
+                           (int)a.tiled, (int)w.tiled, tiled::ClockOut<false>{}, EpilogueArg<true>{e});
+    };
+    const bool lines = rows_on(128, reinterpret_cast<uintptr_t>(y), g.ldy * (g.out_bf16 ? 2 : 4));
+    if (half) lines ? launch(tiled::k_gemm_tiled<true, 2, 0, true, true>) : launch(tiled::k_gemm_tiled<true, 2, 0, false, true>);
+    else lines ? launch(tiled::k_gemm_tiled<true, 4, 0, true, true>) : launch(tiled::k_gemm_tiled<true, 4, 0, false, true>);
     return hipGetLastError();
 }
 

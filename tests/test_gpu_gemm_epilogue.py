@@ -121,6 +121,24 @@ def test_one_tile_kernels(brq, route):
                     c.check(on_route(brq, route, c, la, lw), bias, act, res, dt, pad, in_place=res == dt and pad == 0)
 
 
+@pytest.mark.parametrize("route", ["256x256", "128x256"])
+def test_wide_tiles(brq, route):
+    """Rows and columns that end anywhere in a tile that their alignment allows, K of one superstage and of more, more tiles than a round of the chip."""
+    for M, N, K in ((1, 8, 512), (63, 264, 1024), (65, 248, 512), (129, 136, 1536), (255, 512, 2048), (321, 776, 512), (2049, 8200, 1024)):
+        c = Case(M, N, K, seed=M + N)
+        for i, (la, lw) in enumerate(LAYOUTS):
+            for j, (bias, act, res, dt) in enumerate(FORMS):
+                if M > 2000 and (i + j) % 4:
+                    continue
+                for pad in (0, 8):
+                    print("case", route, M, N, K, la, lw, bias, act, res, dt, pad, flush=True)
+                    c.check(on_route(brq, route, c, la, lw), bias, act, res, dt, pad, in_place=res == dt and pad == 0)
+    c = Case(70, 132, 1024, seed=9)                      # whole 16 bytes of fp32 only
+    for bias, act, res, dt in FORMS:
+        if dt == F32:
+            c.check(on_route(brq, route, c, "tiled", "tiled"), bias, act, res, dt, 4)
+
+
 @pytest.mark.parametrize("route,shapes", [("stream", [(1, 96, 512), (16, 33, 1536), (5, 700, 2560), (3, 4, 4096)]), ("skinny", [(1, 40, 96), (16, 17, 544), (7, 300, 32)]),
                                           ("general", [(1, 1, 32), (33, 65, 96), (70, 130, 544)]), ("few", [(1, 5, 512), (16, 33, 512 * 9), (5, 100, 512 * 13), (3, 70, 544), (7, 16, 512 * 2 + 96), (2, 1, 4096)]), ("any_k", [(1, 5, 256), (64, 129, 1056), (65, 128, 288), (200, 300, 4000)])])
 def test_other_kernels(brq, route, shapes):
