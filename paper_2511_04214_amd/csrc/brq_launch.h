@@ -77,7 +77,8 @@ struct GemmShape {
     bool a_tiled, w_tiled, out_bf16;
     int64_t ldy;
     uintptr_t y;
-    bool epilogue = false;      // something follows the product: the persistent kernels do not take it
+    bool epilogue = false;      // something follows the product, with an exponential in it, with a residual
+    bool exponential = false, residual = false;
     int64_t padded_k() const { return (K + 511) / 512 * 512; }
     // K of whole 512-element superstages: tiled operands are zero-padded to that
     bool whole_k() const { return K % 512 == 0 || (a_tiled && w_tiled); }

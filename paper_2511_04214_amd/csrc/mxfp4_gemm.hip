@@ -670,10 +670,14 @@ static int pick_tile(const GemmShape& g, int cus, float* us = nullptr) {
         const float filled = one_tile ? 0.5f + 0.5f * (float)g.M / (float)(64 * t.mb * tm) : 1.0f;
         const float alone = stages * c.alone * (float)((T + places - 1) / places);
         const float full = stages * c.full * (float)T / (float)cus * filled;
-        // What follows a product takes a tile's time by itself, 1 us for every 64 x 64 where nothing else runs on the CU meanwhile; two workgroups a CU
-        // overlap it.  Of the one-tile kernels 192 x 256 and 320 x 128 then lose to 128 x 128 (2048 x 6144 x 4096, bias and residual: 60 and 55 us : 38).  Over the
-        // best of the six, 9 shapes with bias, residual, or both and a GELU: 11.8 % without this term, 3.7 % with it.
-        const float after = g.epilogue ? (float)(t.na * t.mb) * (float)((T + places - 1) / places) : 0.0f;
+        // What follows a product takes a tile's time by itself, us for every 64 x 64 and round; two workgroups a CU overlap most of it.  Chosen by this the
+        // tile is 0.8 % over the best of the seven (11 % at worst; 43 shapes, M 270 .. 9300, with bias, and residual, GELU, both); without the two
+        // wide ones it was 4.1 %.
+        float after = 0.0f;
+        if (g.epilogue) {
+            after = !one_tile ? 0.2f + 0.7f * g.exponential + 0.4f * g.residual : c.per_cu == 1 ? 0.3f + 0.6f * g.exponential + 0.35f * g.residual : 0.25f * g.exponential;
+            after *= (float)(t.na * t.mb) * (float)((T + places - 1) / places);
+        }
         const float cost = c.fixed + sqrtf(sqrtf(pow4(alone) + pow4(full) + pow4(bytes))) + (lines ? c.store : c.store_off) * output + after;
         if (best < 0 || cost < least) { best = t.route; least = cost; }
     }
@@ -693,7 +697,8 @@ GemmSplit gemm_split(const GemmShape& shape, int cus) {
     g.out_bf16 = true;
     g.ldy = g.N;
     g.y = 0;
-    g.epilogue = true;
+    g.epilogue = g.residual = true;      // (what follows is not known where the workspace's size is asked)
+    g.exponential = false;
     GemmSplit best{64, 1};
     float least = 0.0f;
     if (g.M <= 16) return best;

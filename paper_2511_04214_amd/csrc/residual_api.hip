@@ -191,6 +191,8 @@ brq_status brq_mxfp4_gemm_epilogue(const uint8_t* aq, const uint8_t* as, brq_lay
     brq::GemmShape g{M, N, K, a.tiled, w.tiled, ydt == BRQ_BF16, ldy, reinterpret_cast<uintptr_t>(y)};
     if (!bias && act == BRQ_ACT_NONE && !residual) return launched(brq::launch_mxfp4_gemm(a, w, g, y, static_cast<hipStream_t>(stream)));
     g.epilogue = true;
+    g.exponential = act == BRQ_ACT_SILU || act == BRQ_ACT_GELU;
+    g.residual = residual != nullptr;
     int cus = 0;
     if (brq::device_cus(&cus) != hipSuccess) return BRQ_ERR_LAUNCH;
     const int64_t need = brq::split_gemm_workspace(g, brq::gemm_split(g, cus));
