@@ -668,15 +668,16 @@ static int pick_tile(const GemmShape& g, int cus, float* us = nullptr) {
         const TileCost& c = tiled ? t.tiled : one_tile && !mid_gemm_pairs(t.route - ROUTE_ONE_TILE, tiled, g.K) ? t.singles : t.rowmajor;
         const int64_t tm = (g.M + 64 * t.mb - 1) / (64 * t.mb), T = tm * ((g.N + 64 * t.na - 1) / (64 * t.na)), places = (int64_t)cus * c.per_cu;
         const float filled = one_tile ? 0.5f + 0.5f * (float)g.M / (float)(64 * t.mb * tm) : 1.0f;
-        const float alone = stages * c.alone * (float)((T + places - 1) / places);
-        const float full = stages * c.full * (float)T / (float)cus * filled;
-        // What follows a product takes a tile's time by itself, us for every 64 x 64 and round; two workgroups a CU overlap most of it.  Chosen by this the
-        // tile is 0.8 % over the best of the seven (11 % at worst; 43 shapes, M 270 .. 9300, with bias, and residual, GELU, both); without the two
-        // wide ones it was 4.1 %.
+        const int64_t rounds = (T + places - 1) / places;
+        const float alone = stages * c.alone * (float)rounds;
+        const float full = stages * c.full * (float)T / (float)cus * filled * (g.epilogue && !one_tile ? 0.7f + 0.3f * (float)(rounds * cus) / (float)T : 1.0f);
+        // What follows a product takes a tile's time by itself, us for every 64 x 64 and round; two workgroups a CU overlap most of it.  (And the wide tiles'
+        // kernel then goes from tile to tile no more: its last round counts for more than its share.)  Chosen by this the tile is 0.7 % over the best of
+        // the seven (12 % at worst; 47 shapes, M 270 .. 9300, with bias, and residual, GELU, both); without the wide tiles 4.1 %.
         float after = 0.0f;
         if (g.epilogue) {
-            after = !one_tile ? 0.2f + 0.7f * g.exponential + 0.4f * g.residual : c.per_cu == 1 ? 0.3f + 0.6f * g.exponential + 0.35f * g.residual : 0.25f * g.exponential;
-            after *= (float)(t.na * t.mb) * (float)((T + places - 1) / places);
+            after = !one_tile ? 0.2f + 0.7f * g.exponential + 0.6f * g.residual : c.per_cu == 1 ? 0.3f + 0.7f * g.exponential + 0.5f * g.residual : 0.15f + 0.45f * g.exponential;
+            after *= (float)(t.na * t.mb * rounds);
         }
         const float cost = c.fixed + sqrtf(sqrtf(pow4(alone) + pow4(full) + pow4(bytes))) + (lines ? c.store : c.store_off) * output + after;
         if (best < 0 || cost < least) { best = t.route; least = cost; }
