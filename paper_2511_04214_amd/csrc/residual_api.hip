@@ -152,6 +152,7 @@ brq_status brq_add_rms_norm_backward(const void* h, brq_dtype hdt, int64_t ldh, 
     const int64_t need = dw ? brq::norm_backward_parts(M, K) * K * 4 : 0;
     if (need > 0 && !workspace) return BRQ_ERR_NULL;
     if (need > workspace_bytes) return BRQ_ERR_SHAPE;
+    if (M == 0 && !dw) return BRQ_OK;
     brq::NormBackwardArgs a{};
     a.h = rows(h, hdt, ldh);
     a.gy = rows(gy, gdt, ldgy);
