@@ -3,8 +3,8 @@
 // A row is held in registers from its load to its last store: W wavefronts of 64 lanes, each lane C chunks of 8 elements, chunk
 // number (c * W + wavefront) * 64 + chunk_of_lane(lane).  So everything crosses HBM once, and a wavefront's pass c is 512 consecutive
 // elements, in the order that the rotations and the quantizer want (brq_device.h).  Lanes behind the row's end load its last chunk
-// again, in bounds, and hold zeros.  The sum of squares is taken in fp32: in a lane 8 C products in the order of the elements, then
-// pairs of lanes by chunk number, then the wavefronts in turn.  W and C depend on the sizes alone, so the norm alone and the fused
+// again, in bounds, and count for nothing.  The sum of squares is taken in fp32: in a lane 8 C products in the order of the elements, then
+// pairs of lanes by chunk number, then the wavefronts in turn.  W and C depend on K alone, so the norm alone and the fused
 // call have the same bits.
 #include "mfma_fp4.h"
 #include "brq_launch.h"
@@ -170,10 +170,14 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*part)[N], int wa
     }
 }
 
-// A workgroup goes through rows with a stride: the weight stays in its registers, and the next row is asked for before this one's sum is waited for.
+// A workgroup for every row (or 4 / W of them), everything asked for at once, and registers for nothing beyond it: 31 to 63 with up to two chunks a lane, so that a
+// CU holds 2048 threads of them.  (In a loop over rows the compiler keeps so much from turn to turn that it has 80 to 128.)
+// Many rows are bound by HBM, few by the launch and the chain load, sum, barrier, store.  us in a graph, bf16 in and out with the sum, a loop over rows -> now, alone / fused with B = 32:
+// 1 x 4096 2.6 -> 2.5 / 3.1 -> 2.8, 300 x 8192 6.1 -> 5.3 / 7.0 -> 6.2, 4096 x 1056 8.7 -> 7.4 / 10.7 -> 9.3, 4096 x 8192 41 -> 39 (6.8 TB/s, part of it from the memory-side
+// cache) / 40 -> 38, 2048 x 16384 43 -> 40 / 43 -> 35, 1024 x 32768 66 -> 47 / 55 -> 43.  A residual in fp32: 3 % either way (8192 x 4096 74, 5.4 TB/s).
 template <int W, int C, bool QUANT>
-__global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm(const NormArgs a, const KPad pad) {
-    __shared__ float part[2][threads_of<W> / 64][1];
+__global__ __launch_bounds__(threads_of<W>, C <= 2 ? 8 : 1) void k_add_rms_norm(const NormArgs a, const KPad pad, int64_t row0) {
+    __shared__ float part[threads_of<W> / 64][1];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), sub = wave % W;
     const uint32_t lane = threadIdx.x & 63u, chunk = chunk_of_lane(lane), n = (uint32_t)(a.K / 8);
     uint32_t kc[C];
@@ -184,92 +188,67 @@ __global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm(const NormArgs a
         in[c] = kc[c] < n;
         kc[c] = min(kc[c], n - 1);
     }
-    // up to 2 chunks a lane there are registers for the weight and the next row; above, a row is asked for when its turn comes
-    constexpr bool AHEAD = C <= 2;
-    Raw<C> rx, rr;
-    auto fetch = [&](int64_t first) __attribute__((always_inline)) {
-        const int64_t row = min(first + wave / W, a.M - 1);
-        rx.load(a.x.p + row * a.x.pitch, a.x.bf16, kc);
-        if (a.res.p) rr.load(a.res.p + row * a.res.pitch, a.res.bf16, kc);
-    };
-    if constexpr (AHEAD) fetch((int64_t)blockIdx.x * rows_of<W>);
-    float w[C][8];
-    if (AHEAD && a.w) load_weight(a.w, kc, w);
-    int turn = 0;
-    // (uniform over the workgroup: every thread meets every barrier of row_sums)
-    for (int64_t first = (int64_t)blockIdx.x * rows_of<W>; first < a.M; first += (int64_t)gridDim.x * rows_of<W>) {
-        const int64_t mine = first + wave / W, row = mine < a.M ? mine : a.M - 1;
-        float v[C][8];
-        auto add = [&](float (&x)[8], const float (&r)[8]) __attribute__((always_inline)) {
+    const int64_t mine = row0 + (int64_t)blockIdx.x * rows_of<W> + wave / W, row = min(mine, a.M - 1);
+    float v[C][8], w[C][8];
+    {
+        Raw<C> x, r;
+        x.load(a.x.p + row * a.x.pitch, a.x.bf16, kc);
+        if (a.res.p) r.load(a.res.p + row * a.res.pitch, a.res.bf16, kc);           // uniform
+        if (C <= 2 && a.w) load_weight(a.w, kc, w);
+        x.widen(a.x.bf16, v);
+        if (a.res.p) {
+            float t[C][8];
+            r.widen(a.res.bf16, t);
+            static_for([&](auto c_) __attribute__((always_inline)) {
+                constexpr int c = decltype(c_)::value;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] += r[i];
-            if (a.res.bf16) through_bf16(x);
-        };
-        if constexpr (AHEAD) {
-            rx.widen(a.x.bf16, v);
-            if (a.res.p) {      // uniform
-                float r[C][8];
-                rr.widen(a.res.bf16, r);
-                static_for([&](auto c_) __attribute__((always_inline)) { constexpr int c = decltype(c_)::value; add(v[c], r[c]); }, IC<C>{});
-            }
+                for (int i = 0; i < 8; ++i) v[c][i] += t[c][i];
+                if (a.res.bf16) through_bf16(v[c]);
+            }, IC<C>{});
+        }
+    }
+    // (all that was asked for is here before the sum is stored: else the compiler waits for that store too, in front of the squares)
+    __builtin_amdgcn_s_waitcnt(0x0F70);                 // vmcnt(0)
+    if (a.h.p) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (in[c] && mine < a.M) store_values(a.h.p + row * a.h.pitch, a.h.bf16, kc[c], v[c]);
+    }
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = __builtin_fmaf(v[c][i], v[c][i], s);
+        sum[0] += in[c] ? s : 0.0f;
+    }
+    row_sums<W, 1>(sum, part, wave);
+    const float r = 1.0f / sqrtf(sum[0] / (float)a.K + a.eps);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const bool live = in[c] && mine < a.M;
+        if constexpr (C > 2) {                          // (no registers to have it earlier)
+            __builtin_amdgcn_sched_barrier(0);
+            if (a.w) load_chunk_weight(a.w, kc[c], w[c]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[c][i] *= r;
+            if (a.w) v[c][i] *= w[c][i];
+        }
+        if constexpr (!QUANT) {
+            if (live) store_values(a.y.p + row * a.y.pitch, a.y.bf16, kc[c], v[c]);
         } else {
-            renew(kc);
-            load_row(a.x, row, kc, v);
-            if (a.res.p) {
-                const uint8_t* const from = a.res.p + row * a.res.pitch;
-                static_for([&](auto c_) __attribute__((always_inline)) {
-                    constexpr int c = decltype(c_)::value;
-                    float r[8];
-                    load_one(from, a.res.bf16, kc[c], r);
-                    add(v[c], r);
-                    if constexpr (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
-                }, IC<C>{});
-            }
-        }
-        const int64_t next = first + (int64_t)gridDim.x * rows_of<W>;
-        if (AHEAD && next < a.M) fetch(next);
-        if (a.h.p) {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (in[c] && mine < a.M) store_values(a.h.p + row * a.h.pitch, a.h.bf16, kc[c], v[c]);
-        }
-        float sum[1] = {0.0f};
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            float s = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s = __builtin_fmaf(v[c][i], v[c][i], s);
-            sum[0] += in[c] ? s : 0.0f;
-        }
-        // (the sums' places alternate: the next row's are written while others still read these)
-        row_sums<W, 1>(sum, part[turn], wave);
-        turn ^= 1;
-        if constexpr (!AHEAD) renew(kc);
-        const float r = 1.0f / sqrtf(sum[0] / (float)a.K + a.eps);
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const bool live = in[c] && mine < a.M;
-            if constexpr (!AHEAD) __builtin_amdgcn_sched_barrier(0);
-            if (!AHEAD && a.w) load_chunk_weight(a.w, kc[c], w[c]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[c][i] *= r;
-                if (a.w) v[c][i] *= w[c][i];
-            }
-            if constexpr (!QUANT) {
-                if (live) store_values(a.y.p + row * a.y.pitch, a.y.bf16, kc[c], v[c]);
-            } else {
-                // (whole quads, and whole blocks, are behind the row's end together: what they hold reaches no one else)
-                if (a.y.bf16) through_bf16(v[c]);
-                if (a.signs) apply_signs(v[c], a.signs + (size_t)kc[c] * 8);
-                rotate(v[c], a.l2b, chunk);
-                const uint32_t sb = e8m0_from_amax(quad_max(absmax8(v[c]))), codes = encode8_e2m1(v[c], sb);
-                if (live) {
-                    const uint64_t at = a.tiled ? tiled_code_offset((uint32_t)row, kc[c], pad.stages) : ((uint64_t)row * n + kc[c]) * 4u;
-                    const uint64_t sat = a.tiled ? tiled_scale_offset((uint32_t)row, kc[c], pad.sstages) : ((uint64_t)row * n + kc[c]) >> 2;
-                    *reinterpret_cast<uint32_t*>(a.codes + at) = codes;
-                    if ((lane & 3u) == 0) a.scales[sat] = (uint8_t)sb;
-                }
+            // (whole quads, and whole blocks, are behind the row's end together: what they hold reaches no one else)
+            if (a.y.bf16) through_bf16(v[c]);
+            if (a.signs) apply_signs(v[c], a.signs + (size_t)kc[c] * 8);
+            rotate(v[c], a.l2b, chunk);
+            const uint32_t sb = e8m0_from_amax(quad_max(absmax8(v[c]))), codes = encode8_e2m1(v[c], sb);
+            if (live) {
+                const uint64_t at = a.tiled ? tiled_code_offset((uint32_t)row, kc[c], pad.stages) : ((uint64_t)row * n + kc[c]) * 4u;
+                const uint64_t sat = a.tiled ? tiled_scale_offset((uint32_t)row, kc[c], pad.sstages) : ((uint64_t)row * n + kc[c]) >> 2;
+                *reinterpret_cast<uint32_t*>(a.codes + at) = codes;
+                if ((lane & 3u) == 0) a.scales[sat] = (uint8_t)sb;
             }
         }
     }
@@ -291,16 +270,18 @@ hipError_t launch_add_rms_norm(const NormArgs& a, bool quantize, hipStream_t str
     int cus = 0;
     if (hipError_t e = device_cus(&cus); e != hipSuccess) return e;
     const Split sp = split_of(a.K);
+    constexpr int64_t most = int64_t(1) << 21;          // workgroups of a launch, which has less than 2^32 threads
     const KPad pad = KPad::of(quantize && a.tiled, a.codes, a.scales, a.M, a.K);
     switch (sp.w * 16 + sp.c) {
 #define BRQ_NORM(W, C)                                                                                                                             \
-    case W * 16 + C: {                                                                                                                             \
-        const int64_t rows = (a.M + rows_of<W> - 1) / rows_of<W>, most = (int64_t)cus * (1024 / threads_of<W>);                             \
-        const dim3 grid((uint32_t)(rows < most ? rows : most)), block(threads_of<W>);                                                              \
-        if (quantize) hipLaunchKernelGGL((k_add_rms_norm<W, C, true>), grid, block, 0, stream, a, pad);                                            \
-        else hipLaunchKernelGGL((k_add_rms_norm<W, C, false>), grid, block, 0, stream, a, pad);                                                    \
-        break;                                                                                                                                     \
-    }
+    case W * 16 + C:                                                                                                                               \
+        for (int64_t row = 0; row < a.M; row += most * rows_of<W>) {                                                                               \
+            const int64_t rows = (a.M - row + rows_of<W> - 1) / rows_of<W>;                                                                       \
+            const dim3 grid((uint32_t)(rows < most ? rows : most)), block(threads_of<W>);                                                          \
+            if (quantize) hipLaunchKernelGGL((k_add_rms_norm<W, C, true>), grid, block, 0, stream, a, pad, row);                                   \
+            else hipLaunchKernelGGL((k_add_rms_norm<W, C, false>), grid, block, 0, stream, a, pad, row);                                           \
+        }                                                                                                                                          \
+        break;
         BRQ_NORM(1, 1) BRQ_NORM(2, 1) BRQ_NORM(4, 1) BRQ_NORM(8, 1) BRQ_NORM(16, 1) BRQ_NORM(16, 2) BRQ_NORM(16, 4)
 #undef BRQ_NORM
         default: return hipErrorInvalidValue;

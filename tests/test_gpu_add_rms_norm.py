@@ -268,3 +268,29 @@ def test_refused_tensors(brq):
             brq.add_rms_norm_rotate_quantize_fused(x, 32, y_dtype=torch.float16, stream=stream)
         with pytest.raises(brq.BrqError):
             brq.add_rms_norm_rotate_quantize_fused(x, 128, stream=stream)
+
+
+def test_more_rows_than_a_launch_takes(brq):
+    """More than 2^21 groups of rows: the rows on both sides of the border and the last ones are as they are alone, and no other row is missing."""
+    g = torch.Generator().manual_seed(11)
+    border, K = 1 << 23, 32                             # (four rows a workgroup)
+    M = border + 6
+    x = torch.full((M, K), 0.5, dtype=BF16, device="cuda")
+    x[border - 5:] = rand(g, 11, K, dtype=BF16)
+    w = rand(g, K)
+    y, h = brq.add_rms_norm(x, residual=x, weight=w)
+    q, s, _ = brq.add_rms_norm_rotate_quantize_fused(x, 32, residual=x, weight=w, want_h=False)
+    for i, t in enumerate((y, h, q, s)):
+        few = x[border - 6:].clone()
+        assert torch.equal(t[border - 6:], (*brq.add_rms_norm(few, residual=few, weight=w), *brq.add_rms_norm_rotate_quantize_fused(few, 32, residual=few, weight=w)[:2])[i])
+        assert torch.equal(t[: border - 5].amax(0), t[0]) and torch.equal(t[: border - 5].amin(0), t[0])
+    T = border + 64                                     # tiled: whole slabs of 64 rows, K padded to 512 with zeros
+    x = torch.full((T, K), 0.5, dtype=BF16, device="cuda")
+    x[-70:] = rand(g, 70, K, dtype=BF16)
+    codes, scales = (torch.full((T * n,), 255, dtype=torch.uint8, device="cuda") for n in (256, 16))
+    brq.add_rms_norm_rotate_quantize_fused(x, 32, weight=w, codes=codes, scales=scales, layout="tiled")
+    few = x[-128:].clone()
+    c, s, _ = brq.add_rms_norm_rotate_quantize_fused(few, 32, weight=w, layout="tiled")
+    assert torch.equal(codes[-c.numel():], c) and torch.equal(scales[-s.numel():], s)
+    slabs = codes.view(-1, 64 * 256)[:-2]
+    assert torch.equal(slabs.amax(0), slabs[0]) and torch.equal(slabs.amin(0), slabs[0])
