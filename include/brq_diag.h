@@ -81,7 +81,8 @@ enum {
     BRQ_GEMM_320x128 = 9,
     BRQ_GEMM_256x128 = 10,
     BRQ_GEMM_ANY_K = 11,         /* any shape with K of at least 256, through LDS */
-    BRQ_GEMM_EPILOGUE_FEW = 12   /* of brq_mxfp4_gemm_epilogue alone: M <= 16, K of whole 512-element superstages */
+    BRQ_GEMM_EPILOGUE_FEW = 12   /* of brq_mxfp4_gemm_epilogue alone: K of whole 512-element superstages, M <= 16 with any
+                                    such K, M <= 32, 48, 64 with K up to 16384, 12288, 8192 */
 };
 
 /*

@@ -141,7 +141,8 @@ hipError_t launch_gemm_any_k_with(const Operand& a, const Operand& w, int64_t M,
 hipError_t launch_gemm_mid_with(int tile, const Operand& a, const Operand& w, int64_t M, int64_t N, int64_t K, void* y,
                                 bool out_bf16, int64_t ldy, hipStream_t s, const Epilogue& epi);
 
-// Up to 16 rows, K of whole superstages (mxfp4_gemm_few.hip).
+// Up to 64 rows, K of whole superstages (mxfp4_gemm_few.hip).
+bool few_gemm_supported(const GemmShape& g);
 hipError_t launch_gemm_few(const Operand& a, const Operand& w, const GemmShape& g, void* y, const Epilogue& epi, hipStream_t s);
 
 // The one-tile kernels split along K, with what follows the product where the slices are joined (mxfp4_gemm_split.hip).

@@ -686,6 +686,34 @@ static int pick_tile(const GemmShape& g, int cus, float* us = nullptr) {
     return best;
 }
 
+// With something behind the product, up to 16 rows: split along K over a workgroup's wavefronts (mxfp4_gemm_few.hip) or streamed.  The former starts a
+// workgroup for 16 columns, which has to pay: few columns or a long K, and with row-major operands, whose lines it asks for in halves, few rows or
+// few columns.  Its time over the streaming kernel's, 1 / 16 rows (182 shapes): tiled, N <= 4096, K = 512 1.03 / 1.05, K = 1024 0.91 / 0.94, K = 4096 0.63 /
+// 0.67, 16384 0.58 / 0.64; N 6144 to 12288, K = 1024 1.07 / 1.15, 2048 0.95 / 0.98, 4096 0.76 / 0.84, 8192 0.92 / 0.94, 16384 1.00 / 1.10; N from 16384,
+// K = 2048 1.07 / 1.13, 4096 0.86 / 0.97, 8192 1.03 / 1.10.  Row-major, N <= 4096, K = 1024 1.02 / 1.13, 2048 0.86 / 0.96, from 4096 0.62 / 0.78; N above,
+// K = 2048 1.20 / 1.49, from 4096 1 / 4 / 8 / 16 rows 0.89 / 0.95 / 1.03 / 1.12.
+// 17 to 64 rows, against one-tile kernels and those split along K, 24 / 32 / 48 / 64 rows (all on either side of a border, 420 shapes in all): tiled, N = 4096, K = 512 0.80 / 0.80 / 0.96 /
+// 1.07, 1024 0.73 / 0.74 / 0.87 / 1.00, 4096 0.55 / 0.54 / 0.59 / 0.63, 8192 0.67 / 0.68 / 0.75 / 0.81, 11264 0.74 / 0.76 / 0.86 / 0.93, 16384 0.85 / 0.88 / 0.99 / 1.02; N = 8192, K = 1024
+// 0.95 / 0.96 / 1.09 / 1.23, 2048 0.86 / 0.87 / 0.98 / 1.10, 4096 0.67 / 0.67 / 0.85 / 0.93, 8192 0.85 / 0.84 / 0.88 / 0.92, 16384 0.86 / 0.88 / 1.04; N = 12288, K = 2048 1.03 / 1.06 /
+// 1.19 / 1.33, 4096 0.79 / 0.80 / 0.86 / 0.91, 8192 0.86 / 0.88 / 0.86 / 0.90, 11264 0.92 / 0.93; N = 14336 0.9 to 2.  Row-major, N = 4096, K = 1024 0.89 / 0.93 / 1.13 / 1.33, 4096
+// 0.62 / 0.66 / 0.74 / 0.80, 8192 0.81 / 0.83 / 1.02 / 1.15; N = 8192, K = 2048 0.98 / 1.01 / 1.15 / 1.33, 4096 0.73 / 0.81 / 0.89 / 1.01, 8192 0.91 / 0.94 / 1.00 / 1.15; N = 12288,
+// K = 4096 0.75 / 0.76 / 0.81 / 0.91, 8192 0.90 / 0.93 / 1.05.
+static bool gemm_few_faster(const GemmShape& g, int cus) {
+    if (!gemm_route_supported(ROUTE_FEW, g)) return false;
+    const bool tiled = g.a_tiled && g.w_tiled;
+    if (g.M > 16) {
+        static const struct { int64_t from, to; } K[2][3][3] = {      // [tiled][columns][tiles of 16 rows, from 2 on]
+            {{{1024, 8192}, {2048, 4096}, {4096, 4096}}, {{4096, 8192}, {4096, 4096}, {1, 0}}, {{4096, 12288}, {4096, 6144}, {4096, 4096}}},
+            {{{512, 16384}, {512, 12288}, {1024, 8192}}, {{1024, 16384}, {2048, 12288}, {4096, 8192}}, {{4096, 12288}, {4096, 8192}, {4096, 8192}}}};
+        if (g.N > 48 * (int64_t)cus) return false;
+        const auto& k = K[tiled][g.N <= 16 * (int64_t)cus ? 0 : g.N <= 32 * (int64_t)cus ? 1 : 2][(g.M - 1) / 16 - 1];
+        return g.K >= k.from && g.K <= k.to;
+    }
+    if (g.N <= 16 * (int64_t)cus) return g.K >= (tiled ? 1024 : 2048);
+    if (!tiled) return g.K >= 4096 && g.M <= 4;
+    return g.N <= 48 * (int64_t)cus ? g.K >= 2048 : g.K >= 4096 && g.K < 8192;
+}
+
 // Whether to split a product with something behind it along K: for few tiles and a long K.  By the same estimate, with a slice's stages for K's and
 // its tiles times the slices; `alone` is 1.36 of the table's (a stage's operands come from HBM, and nobody else's are on their way), a second
 // workgroup on a CU costs 0.88 of a first (whole tiles of these two are held against that), and where some CUs have one more than others the bytes take longer by that imbalance to the power 0.6.  The join,
@@ -702,7 +730,7 @@ GemmSplit gemm_split(const GemmShape& shape, int cus) {
     g.exponential = false;
     GemmSplit best{64, 1};
     float least = 0.0f;
-    if (g.M <= 16) return best;
+    if (g.M <= 16 || gemm_few_faster(g, cus)) return best;
     const int whole = pick_tile(g, cus, &least);
     if (whole < 0) return best;
     const bool tiled = g.a_tiled && g.w_tiled;
@@ -738,7 +766,7 @@ bool gemm_route_supported(int route, const GemmShape& g) {
         case ROUTE_256x256:
         case ROUTE_128x256: return tiled_gemm_supported(g.M, g.N, g.K, g.out_bf16, g.ldy, g.a_tiled && g.w_tiled);
         case ROUTE_ANY_K: return g.K >= 256;
-        case ROUTE_FEW: return g.epilogue && gemm_route_supported(ROUTE_STREAM, g);
+        case ROUTE_FEW: return g.epilogue && few_gemm_supported(g);
         default: return route >= ROUTE_ONE_TILE && route < ROUTE_ANY_K && mid_gemm_supported(route - ROUTE_ONE_TILE, g);
     }
 }
@@ -772,20 +800,6 @@ static bool any_k(const GemmShape& g) {
     if (g.K < 256) return false;
     if (g.M <= 64) return g.K >= 2048 || (g.N + 127) / 128 * g.K >= 65536;
     return g.K >= 4096 || (double)((g.M + 31) / 32) * (double)((g.N + 31) / 32) * (double)g.K >= (double)(1 << 20);
-}
-
-// With something behind the product, up to 16 rows: split along K over a workgroup's wavefronts (mxfp4_gemm_few.hip) or streamed.  The former starts a
-// workgroup for 16 columns, which has to pay: few columns or a long K, and with row-major operands, whose lines it asks for in halves, few rows or
-// few columns.  Its time over the streaming kernel's, 1 / 16 rows (182 shapes): tiled, N <= 4096, K = 512 1.03 / 1.05, K = 1024 0.91 / 0.94, K = 4096 0.63 /
-// 0.67, 16384 0.58 / 0.64; N 6144 to 12288, K = 1024 1.07 / 1.15, 2048 0.95 / 0.98, 4096 0.76 / 0.84, 8192 0.92 / 0.94, 16384 1.00 / 1.10; N from 16384,
-// K = 2048 1.07 / 1.13, 4096 0.86 / 0.97, 8192 1.03 / 1.10.  Row-major, N <= 4096, K = 1024 1.02 / 1.13, 2048 0.86 / 0.96, from 4096 0.62 / 0.78; N above,
-// K = 2048 1.20 / 1.49, from 4096 1 / 4 / 8 / 16 rows 0.89 / 0.95 / 1.03 / 1.12.
-static bool gemm_few_faster(const GemmShape& g, int cus) {
-    if (!gemm_route_supported(ROUTE_FEW, g)) return false;
-    const bool tiled = g.a_tiled && g.w_tiled;
-    if (g.N <= 16 * (int64_t)cus) return g.K >= (tiled ? 1024 : 2048);
-    if (!tiled) return g.K >= 4096 && g.M <= 4;
-    return g.N <= 48 * (int64_t)cus ? g.K >= 2048 : g.K >= 4096 && g.K < 8192;
 }
 
 int gemm_route(const GemmShape& g, int cus) {

@@ -153,6 +153,33 @@ def test_other_kernels(brq, route, shapes):
                     c.check(on_route(brq, route, c, la, lw), bias, act, res, dt, pad, in_place=res == dt and pad == 8)
 
 
+# N: a ragged tile of 16, 32 and 48 columns (which of the three is by N); K: 1 to 4 superstages a wavefront, the last one's not all there, tiled ones that end inside a superstage
+@pytest.mark.parametrize("N", [1, 100, 4099, 8213])
+@pytest.mark.parametrize("M,Ks", [(17, (512, 4096 + 32, 8192 + 512, 16384)), (32, (4096, 8192, 12288 + 512)), (33, (512 + 96, 4096, 8192, 12288)), (48, (4096 + 512, 8192 + 512)),
+                                  (49, (512, 4096, 4096 + 512)), (64, (4096 - 32, 8192))])
+def test_up_to_64_rows(brq, M, Ks, N):
+    for i, K in enumerate(Ks):
+        c = Case(M, N, K, seed=M + N)
+        for j, (la, lw) in enumerate(LAYOUTS):
+            if K % 512 and (la, lw) != ("tiled", "tiled"):
+                continue
+            for k, (bias, act, res, dt) in enumerate(FORMS):
+                if (i + j + k) % 3:
+                    continue
+                pad = 8 * (k % 2)
+                print("case", M, N, K, la, lw, bias, act, res, dt, pad, flush=True)
+                c.check(on_route(brq, "few", c, la, lw), bias, act, res, dt, pad, in_place=res == dt and pad == 8)
+
+
+def test_few_rows_refuse_longer_k(brq):
+    """What the kernels for up to 64 rows do not take is refused by name, and taken by the call."""
+    for M, K in ((17, 16384 + 512), (33, 12288 + 512), (49, 8192 + 512), (65, 512)):
+        c = Case(M, 40, K, seed=K)
+        with pytest.raises(RuntimeError, match="shape"):
+            c.check(on_route(brq, "few", c, "tiled", "tiled"), True, None, None, BF16)
+        c.check(lambda out, bias, act, res: brq.mxfp4_gemm_epilogue(*c.a["tiled"], *c.w["tiled"], out=out, bias=bias, a_layout="tiled", w_layout="tiled", M=M, N=40, K=K), True, None, None, BF16)
+
+
 @pytest.mark.parametrize("route", ["64x128", "128x128"])
 def test_split_along_k(brq, route):
     """Slices of equal and unequal length, to 16; row-major K that ends inside the last slice's last superstage."""
@@ -187,7 +214,7 @@ def test_long_k_of_few_rows(brq):
 
 def test_the_call(brq):
     """Through the dispatcher, both ways of the binding; what the call makes, takes and returns."""
-    for M, N, K in ((1, 256, 512), (16, 200, 544), (40, 72, 96), (100, 520, 1024), (300, 136, 2048), (130, 1000, 1056), (700, 260, 512), (48, 260, 7168)):
+    for M, N, K in ((1, 256, 512), (16, 200, 544), (40, 72, 96), (100, 520, 1024), (300, 136, 2048), (130, 1000, 1056), (700, 260, 512), (48, 260, 7168), (130, 260, 7168)):
         c = Case(M, N, K, seed=K)
         for la, lw in LAYOUTS:
             kw = dict(a_layout=la, w_layout=lw, M=M, N=N, K=K)
@@ -202,7 +229,7 @@ def test_the_call(brq):
                                                   stream=stream, **kw)
                     assert new.dtype == dt and torch.equal(new, got)
         need = brq.mxfp4_gemm_epilogue_workspace(M, N, K, "tiled", "tiled")
-        assert (need > 0) == (K == 7168)
+        assert (need > 0) == ((M, K) == (130, 7168))
         if need:                                         # few tiles and a long K: split, in a workspace of the caller's too
             assert need % (M * N * 4) == 0
             kw = dict(a_layout="tiled", w_layout="tiled", M=M, N=N, K=K)

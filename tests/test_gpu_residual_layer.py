@@ -64,8 +64,8 @@ class Layer:
         return values(*(q if self.layout == "rowmajor" else self.brq.to_rowmajor(*q, M, K)))
 
 
-# one token, few, a batch whose second product is split along K, a ragged prompt; blocks as wide as a wavefront holds
-@pytest.mark.parametrize("T,D,F,B,dtype,layout", [(1, 256, 1024, 32, BF16, "tiled"), (13, 512, 2048, 64, F32, "tiled"), (48, 256, 7168, 32, BF16, "tiled"),
+# one token, few, a batch in decoding, one whose second product is split along K, a ragged prompt; blocks as wide as a wavefront holds
+@pytest.mark.parametrize("T,D,F,B,dtype,layout", [(1, 256, 1024, 32, BF16, "tiled"), (13, 512, 2048, 64, F32, "tiled"), (48, 256, 7168, 32, BF16, "tiled"), (130, 256, 7168, 32, BF16, "tiled"),
                                                   (300, 512, 1536, 512, BF16, "rowmajor"), (700, 544, 1056, 32, F32, "rowmajor")])
 def test_layer(brq, T, D, F, B, dtype, layout):
     m = Layer(brq, T, D, F, B, dtype, layout)
