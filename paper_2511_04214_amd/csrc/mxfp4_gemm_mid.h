@@ -137,7 +137,7 @@ __device__ __forceinline__ void store_tile(v16f (&acc)[NA][MB], uint8_t* lds, vo
     }, IC<NM>{});
 }
 
-// The residuals of a wavefront's part of a tile as they lie in memory, where all 8 columns of a lane's are there: of bf16 lo.xy and lo.zw, of fp32 lo and hi.
+// The residuals of a wavefront's part of a tile as they lie in memory, two of bf16 to a register: lo, of fp32 lo and hi.
 // A lane has 8 columns of rows (lane >> 3) + 8 j of every 32 x 64 block: for bf16 out 8 neighbours, for fp32 out 4 of each half.
 template <int NA, int MB>
 struct TileResiduals {
@@ -156,7 +156,7 @@ struct TileResiduals {
         for (int x = 0; x < NB; ++x) {
             const int row = (x % MB) * 32, col = (x / MB) * 64 + o0;
             const uint8_t* const at = e.res + (row0 + row) * e.res_pitch + (col0 + col) * (e.res_bf16 ? 2 : 4);
-            const int64_t mr = e.res && N - col0 - col >= O1 + 4 ? M - row0 - row : 0;
+            const int64_t left = N - col0 - col, mr = e.res && left > 0 ? M - row0 - row : 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 // (values of their own until all branches have met: a branch that ends by storing to these arrays, next to another that does,
@@ -164,7 +164,20 @@ struct TileResiduals {
                 u4 l = {0, 0, 0, 0}, h = {0, 0, 0, 0};
                 if (8 * j < mr) {
                     const uint8_t* const p = at + (int64_t)(8 * j) * e.res_pitch;
-                    if (!e.res_bf16) {
+                    if (left < O1 + 4) {                       // a row's last columns, one by one; past the last: the last one
+                        unsigned int t[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int64_t o = min((int64_t)(k < 4 ? k : O1 + k - 4), left - 1);
+                            t[k] = e.res_bf16 ? (unsigned int)reinterpret_cast<const uint16_t*>(p)[o] : reinterpret_cast<const unsigned int*>(p)[o];
+                        }
+                        if (e.res_bf16) {
+                            l = u4{t[0] | t[1] << 16, t[2] | t[3] << 16, t[4] | t[5] << 16, t[6] | t[7] << 16};
+                        } else {
+                            l = u4{t[0], t[1], t[2], t[3]};
+                            h = u4{t[4], t[5], t[6], t[7]};
+                        }
+                    } else if (!e.res_bf16) {
                         l = *reinterpret_cast<const u4_any*>(p);
                         h = *reinterpret_cast<const u4_any*>(p + 4 * O1);
                     } else if (bf16) {
@@ -185,6 +198,8 @@ struct TileResiduals {
 // time, 8 KB of a wavefront's own (`lds`: 32 KB that nobody reads any more), 16-byte chunk c of row i at i * 256 + ((c ^ (i & 15)) << 4).  For bf16
 // out a lane then stores 16 bytes a row, for fp32 out twice 16, each time 128 contiguous bytes per 8 lanes.  The residuals of the whole tile are
 // asked for before the first is used, and on the small tiles before the last superstage.
+// A lane with a row's last columns goes the same way and stores (and asks for residuals) element by element, in bounds: us, each of its 32 elements by itself ->
+// now, bias / bf16 residual too: 100 x 575 x 512 11.4 -> 6.6 / 14.6 -> 8.9, 1000 x 4001 x 4096 18.2 -> 15.5 / 19.4 -> 18.5, fp32 out 1000 x 4000 x 4096 26.3 -> 18.6.
 // (The output's type is looked at here: as a template's argument it doubles what there is to compile.)
 template <int NA, int MB>
 __device__ __forceinline__ void store_tile_with(const Epilogue& e, v16f (&acc)[NA][MB], const TileResiduals<NA, MB>& res, uint8_t* lds, void* y, int64_t ldy, int64_t m0, int64_t n0, int M, int N, int lines) {
@@ -223,7 +238,7 @@ __device__ __forceinline__ void store_tile_with(const Epilogue& e, v16f (&acc)[N
         }, IC<2>{});
         const int64_t left = ncols - A0 * 32 - o0;             // columns from the lane's first on
         const int64_t mr = mrem - B * 32;                      // rows
-        if (left >= O1 + 4) {
+        if (left > 0) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int i = i0 + 8 * j;
@@ -250,25 +265,20 @@ __device__ __forceinline__ void store_tile_with(const Epilogue& e, v16f (&acc)[N
                     if (lines) __builtin_nontemporal_store(o, reinterpret_cast<u4*>(to));       // uniform
                     else *reinterpret_cast<u4_any*>(to) = o;
                 };
-                if (bf16) {
+                if (left < O1 + 4) {                           // a row's last columns, one by one
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int o = k < 4 ? k : O1 + k - 4;
+                        if (o >= left) continue;
+                        if (bf16) reinterpret_cast<uint16_t*>(p)[o] = (uint16_t)f32_to_bf16_bits(v[k]);
+                        else reinterpret_cast<float*>(p)[o] = v[k];
+                    }
+                } else if (bf16) {
                     store(p, u4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
                 } else {
                     store(p, u4{as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3])});
                     store(p + 128, u4{as_u32(v[4]), as_u32(v[5]), as_u32(v[6]), as_u32(v[7])});
                 }
-            }
-        } else if (left > 0) {                                 // a row's last columns, one by one
-#pragma unroll 1
-            for (int jk = 0; jk < 32; ++jk) {
-                const int j = jk >> 3, k = jk & 7, i = i0 + 8 * j, o = k < 4 ? k : O1 + k - 4, at = o0 + o;
-                if (8 * j >= mr || o >= left) continue;
-                float v[1] = {*reinterpret_cast<const float*>(ebuf + i * 256 + (((at >> 2) ^ (i & 15)) << 4) + (at & 3) * 4)};
-                const int64_t row = row0 + B * 32 + 8 * j, col = col0 + A0 * 32 + at;
-                if (e.bias) v[0] += e.bias[col];
-                activate(v, e.act);
-                if (e.res) v[0] += residual_at(e, row, col);
-                if (bf16) reinterpret_cast<uint16_t*>(y)[row * ldy + col] = (uint16_t)f32_to_bf16_bits(v[0]);
-                else reinterpret_cast<float*>(y)[row * ldy + col] = v[0];
             }
         }
     }, IC<NB>{});
