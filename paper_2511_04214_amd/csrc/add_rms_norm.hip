@@ -172,9 +172,9 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*part)[N], int wa
 
 // A workgroup for every row (or 4 / W of them), everything asked for at once, and registers for nothing beyond it: 31 to 63 with up to two chunks a lane, so that a
 // CU holds 2048 threads of them.  (In a loop over rows the compiler keeps so much from turn to turn that it has 80 to 128.)
-// Many rows are bound by HBM, few by the launch and the chain load, sum, barrier, store.  us in a graph, bf16 in and out with the sum, a loop over rows -> now, alone / fused with B = 32:
-// 1 x 4096 2.6 -> 2.5 / 3.1 -> 2.8, 300 x 8192 6.1 -> 5.3 / 7.0 -> 6.2, 4096 x 1056 8.7 -> 7.4 / 10.7 -> 9.3, 4096 x 8192 41 -> 39 (6.8 TB/s, part of it from the memory-side
-// cache) / 40 -> 38, 2048 x 16384 43 -> 40 / 43 -> 35, 1024 x 32768 66 -> 47 / 55 -> 43.  A residual in fp32: 3 % either way (8192 x 4096 74, 5.4 TB/s).
+// Many rows are bound by HBM, few by the launch and the chain load, sum, barrier, store.  us, bf16 in and out with the sum, inputs in no cache, a loop over rows -> now, alone / fused with
+// B = 32: 1 x 4096 2.8 -> 2.7 / 3.3 -> 3.0, 4096 x 2048 14.6 -> 14.8 / 15.0 -> 14.0, 4096 x 4096 26.1 -> 25.9 (5.2 TB/s) / 26.8 -> 25.2, 4096 x 6144 40.3 -> 40.4 / 46.9 -> 36.2, 4096 x 8192
+// 50.4 -> 51.0 / 53.4 -> 46.5, 4096 x 16384 102 -> 100 / 100 -> 90, in the caches 1024 x 32768 66 -> 47 / 55 -> 43.  A residual in fp32: 8192 x 4096 76 (5.3 TB/s), 8192 x 8192 146 -> 149.
 template <int W, int C, bool QUANT>
 __global__ __launch_bounds__(threads_of<W>, C <= 2 ? 8 : 1) void k_add_rms_norm(const NormArgs a, const KPad pad, int64_t row0) {
     __shared__ float part[threads_of<W> / 64][1];
@@ -269,7 +269,10 @@ Split split_of(int64_t K) {
 hipError_t launch_add_rms_norm(const NormArgs& a, bool quantize, hipStream_t stream) {
     int cus = 0;
     if (hipError_t e = device_cus(&cus); e != hipSuccess) return e;
-    const Split sp = split_of(a.K);
+    // Rows of 4097 to 8192: four workgroups of 8 wavefronts on a CU get further than two of 16 that meet at barriers, us, inputs in no cache: 4096 x 6144 fused 44.2 -> 36.2, alone
+    // 42.1 -> 40.4, 4096 x 8192 51.3 -> 46.5, 52.8 -> 51.0, with a residual in fp32 75.9 -> 76.2.  (Fewer wavefronts for shorter rows: 1 x 4096 3.0 -> 3.5.)
+    Split sp = split_of(a.K);
+    if (sp.w == 16 && sp.c == 1) sp = {8, 2};
     constexpr int64_t most = int64_t(1) << 21;          // workgroups of a launch, which has less than 2^32 threads
     const KPad pad = KPad::of(quantize && a.tiled, a.codes, a.scales, a.M, a.K);
     switch (sp.w * 16 + sp.c) {
@@ -282,7 +285,7 @@ hipError_t launch_add_rms_norm(const NormArgs& a, bool quantize, hipStream_t str
             else hipLaunchKernelGGL((k_add_rms_norm<W, C, false>), grid, block, 0, stream, a, pad, row);                                           \
         }                                                                                                                                          \
         break;
-        BRQ_NORM(1, 1) BRQ_NORM(2, 1) BRQ_NORM(4, 1) BRQ_NORM(8, 1) BRQ_NORM(16, 1) BRQ_NORM(16, 2) BRQ_NORM(16, 4)
+        BRQ_NORM(1, 1) BRQ_NORM(2, 1) BRQ_NORM(4, 1) BRQ_NORM(8, 1) BRQ_NORM(8, 2) BRQ_NORM(16, 2) BRQ_NORM(16, 4)
 #undef BRQ_NORM
         default: return hipErrorInvalidValue;
     }
