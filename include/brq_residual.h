@@ -28,7 +28,7 @@ extern "C" {
  *     y[m][k] = h[m][k] / sqrt(mean_k h[m][k]^2 + eps) * w[k]     of the rounded h; rounded once to ydt
  * in fp32.  res NULL: h = x, and `h` must be NULL (rdt and ldr are not looked at).  h NULL: the sum is not
  * wanted.  w: [K] fp32, 16-byte aligned, or NULL (no weight).  eps >= 0 and not NaN; with eps = 0 a row of
- * zeros comes out as NaN.  The sum of a row's squares has to be finite in fp32.
+ * zeros comes out as NaN, and one whose squares vanish in fp32 as infinities.  The sum of a row's squares has to be finite in fp32.
  * x [M][ldx] of xdt, res [M][ldr] and h [M][ldh] of rdt, y [M][ldy] of ydt.  K <= 32768.
  */
 brq_status brq_add_rms_norm(const void* x, brq_dtype xdt, int64_t ldx, const void* res, brq_dtype rdt,
