@@ -316,8 +316,9 @@ __global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm_backward(const N
         in[c] = kc[c] < n;
         kc[c] = min(kc[c], n - 1);
     }
-    // registers: one chunk a lane leaves room for the weight and all of the next row, more for neither
-    constexpr bool AHEAD = C == 1;
+    // registers: one chunk a lane leaves room for the weight and all of the next row, more for neither, four not for gy either: asked for again, from the L2 (2048 x 20000
+    // 413 -> 143 us, 333 x 32768 92 -> 45; h from there too 149, 47)
+    constexpr bool AHEAD = C == 1, KEEP = C <= 2;          // gy stays
     Raw<C> rh, rg, rd;
     auto fetch = [&](int64_t first) __attribute__((always_inline)) {
         const int64_t row = min(first + wave / W, a.M - 1);
@@ -326,8 +327,9 @@ __global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm_backward(const N
         if (a.gh.p) rd.load(a.gh.p + row * a.gh.pitch, a.gh.bf16, kc);
     };
     if constexpr (AHEAD) fetch((int64_t)blockIdx.x * rows_of<W>);
-    float w[C][8], dw[LDS ? 1 : C][8] = {};
-    if (AHEAD && a.w) load_weight(a.w, kc, w);
+    float w[KEEP ? C : 1][8], dw[LDS ? 1 : C][8] = {};
+    if constexpr (AHEAD)
+        if (a.w) load_weight(a.w, kc, w);
     // LDS: where nothing else is left for them, this lane's sums lie there: 16 bytes of a lane next to its neighbours', halves apart
     float* const mine_lds = shared + threadIdx.x * 4;
     if constexpr (LDS) {
@@ -339,14 +341,14 @@ __global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm_backward(const N
     // (uniform over the workgroup: every thread meets every barrier of row_sums)
     for (int64_t first = (int64_t)blockIdx.x * rows_of<W>; first < a.M; first += (int64_t)gridDim.x * rows_of<W>) {
         const int64_t mine = first + wave / W, row = mine < a.M ? mine : a.M - 1;
-        float h[C][8], g[C][8], sums[2] = {0.0f, 0.0f};
+        float h[C][8], g[KEEP ? C : 1][8], sums[2] = {0.0f, 0.0f};
         if constexpr (AHEAD) {
             rh.widen(a.h.bf16, h);
             rg.widen(a.gy.bf16, g);
         } else {
             renew(kc);
             load_row(a.h, row, kc, h);
-            load_row(a.gy, row, kc, g);
+            if constexpr (KEEP) load_row(a.gy, row, kc, g);
         }
         [[maybe_unused]] const Raw<C> other = rd;
         const int64_t next = first + (int64_t)gridDim.x * rows_of<W>;
@@ -355,11 +357,12 @@ __global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm_backward(const N
         for (int c = 0; c < C; ++c) {
             float s = 0.0f, d = 0.0f;
             if constexpr (!AHEAD) __builtin_amdgcn_sched_barrier(0);
-            if (!AHEAD && a.w) load_chunk_weight(a.w, kc[c], w[c]);
+            if constexpr (!KEEP) load_one(a.gy.p + row * a.gy.pitch, a.gy.bf16, kc[c], g[0]);
+            if (!AHEAD && a.w) load_chunk_weight(a.w, kc[c], w[KEEP ? c : 0]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 s = __builtin_fmaf(h[c][i], h[c][i], s);
-                d = __builtin_fmaf(a.w ? g[c][i] * w[c][i] : g[c][i], h[c][i], d);
+                d = __builtin_fmaf(a.w ? g[KEEP ? c : 0][i] * w[KEEP ? c : 0][i] : g[KEEP ? c : 0][i], h[c][i], d);
             }
             sums[0] += in[c] ? s : 0.0f;
             sums[1] += in[c] ? d : 0.0f;
@@ -379,13 +382,17 @@ __global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm_backward(const N
             float o[8], t[8];
             if (!AHEAD && a.w) {            // once more, from the L2, instead of a register each meanwhile
                 asm volatile("" ::: "memory");
-                load_chunk_weight(a.w, kc[c], w[c]);
+                load_chunk_weight(a.w, kc[c], w[KEEP ? c : 0]);
+            }
+            if constexpr (!KEEP) {
+                asm volatile("" ::: "memory");
+                load_one(a.gy.p + row * a.gy.pitch, a.gy.bf16, kc[c], g[0]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float u = h[c][i] * r;
-                t[i] = live ? g[c][i] * u : 0.0f;
-                o[i] = r * ((a.w ? g[c][i] * w[c][i] : g[c][i]) - u * mean);
+                const float u = h[c][i] * r, gi = g[KEEP ? c : 0][i];
+                t[i] = live ? gi * u : 0.0f;
+                o[i] = r * ((a.w ? gi * w[KEEP ? c : 0][i] : gi) - u * mean);
                 if (a.gh.p) o[i] += d[c][i];
             }
             if (live) store_values(a.dh.p + row * a.dh.pitch, a.dh.bf16, kc[c], o);
