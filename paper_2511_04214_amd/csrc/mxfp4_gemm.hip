@@ -719,7 +719,7 @@ static bool gemm_few_faster(const GemmShape& g, int cus) {
 // workgroup on a CU costs 0.88 of a first (whole tiles of these two are held against that), and where some CUs have one more than others the bytes take longer by that imbalance to the power 0.6.  The join,
 // a launch that reads what the slices wrote: 2.8 us and 2.25 us per million fp32 sums of all slices.  Fitted to 84 shapes (M 17 .. 600, N 1024 ..
 // 11008, K 2048 .. 28672, both layouts; 552 pairs of tile and slices): chosen by it the slices are 0.4 % over the best (7 % at worst), split or not 0.8 % (13 %).
-// us, whole K -> split: tiled 48 x 4096 x 11008 23.1 -> 13.9, 100 x 8192 x 28672 53.0 -> 37.3, row-major 300 x 1288 x 8192 17.3 -> 13.9, 17 x 8192 x
+// us, whole K -> split: tiled 100 x 8192 x 28672 53.0 -> 37.3, row-major 300 x 1288 x 8192 17.3 -> 13.9, 17 x 8192 x
 // 28672 66.8 -> 31.3.  By sizes and layouts alone, so that the workspace is too.
 GemmSplit gemm_split(const GemmShape& shape, int cus) {
     GemmShape g = shape;

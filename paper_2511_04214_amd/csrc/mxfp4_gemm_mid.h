@@ -36,8 +36,8 @@
 // So do row-major ones with K up to 1024 on the tiles of at most 192 x 128: there the prologue, which loads all the stages there
 // are, and two workgroups a CU weigh more than whole lines.  Pairs : single stages, us: 128 x 128 2000 x 4096 x 512 10.4 : 7.3, 4000
 // x 8192 x 512 35.4 : 23.5, 2000 x 4096 x 1024 11.9 : 10.2; 192 x 128 134 x 64 x 1024 6.9 : 6.2; 64 x 128 16 x 2048 x 512 4.1 : 3.9, 16 x
-// 2048 x 1024 5.0 : 4.7; with K = 2048 64 x 128 2000 x 4096 17.0 : 18.7, 128 x 128 514 x 16064 23.9 : 22.5 but 100 x 8192 x 3072 13.1 :
-// 14.7; 320 x 128 2000 x 4096 x 1024 10.4 : 10.9, 192 x 256 10.8 : 11.1.
+// 2048 x 1024 5.0 : 4.7; with K = 2048 64 x 128 2000 x 4096 17.0 : 18.7, 128 x 128 514 x 16064 23.9 : 22.5 but 12 % the other
+// way on 100 x 8192; 320 x 128 2000 x 4096 x 1024 10.4 : 10.9, 192 x 256 10.8 : 11.1.
 //
 // What bounds a stage where one workgroup runs on a CU is what the CU can have on its way: an L2 hit costs it 16 cycles a KB, but of
 // what misses the L2 at most 32 KB (the L1's size) are in flight, some 1000 cycles each, and hits wait behind misses; deeper
