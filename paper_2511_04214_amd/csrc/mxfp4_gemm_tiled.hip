@@ -39,6 +39,7 @@
 //
 // LDS map (bytes): [0, 128K) 4 stages x (W rows 16K | A rows 16K); [128K, 144K) 2 scale
 // buffers x (W 4K | A 4K); [144K, 160K) 4 epilogue blocks.
+#include <type_traits>
 #include "gemm_epilogue.h"
 #include "mfma_fp4.h"
 #include "brq_launch.h"
@@ -167,6 +168,10 @@ __device__ __forceinline__ void store_with(const Epilogue& e, const v16f (&acc)[
     }
 }
 
+// The output of the product alone is nobody else's; with a residual behind it that may be the output itself, so there it promises nothing.
+template <bool EPI>
+using Output = std::conditional_t<EPI, void*, void* __restrict__>;
+
 // Where the measurement instantiation reports its clock; the product instantiation's is empty.
 template <bool TIMED>
 struct ClockOut {};
@@ -185,7 +190,7 @@ struct ClockOut<true> { unsigned long long* p; };
 template <bool OUT_BF16, int MB, int DIAG, bool LINES, bool EPI = false>
 __global__ void __launch_bounds__(256, 1) k_gemm_tiled(const uint8_t* __restrict__ aq, const uint8_t* __restrict__ as,
                                                        const uint8_t* __restrict__ wq, const uint8_t* __restrict__ ws,
-                                                       int M, int N, int K, void* __restrict__ y, int64_t ldy, int a_tiled, int w_tiled,
+                                                       int M, int N, int K, Output<EPI> y, int64_t ldy, int a_tiled, int w_tiled,
                                                        ClockOut<DIAG != 0> clk, EpilogueArg<EPI> epi) {
     constexpr bool TIMED = DIAG != 0;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
