@@ -8,8 +8,8 @@
  * of brq.h hold (device pointers, caller-owned buffers, nothing allocated, work enqueued on `stream`,
  * argument errors found on the host before anything is launched, K % 32 == 0, 16-byte aligned pointers and
  * row pitches), and these besides:
- *   - Outputs may not overlap inputs, except that a sum may replace a summand: an output of the same
- *     address, dtype and row pitch as the residual it adds (and, of the norm, as x).
+ *   - Outputs may not overlap inputs or one another, except that an output may take the place of an input matrix
+ *     where its function below says so: the same address, dtype and row pitch (anything else at that address is refused).
  *   - A workspace is one call's until that call's work is done: calls on one stream may share it, calls on two may not.
  *   - Infinities and NaN are not refused: they stay in their row (norms) or element (bias, residual).
  */
@@ -29,7 +29,7 @@ extern "C" {
  * in fp32.  res NULL: h = x, and `h` must be NULL (rdt and ldr are not looked at).  h NULL: the sum is not
  * wanted.  w: [K] fp32, 16-byte aligned, or NULL (no weight).  eps >= 0 and not NaN; with eps = 0 a row of
  * zeros comes out as NaN, and one whose squares vanish in fp32 as infinities.  The sum of a row's squares has to be finite in fp32.
- * x [M][ldx] of xdt, res [M][ldr] and h [M][ldh] of rdt, y [M][ldy] of ydt.  K <= 32768.
+ * x [M][ldx] of xdt, res [M][ldr] and h [M][ldh] of rdt, y [M][ldy] of ydt.  K <= 32768.  h and y may each take the place of x or of res.
  */
 brq_status brq_add_rms_norm(const void* x, brq_dtype xdt, int64_t ldx, const void* res, brq_dtype rdt,
                             int64_t ldr, int64_t M, int64_t K, const float* w, float eps, void* h, int64_t ldh,
@@ -40,8 +40,8 @@ brq_status brq_add_rms_norm(const void* x, brq_dtype xdt, int64_t ldx, const voi
  * the gradient gh that reaches h by the other way, through the residual stream (NULL: none):
  *     r = 1 / sqrt(mean h^2 + eps),   g = gy w,
  *     dh = r (g - h r^2 mean_k(g h)) + gh,      dw[k] = sum_m gy[m][k] h[m][k] r[m]
- * dh is the gradient of x and of res alike.  h, gh and dh are of hdt, gy of gdt; dh may be gh's buffer (the
- * same address and pitch).  dw: [K] fp32, set, not added to; NULL: not wanted (must be NULL where w is).
+ * dh is the gradient of x and of res alike.  h, gh and dh are of hdt, gy of gdt; dh may take the place of h, gy
+ * or gh.  dw: [K] fp32, set, not added to; NULL: not wanted (must be NULL where w is).
  * M = 0 sets it to zero.  Its sums are made in an order that depends on the sizes alone.
  * workspace: brq_add_rms_norm_backward_workspace bytes, 16-byte aligned; may be NULL where dw is.
  */
@@ -55,7 +55,7 @@ brq_status brq_add_rms_norm_backward_workspace(int64_t M, int64_t K, int64_t* by
  * The norm in front of the online step:
  *     brq_rotate_quantize_fused(y, B, signs)   with (h, y) = brq_add_rms_norm(x, res, w, eps) and y of ydt,
  * in one pass; y never visits memory.  Bit-identical to that two-call sequence of THIS library (ydt =
- * BRQ_BF16 rounds y to bf16 before the rotation; BRQ_F32 keeps the fp32 value).
+ * BRQ_BF16 rounds y to bf16 before the rotation; BRQ_F32 keeps the fp32 value).  h may take the place of x or of res.
  * B = 1 (no rotation; signs must then be NULL) or 8 ... 512: blocks that a wavefront holds.  Wider ones,
  * and rows above 32768: the two calls.
  */
@@ -70,8 +70,7 @@ brq_status brq_add_rms_norm_rotate_quantize_fused(const void* x, brq_dtype xdt, 
  *     y[m][n] = act(p[m][n] + bias[n]) + residual[m][n],     p the product of brq_mxfp4_gemm in fp32
  * evaluated in fp32 on the accumulators and rounded once to ydt.
  * bias: [N] fp32, 4-byte aligned, or NULL.  residual: [M][ldr] of rdt or NULL (rdt and ldr are then not looked
- * at); its address is a multiple of its element's size, its pitch free, and it may be y itself (same address,
- * dtype and pitch).  y's pitch is free (>= N) as in brq_mxfp4_gemm.
+ * at); its address is a multiple of its element's size, its pitch free, and y may take its place.  y's pitch is free (>= N) as in brq_mxfp4_gemm.
  * act of t:  BRQ_ACT_RELU  max(t, 0) (NaN stays NaN);   BRQ_ACT_SILU  t / (1 + exp(-t));
  *            BRQ_ACT_GELU  t/2 erfc(-t / sqrt 2)  (the exact one, not its tanh form)
  * workspace: brq_mxfp4_gemm_epilogue_workspace bytes (may be 0, then NULL; where nothing follows the product too),

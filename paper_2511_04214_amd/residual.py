@@ -72,7 +72,7 @@ def add_rms_norm(x, residual=None, weight=None, eps=1e-6, out_dtype=None, out=No
     """(y, h): h = x + residual in the residual's dtype, y = h / sqrt(mean h^2 + eps) * weight, a row at a time (brq_add_rms_norm).
 
     x, residual [M, K]; weight fp32 [K] (None: none).  y is of out_dtype (None: x's).  h is None without a residual, and where neither
-    h_out nor want_h asks for it.  h_out may be the residual itself, or x where their dtypes agree."""
+    h_out nor want_h asks for it.  h_out and out may each be x or the residual itself, where dtypes agree (not both the same)."""
     r = _native("add_rms_norm", stream, x, residual, weight, eps, out_dtype, out, h_out, want_h)
     if r is not None:
         return r
@@ -97,8 +97,8 @@ def add_rms_norm_backward_workspace(M, K):
 
 def add_rms_norm_backward(h, gy, gh=None, weight=None, eps=1e-6, dh=None, workspace=None, stream=None):
     """(dh, dw) from the sum h of add_rms_norm (x where there was no residual), the gradient gy of its y and the gradient gh that h has
-    from elsewhere (None: none) (brq_add_rms_norm_backward).  dh, of h's dtype, is the gradient of x and of the residual; it may be gh.
-    dw is fp32 [K], None without a weight."""
+    from elsewhere (None: none) (brq_add_rms_norm_backward).  dh, of h's dtype, is the gradient of x and of the residual; it may be h, gh, or gy where
+    dtypes agree.  dw is fp32 [K], None without a weight."""
     r = _native("add_rms_norm_backward", stream, h, gy, gh, weight, eps, dh, workspace)
     if r is not None:
         return r
