@@ -101,6 +101,16 @@ brq_status brq_diag_mxfp4_gemm_on(int32_t route, const uint8_t* aq, const uint8_
                                   brq_dtype ydt, int64_t ldy, void* stream);
 
 /*
+ * *route, *slices = what brq_mxfp4_gemm_epilogue (brq_residual.h) takes on a device of `cus` compute units, with an output that
+ * begins on a 128-byte line: the kernel, and into how many slices it is split along K (1: not split).  bias, residual: whether there is
+ * one; act: a brq_activation.  Host arithmetic only.  BRQ_ERR_LAUNCH: the choice is a kernel that would not take the shape (there is
+ * no such shape).
+ */
+brq_status brq_diag_mxfp4_gemm_epilogue_route(brq_layout a_layout, brq_layout w_layout, int64_t M, int64_t N, int64_t K,
+                                              int32_t bias, int32_t act, int32_t residual, brq_dtype ydt, int64_t ldy,
+                                              int64_t cus, int32_t* route, int32_t* slices);
+
+/*
  * brq_mxfp4_gemm_epilogue (brq_residual.h) on the kernel `route`, also where nothing follows the product; BRQ_ERR_SHAPE where that
  * kernel does not take the shape, or takes no epilogue.  slices > 1 (BRQ_GEMM_64x128 and BRQ_GEMM_128x128, 2 to 16 slices of at least
  * 1024 of K): split along K, with a workspace of slices * M * ceil4(N) * 4 bytes.

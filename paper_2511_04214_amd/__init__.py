@@ -27,7 +27,7 @@ EXPORTS = ["brq_init", "brq_block_rotate", "brq_operand_bytes", "brq_mxfp4_quant
            "brq_diag_mxfp4_gemm_on", "brq_qk_norm_rope", "brq_qk_norm_rope_backward", "brq_qk_norm_rope_backward_workspace", "brq_kv4_page_bytes",
            "brq_kv4_append", "brq_kv4_read", "brq_kv4_attention", "brq_kv4_attention_workspace", "brq_kv4_pages_workspace", "brq_kv4_pages_copy",
            "brq_kv4_pages_fork", "brq_kv4_pages_free", "brq_kv4_pages_reserve", "brq_kv4_pages_compact", "brq_diag_kv4_attention_route",
-           "brq_add_rms_norm", "brq_add_rms_norm_backward", "brq_add_rms_norm_backward_workspace", "brq_add_rms_norm_rotate_quantize_fused", "brq_mxfp4_gemm_epilogue", "brq_mxfp4_gemm_epilogue_workspace", "brq_diag_mxfp4_gemm_epilogue_on",
+           "brq_add_rms_norm", "brq_add_rms_norm_backward", "brq_add_rms_norm_backward_workspace", "brq_add_rms_norm_rotate_quantize_fused", "brq_mxfp4_gemm_epilogue", "brq_mxfp4_gemm_epilogue_workspace", "brq_diag_mxfp4_gemm_epilogue_on", "brq_diag_mxfp4_gemm_epilogue_route",
            "brq_strerror", "brq_version"]
 
 _lib = None
@@ -553,5 +553,5 @@ from .attention import (KV4_PAGE, KV4_ROUTES, diag_kv4_attention_route, kv4_appe
                         qk_norm_rope_backward, qk_norm_rope_backward_workspace)
 from . import residual as _residual            # noqa: E402
 from .residual import (ACTIVATIONS, EPILOGUE_ROUTES, add_rms_norm, add_rms_norm_backward, add_rms_norm_backward_workspace,  # noqa: E402,F401
-                       add_rms_norm_rotate_quantize_fused, diag_mxfp4_gemm_epilogue_on, mxfp4_gemm_epilogue,
+                       add_rms_norm_rotate_quantize_fused, diag_mxfp4_gemm_epilogue_on, diag_mxfp4_gemm_epilogue_route, mxfp4_gemm_epilogue,
                        mxfp4_gemm_epilogue_workspace)

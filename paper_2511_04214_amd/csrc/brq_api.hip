@@ -313,6 +313,28 @@ brq_status brq_diag_mxfp4_gemm_route(brq_layout a_layout, brq_layout w_layout, i
     return BRQ_OK;
 }
 
+brq_status brq_diag_mxfp4_gemm_epilogue_route(brq_layout a_layout, brq_layout w_layout, int64_t M, int64_t N, int64_t K, int32_t bias,
+                                              int32_t act, int32_t residual, brq_dtype ydt, int64_t ldy, int64_t cus, int32_t* route,
+                                              int32_t* slices) {
+    alignas(16) static const uint8_t operand[16] = {};
+    brq_status st = brq::check_gemm(operand, operand, a_layout, operand, operand, w_layout, M, N, K, operand, ydt, ldy);
+    if (st != BRQ_OK) return st;
+    if (act < brq::ACT_NONE || act > brq::ACT_GELU) return BRQ_ERR_ACTIVATION;
+    if (!route || !slices) return BRQ_ERR_NULL;
+    if (M == 0 || N == 0 || cus < 1 || cus >= (int64_t(1) << 31)) return BRQ_ERR_SHAPE;
+    brq::GemmShape g{M, N, K, a_layout == BRQ_LAYOUT_TILED, w_layout == BRQ_LAYOUT_TILED, ydt == BRQ_BF16, ldy, 0};
+    g.epilogue = bias || act != brq::ACT_NONE || residual;
+    g.exponential = act == brq::ACT_SILU || act == brq::ACT_GELU;
+    g.residual = residual != 0;
+    const brq::GemmChoice c = brq::gemm_choice(g, (int)cus);
+    // (what the launch would answer to a kernel that does not take the shape, or is not there)
+    if (!brq::gemm_route_supported(c.route, g) || (c.route == brq::ROUTE_FEW && !brq::few_gemm_has_kernel(g, (int)cus))) return BRQ_ERR_LAUNCH;
+    if (c.slices > 1 && !brq::gemm_split_supported(g, {c.route == brq::ROUTE_ONE_TILE ? 64 : 128, c.slices})) return BRQ_ERR_LAUNCH;
+    *route = c.route;
+    *slices = c.slices;
+    return BRQ_OK;
+}
+
 brq_status brq_diag_mxfp4_gemm_on(int32_t route, const uint8_t* aq, const uint8_t* as, brq_layout a_layout, const uint8_t* wq,
                                   const uint8_t* ws, brq_layout w_layout, int64_t M, int64_t N, int64_t K, void* y,
                                   brq_dtype ydt, int64_t ldy, void* stream) {

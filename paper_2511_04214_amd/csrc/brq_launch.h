@@ -143,6 +143,7 @@ hipError_t launch_gemm_mid_with(int tile, const Operand& a, const Operand& w, in
 
 // Up to 64 rows, K of whole superstages (mxfp4_gemm_few.hip).
 bool few_gemm_supported(const GemmShape& g);
+bool few_gemm_has_kernel(const GemmShape& g, int cus);      // whether the launch below finds one: host arithmetic
 hipError_t launch_gemm_few(const Operand& a, const Operand& w, const GemmShape& g, void* y, const Epilogue& epi, hipStream_t s);
 
 // The one-tile kernels split along K, with what follows the product where the slices are joined (mxfp4_gemm_split.hip).
@@ -154,6 +155,10 @@ bool gemm_split_supported(const GemmShape& g, const GemmSplit& s);
 hipError_t launch_gemm_split(const GemmSplit& sp, const Operand& a, const Operand& w, const GemmShape& g, void* y, void* workspace,
                              const Epilogue& epi, hipStream_t s);
 hipError_t setup_gemm_split();
+
+// What launch_mxfp4_gemm takes: host arithmetic.
+struct GemmChoice { int route, slices; };     // slices > 1: that tile's kernel split along K
+GemmChoice gemm_choice(const GemmShape& g, int cus);
 
 // Tiled -> row-major copy of a quantized operand.
 hipError_t launch_to_rowmajor(const uint8_t* codes_t, const uint8_t* scales_t, int64_t rows, int64_t K,

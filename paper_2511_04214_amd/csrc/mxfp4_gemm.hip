@@ -818,6 +818,12 @@ int gemm_route(const GemmShape& g, int cus) {
     return t >= 0 ? t : g.M <= 16 ? ROUTE_SKINNY : any_k(g) ? ROUTE_ANY_K : ROUTE_GENERAL;
 }
 
+GemmChoice gemm_choice(const GemmShape& g, int cus) {
+    if (g.epilogue)
+        if (const GemmSplit sp = gemm_split(g, cus); sp.slices > 1) return {sp.rows == 64 ? ROUTE_ONE_TILE : ROUTE_ONE_TILE + 1, sp.slices};
+    return {gemm_route(g, cus), 1};
+}
+
 // The kernels of this file; EPI: with what follows the product.
 template <bool EPI>
 static hipError_t launch_here(int route, const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, EpilogueArg<EPI> epi) {
@@ -860,9 +866,9 @@ hipError_t launch_gemm_route(int route, const Operand& a, const Operand& w, cons
 hipError_t launch_mxfp4_gemm(const Operand& a, const Operand& w, const GemmShape& g, void* y, hipStream_t s, const Epilogue* epi, void* workspace) {
     int cus = 0;
     if (hipError_t e = device_cus(&cus); e != hipSuccess) return e;      // (also the per-device kernel set-up)
-    if (epi)
-        if (const GemmSplit sp = gemm_split(g, cus); sp.slices > 1) return launch_gemm_split(sp, a, w, g, y, workspace, *epi, s);
-    return launch_gemm_route(gemm_route(g, cus), a, w, g, y, s, epi);
+    const GemmChoice c = gemm_choice(g, cus);
+    if (epi && c.slices > 1) return launch_gemm_split({c.route == ROUTE_ONE_TILE ? 64 : 128, c.slices}, a, w, g, y, workspace, *epi, s);
+    return launch_gemm_route(c.route, a, w, g, y, s, epi);
 }
 
 }  // namespace brq

@@ -149,6 +149,18 @@ FewKern few_kern_of(int tiles, int64_t count) { return tiles == 2 ? few_kern<2, 
 
 int64_t superstages(const GemmShape& g) { return (g.padded_k() / 512 + WAVES - 1) / WAVES; }
 
+// Tiles of columns: as many as a round of the chip needs, at most 3, and of two tiles of rows one where K is one superstage a wavefront and a CU so holds more than one
+// workgroup (32 x 8192 x 4096 7.6 with two -> 6.6 us, 32 x 6144 x 4096 6.8 -> 6.5).
+struct FewChoice { FewKern kern; int cols; };      // kern null: there is none
+FewChoice few_choice(const GemmShape& g, int cus) {
+    const int64_t count = superstages(g);
+    const int tiles = (int)((g.M + 15) / 16);
+    int cols = tiles == 1 || g.N <= 16 * (int64_t)cus ? 1 : g.N <= 32 * (int64_t)cus ? 2 : 3;
+    if (tiles == 2 && cols == 2 && count == 1 && g.K > 2048) cols = 1;
+    while (cols > 1 && count > most_of(tiles, cols)) --cols;
+    return {tiles == 1 ? few_kern<1, 1>(count) : cols == 1 ? few_kern_of<1>(tiles, count) : cols == 2 ? few_kern_of<2>(tiles, count) : few_kern_of<3>(tiles, count), cols};
+}
+
 }  // namespace
 
 bool few_gemm_supported(const GemmShape& g) {
@@ -156,17 +168,14 @@ bool few_gemm_supported(const GemmShape& g) {
     return g.M <= 16 || superstages(g) <= most_of((int)((g.M + 15) / 16), 1);
 }
 
-// Tiles of columns: as many as a round of the chip needs, at most 3, and of two tiles of rows one where K is one superstage a wavefront and a CU so holds more than one
-// workgroup (32 x 8192 x 4096 7.6 with two -> 6.6 us, 32 x 6144 x 4096 6.8 -> 6.5).
+bool few_gemm_has_kernel(const GemmShape& g, int cus) { return few_choice(g, cus).kern != nullptr; }
+
 hipError_t launch_gemm_few(const Operand& a, const Operand& w, const GemmShape& g, void* y, const Epilogue& epi, hipStream_t s) {
     int cus = 0;
     if (hipError_t e = device_cus(&cus); e != hipSuccess) return e;
-    const int64_t count = superstages(g);
-    const int tiles = (int)((g.M + 15) / 16);
-    int cols = tiles == 1 || g.N <= 16 * (int64_t)cus ? 1 : g.N <= 32 * (int64_t)cus ? 2 : 3;
-    if (tiles == 2 && cols == 2 && count == 1 && g.K > 2048) cols = 1;
-    while (cols > 1 && count > most_of(tiles, cols)) --cols;
-    const FewKern kern = tiles == 1 ? few_kern<1, 1>(count) : cols == 1 ? few_kern_of<1>(tiles, count) : cols == 2 ? few_kern_of<2>(tiles, count) : few_kern_of<3>(tiles, count);
+    const FewChoice c = few_choice(g, cus);
+    const FewKern kern = c.kern;
+    const int cols = c.cols;
     if (!kern) return hipErrorInvalidValue;
     hipLaunchKernelGGL(kern, dim3((uint32_t)((g.N + 16 * cols - 1) / (16 * cols))), dim3(64 * WAVES), 0, s, a.codes, a.scales, (int)a.tiled, w.codes, w.scales, (int)w.tiled,
                        (int)g.M, (int)g.N, (int)g.K, y, g.ldy, epi);

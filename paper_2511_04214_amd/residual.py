@@ -28,6 +28,7 @@ def declare(L):
             ("add_rms_norm_backward_workspace", [i64, i64, ctypes.POINTER(i64)]),
             ("add_rms_norm_rotate_quantize_fused", [vp, i32, i64, vp, i32, i64, i64, i64, vp, f32, vp, i64, i32, i64, vp, vp, vp, i32, vp]),
             ("diag_mxfp4_gemm_epilogue_on", [i32, i32, vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, vp, i32, i64, vp, i64, vp]),
+            ("diag_mxfp4_gemm_epilogue_route", [i32, i32, i64, i64, i64, i32, i32, i32, i32, i64, i64, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]),
             ("mxfp4_gemm_epilogue", [vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, vp, i32, i64, vp, i64, vp]),
             ("mxfp4_gemm_epilogue_workspace", [i32, i32, i64, i64, i64, ctypes.POINTER(i64)])):
         f = getattr(L, "brq_" + name)
@@ -182,6 +183,17 @@ def mxfp4_gemm_epilogue(aq, as_, wq, ws, bias=None, activation=None, residual=No
                                                    _array(workspace, "workspace", torch.uint8, (None,), True),
                                                    0 if workspace is None else workspace.numel(), _brq._stream(stream)))
     return y
+
+
+def diag_mxfp4_gemm_epilogue_route(M, N, K, a_layout="rowmajor", w_layout="rowmajor", bias=False, activation=None, residual=False, out_dtype=torch.float32,
+                                   ldy=None, cus=256):
+    """(kernel, slices) that mxfp4_gemm_epilogue takes on a device of `cus` compute units: one of EPILOGUE_ROUTES, split along K into so many
+    (brq_diag_mxfp4_gemm_epilogue_route; needs no GPU)."""
+    r, n = ctypes.c_int32(), ctypes.c_int32()
+    _brq._check(_brq.lib().brq_diag_mxfp4_gemm_epilogue_route(
+        _brq._layout_code(a_layout), _brq._layout_code(w_layout), M, N, K, bool(bias), _activation(activation), bool(residual),
+        _brq.BRQ_BF16 if out_dtype == torch.bfloat16 else _brq.BRQ_F32, N if ldy is None else ldy, cus, ctypes.byref(r), ctypes.byref(n)))
+    return EPILOGUE_ROUTES[r.value], n.value
 
 
 def diag_mxfp4_gemm_epilogue_on(route, aq, as_, wq, ws, out, K, bias=None, activation=None, residual=None, a_layout="rowmajor",
