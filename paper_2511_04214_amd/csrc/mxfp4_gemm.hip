@@ -692,19 +692,25 @@ static int pick_tile(const GemmShape& g, int cus, float* us = nullptr) {
 // 0.67, 16384 0.58 / 0.64; N 6144 to 12288, K = 1024 1.07 / 1.15, 2048 0.95 / 0.98, 4096 0.76 / 0.84, 8192 0.92 / 0.94, 16384 1.00 / 1.10; N from 16384,
 // K = 2048 1.07 / 1.13, 4096 0.86 / 0.97, 8192 1.03 / 1.10.  Row-major, N <= 4096, K = 1024 1.02 / 1.13, 2048 0.86 / 0.96, from 4096 0.62 / 0.78; N above,
 // K = 2048 1.20 / 1.49, from 4096 1 / 4 / 8 / 16 rows 0.89 / 0.95 / 1.03 / 1.12.
-// 17 to 64 rows, against one-tile kernels and those split along K, 24 / 32 / 48 / 64 rows (all on either side of a border, 420 shapes in all): tiled, N = 4096, K = 512 0.80 / 0.80 / 0.96 /
-// 1.07, 1024 0.73 / 0.74 / 0.87 / 1.00, 4096 0.55 / 0.54 / 0.59 / 0.63, 8192 0.67 / 0.68 / 0.75 / 0.81, 11264 0.74 / 0.76 / 0.86 / 0.93, 16384 0.85 / 0.88 / 0.99 / 1.02; N = 8192, K = 1024
-// 0.95 / 0.96 / 1.09 / 1.23, 2048 0.86 / 0.87 / 0.98 / 1.10, 4096 0.67 / 0.67 / 0.85 / 0.93, 8192 0.85 / 0.84 / 0.88 / 0.92, 16384 0.86 / 0.88 / 1.04; N = 12288, K = 2048 1.03 / 1.06 /
-// 1.19 / 1.33, 4096 0.79 / 0.80 / 0.86 / 0.91, 8192 0.86 / 0.88 / 0.86 / 0.90, 11264 0.92 / 0.93; N = 14336 0.9 to 2.  Row-major, N = 4096, K = 1024 0.89 / 0.93 / 1.13 / 1.33, 4096
-// 0.62 / 0.66 / 0.74 / 0.80, 8192 0.81 / 0.83 / 1.02 / 1.15; N = 8192, K = 2048 0.98 / 1.01 / 1.15 / 1.33, 4096 0.73 / 0.81 / 0.89 / 1.01, 8192 0.91 / 0.94 / 1.00 / 1.15; N = 12288,
-// K = 4096 0.75 / 0.76 / 0.81 / 0.91, 8192 0.90 / 0.93 / 1.05.
+// 17 to 64 rows: a window of K, its ends where the kernel's time meets that of what the call takes else (one-tile kernels, whole or split along K).  Its time over theirs, with
+// a bias, bf16 out, weights in no cache, 1524 shapes (M 17 .. 64, N 1000 .. 12288, K 512 .. 16384 as far as there are kernels): last K outside, first and last inside, first
+// outside, and the mean over the window.
+//                        up to 32 rows                                               48                                                         64
+//   tiled     N <=  4096            512 0.80, 16384 0.91                  0.70                512 0.94, 12288 0.89                  0.78     512 1.05, 1024 0.95, 8192 0.86             0.79
+//             N <=  8192   512 1.02, 1024 0.92, 16384 0.93                0.84     1024 1.03, 1536 0.94, 12288 0.99                 0.87     1536 1.02, 2048 0.95, 8192 0.96            0.88
+//             N <= 12288   1536 0.99, 2048 0.95, 12288 0.92, 13824 1.33   0.89     2048 1.06, 2560 0.97, 8192 0.94, 8704 1.33       0.93     2560 1.04, 3584 0.92, 8192 0.95            0.95
+//   row-major N <=  4096   512 0.97, 1024 0.87, 12288 0.96, 13824 1.01    0.76     1024 1.07, 1536 0.88, 8192 1.01, 8704 1.14       0.83     1536 1.00, 2048 0.95, 4096 0.83, 4608 1.09 0.82
+//             N <=  8192   1024 1.05, 1536 0.89, 8192 0.93, 8704 1.03     0.85     2048 0.97, 2560 0.80, 7168 0.93, 8192 1.04       0.85     2048 1.08, 2560 0.89, 4096 0.80, 4608 1.12 0.81
+//             N <= 12288   2048 1.00, 2560 0.84, 12288 0.96, 13824 1.48   0.91     2048 1.15, 2560 0.95, 7168 0.97, 8192 1.08       0.91     2560 1.04, 3584 0.87, 4096 0.87, 4608 1.19 0.87
+// (Up to 4096 a wavefront has one superstage: a second one ends the windows of many row-major rows.  Between two superstages and HBM's bound a window can be above 1: tiled 64 x 12288 x 4608 1.14.)
+// So chosen a call takes 0.3 % more than the better of the two on average, 15 % at worst.
 static bool gemm_few_faster(const GemmShape& g, int cus) {
     if (!gemm_route_supported(ROUTE_FEW, g)) return false;
     const bool tiled = g.a_tiled && g.w_tiled;
     if (g.M > 16) {
         static const struct { int64_t from, to; } K[2][3][3] = {      // [tiled][columns][tiles of 16 rows, from 2 on]
-            {{{1024, 8192}, {2048, 4096}, {4096, 4096}}, {{4096, 8192}, {4096, 4096}, {1, 0}}, {{4096, 12288}, {4096, 6144}, {4096, 4096}}},
-            {{{512, 16384}, {512, 12288}, {1024, 8192}}, {{1024, 16384}, {2048, 12288}, {4096, 8192}}, {{4096, 12288}, {4096, 8192}, {4096, 8192}}}};
+            {{{1024, 12288}, {1536, 8192}, {2048, 4096}}, {{1536, 8192}, {2560, 7168}, {2560, 4096}}, {{2560, 12288}, {2560, 7168}, {3584, 4096}}},
+            {{{512, 16384}, {512, 12288}, {1024, 8192}}, {{1024, 16384}, {1536, 12288}, {2048, 8192}}, {{2048, 12288}, {2560, 8192}, {3584, 8192}}}};
         if (g.N > 48 * (int64_t)cus) return false;
         const auto& k = K[tiled][g.N <= 16 * (int64_t)cus ? 0 : g.N <= 32 * (int64_t)cus ? 1 : 2][(g.M - 1) / 16 - 1];
         return g.K >= k.from && g.K <= k.to;

@@ -40,6 +40,29 @@ def test_choice(shape, layout, want):
     assert choice(*shape, layout=layout) == want
 
 
+# [layout][columns][rows]: the first and last K that the few-rows kernel takes; tiled, and for long K, up to where there are kernels
+WINDOWS = {"rowmajor": {4096: {32: (1024, 12288), 48: (1536, 8192), 64: (2048, 4096)}, 8192: {32: (1536, 8192), 48: (2560, 7168), 64: (2560, 4096)},
+                        12288: {32: (2560, 12288), 48: (2560, 7168), 64: (3584, 4096)}},
+           "tiled": {4096: {32: (512, 16384), 48: (512, 12288), 64: (1024, 8192)}, 8192: {32: (1024, 16384), 48: (1536, 12288), 64: (2048, 8192)},
+                     12288: {32: (2048, 12288), 48: (2560, 8192), 64: (3584, 8192)}}}
+
+
+@pytest.mark.parametrize("layout", ["tiled", "rowmajor"])
+def test_few_rows_windows(layout):
+    """17 to 64 rows: every K of a window, which is no single size, and none beside it."""
+    Ks = sorted({*range(512, 20000, 1024), 1024, 2048, 4096, 5120, 7168, 8192, 12288, 16384})
+    for top, by_rows in WINDOWS[layout].items():
+        for rows, (first, last) in by_rows.items():
+            assert first < last
+            for M in (rows - 15, rows):
+                for N in (top - 4095, top - 1000, top):
+                    for K in Ks:
+                        assert (choice(M, N, K, layout=layout)[0] == "few") == (first <= K <= last), (M, N, K)
+    for M in (17, 32, 48, 64):
+        for K in Ks:
+            assert choice(M, 12289, K, layout=layout)[0] != "few"
+
+
 def test_nothing_behind_is_the_product_alone():
     for shape in ((1, 4096, 4096), (48, 4096, 4096), (100, 8192, 28672), (4096, 6144, 4096)):
         for layout in ("tiled", "rowmajor"):
