@@ -56,8 +56,8 @@ brq_status brq_add_rms_norm_backward_workspace(int64_t M, int64_t K, int64_t* by
  *     brq_rotate_quantize_fused(y, B, signs)   with (h, y) = brq_add_rms_norm(x, res, w, eps) and y of ydt,
  * in one pass; y never visits memory.  Bit-identical to that two-call sequence of THIS library (ydt =
  * BRQ_BF16 rounds y to bf16 before the rotation; BRQ_F32 keeps the fp32 value).  h may take the place of x or of res.
- * B = 1 (no rotation; signs must then be NULL) or 8 ... 512: blocks that a wavefront holds.  Wider ones,
- * and rows above 32768: the two calls.
+ * B = 1 (no rotation; signs must then be NULL) or 8 ... 512: blocks that a wavefront holds.  Wider ones: the
+ * two calls.  K <= 32768, as the norm alone.
  */
 brq_status brq_add_rms_norm_rotate_quantize_fused(const void* x, brq_dtype xdt, int64_t ldx, const void* res,
                                                   brq_dtype rdt, int64_t ldr, int64_t M, int64_t K, const float* w,
@@ -67,8 +67,11 @@ brq_status brq_add_rms_norm_rotate_quantize_fused(const void* x, brq_dtype xdt, 
 
 /*
  * The W4A4 product with what follows it:
- *     y[m][n] = act(p[m][n] + bias[n]) + residual[m][n],     p the product of brq_mxfp4_gemm in fp32
- * evaluated in fp32 on the accumulators and rounded once to ydt.
+ *     y[m][n] = act(p[m][n] + bias[n]) + residual[m][n],     p[m][n] = sum_k deq(a)[m][k] deq(w)[n][k] in fp32
+ * evaluated in fp32 on the accumulators and rounded once to ydt.  p is not bit for bit brq_mxfp4_gemm's: up to 64 rows, and few
+ * tiles with a long K, go to kernels that add its terms in another order (no less exact), so the last bits of a row may differ with M
+ * too.  The same call gives the same bits.  With nothing behind the product (no bias, BRQ_ACT_NONE, no residual) the call is
+ * brq_mxfp4_gemm, its kernels and its bits.
  * bias: [N] fp32, 4-byte aligned, or NULL.  residual: [M][ldr] of rdt or NULL (rdt and ldr are then not looked
  * at); its address is a multiple of its element's size, its pitch free, and y may take its place.  y's pitch is free (>= N) as in brq_mxfp4_gemm.
  * act of t:  BRQ_ACT_RELU  max(t, 0) (NaN stays NaN);   BRQ_ACT_SILU  t / (1 + exp(-t));
