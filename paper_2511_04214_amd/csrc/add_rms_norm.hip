@@ -317,7 +317,8 @@ __global__ __launch_bounds__(threads_of<W>) void k_add_rms_norm_backward(const N
         kc[c] = min(kc[c], n - 1);
     }
     // registers: one chunk a lane leaves room for the weight and all of the next row, more for neither, four not for gy either: asked for again, from the L2 (2048 x 20000
-    // 413 -> 143 us, 333 x 32768 92 -> 45; h from there too 149, 47)
+    // 413 -> 143 us, 333 x 32768 92 -> 45; h from there too 149, 47).  Four still do not fit the 128 registers that 1024 threads leave a lane: 42 are spilled to scratch
+    // memory, 76 bytes a lane, and 2048 x 20000 takes 143 to 147 us for 57 that its 328 MB do (fp32 201 for 113).
     constexpr bool AHEAD = C == 1, KEEP = C <= 2;          // gy stays
     Raw<C> rh, rg, rd;
     auto fetch = [&](int64_t first) __attribute__((always_inline)) {
